@@ -28,7 +28,8 @@
  *     buffers on different streams race.
  *   - err_flag (optional, may be NULL): a caller-owned device int32 that kernels OR with
  *     CG_FLAG_* bits when they meet a non-finite input, a side-info value that overflows
- *     binary16, or an append position outside the cache.  The library never clears it.
+ *     binary16, an append position outside the cache, or a page pool without a free page.  The
+ *     library never clears it.
  *   - Device pointers must be 16-byte aligned (CG_ERR_ALIGN otherwise).  A view with T = 0
  *     touches no memory and may carry a NULL pointer.
  *   - Tensors: element (l, b, h, t, c) of a cg_kv_view sits at
@@ -99,7 +100,7 @@ enum {
 };
 
 /* device error-flag bits */
-enum { CG_FLAG_NONFINITE = 1, CG_FLAG_SIDE_OVERFLOW = 2, CG_FLAG_POS_RANGE = 4 };
+enum { CG_FLAG_NONFINITE = 1, CG_FLAG_SIDE_OVERFLOW = 2, CG_FLAG_POS_RANGE = 4, CG_FLAG_POOL_EMPTY = 8 };
 
 /* gauge kinds (section 4.1 and the controls of section 4.3) */
 enum {
@@ -161,6 +162,33 @@ typedef struct cg_page_table {
   const int32_t* pages;
   int32_t max_pages, page_size;
 } cg_page_table;
+
+/* Free pages of a pool of n_pages pages: a stack, free_pages[0 .. *free_count) (device int32, the
+ * newest on top), which kv_page_map pops and kv_page_release pushes. */
+typedef struct cg_page_pool {
+  int32_t* free_pages;  /* device [n_pages] */
+  int32_t* free_count;  /* device [1] */
+  int32_t n_pages;
+} cg_page_pool;
+
+/* Rotary positions.  Which channels make a pair: HALF (i, i + d_rot / 2), PAIRS (2 i, 2 i + 1). */
+enum { CG_ROPE_HALF = 0, CG_ROPE_PAIRS = 1 };
+/* Scaling of the frequencies f_i = base^(-2 i / d_rot) (radians per position) for contexts longer than
+ * the trained one: NONE; LINEAR f / factor (position interpolation); RAMP by the turns a pair makes over
+ * the trained length, t_i = train_len f_i / (2 pi): f (1 - w) / factor + f w with
+ * w = clamp((t_i - low) / (high - low), 0, 1). */
+enum { CG_ROPE_NONE = 0, CG_ROPE_LINEAR = 1, CG_ROPE_RAMP = 2 };
+typedef struct cg_rope {
+  int32_t d_rot, layout, scaling, train_len;  /* channels [0, d_rot) turn, the others stay; d_rot even, <= 256 */
+  double base, factor, low, high, amplitude;  /* amplitude: factor of the turned channels (1: a rotation) */
+} cg_rope;
+/* What kv_rope reads of it: turns per position of every pair as 64-bit fractions. */
+typedef struct cg_rope_plan {
+  int32_t d_rot, layout;
+  float amplitude;
+  int32_t reserved;
+  uint64_t step[128];
+} cg_rope_plan;
 
 /* Static message for a status code. */
 const char* cg_status_str(int32_t status);
@@ -360,6 +388,81 @@ int32_t kv_encode_paged(int32_t s, const cg_kv_view* X, const cg_page_table* pag
 int32_t kv_append_paged(int32_t l0, int32_t l1, const cg_kv_view* k_new, const cg_kv_view* v_new, const int32_t* pos,
                         const cg_page_table* pages, const void* G_dev, cg_gauge_shape shp, const cg_codec* codec,
                         const cg_cache* kc, const cg_cache* vc, int32_t* err_flag, void* stream);
+
+/* Tables and slots of one serving step from the rows' lengths, on the device.  Row b holds held[b]
+ * positions and adds add[b] tokens (device int32 [B]); the step's tokens are packed row after row.  Writes
+ *   lens[b]  held[b] + add[b]                                    (device int32 [B]; may be `held` itself)
+ *   cu[b]    the row's first packed token, cu[B] their number    (device int32 [B + 1])
+ *   pages    row b's entries [ceil(held / P), ceil(lens / P)), P = page_size, taken from the top of the pool's
+ *            stack, rows in order (device int32 [B][max_pages], the table of cg_page_table; other entries stay)
+ *   pos[i], slots[i]  position in its row of packed token i, and page * P + position mod P: where
+ *            kv_append_slots puts it (device int32 [N]; -1 for i >= cu[B])
+ * and the pool's free_count.  N: packed tokens there is room for.  Rows past the table's
+ * max_pages * P positions, negative lengths, and more than N tokens set CG_FLAG_POS_RANGE; a pool that
+ * runs out sets CG_FLAG_POOL_EMPTY and leaves -1 in the table.  Tokens without a page get slot -1, a negative
+ * add counts as 0, a row with a negative held takes no page.  page_size a multiple of 64;
+ * n_pages * page_size and max_pages * page_size below 2^31 (CG_ERR_CAPACITY).  Errors: CG_ERR_ARG,
+ * CG_ERR_SHAPE, CG_ERR_ALIGN, CG_ERR_CAPACITY, CG_ERR_DEVICE. */
+int32_t kv_page_map(const int32_t* held, const int32_t* add, int32_t B, const cg_page_pool* pool, int32_t* pages,
+                    int32_t max_pages, int32_t page_size, int32_t N, int32_t* cu, int32_t* lens, int32_t* pos,
+                    int32_t* slots, int32_t* err_flag, void* stream);
+
+/* Gives the pages of the rows with done[b] != 0 (device int32 [B]) back to the pool: the entries
+ * [0, ceil(lens[b] / page_size)) of their tables are pushed row after row (entries outside the pool are left
+ * out) and become -1, lens[b] becomes 0.  A stack that would pass n_pages (pages given back twice) sets
+ * CG_FLAG_POS_RANGE.  Errors: as kv_page_map. */
+int32_t kv_page_release(int32_t* lens, const int32_t* done, int32_t B, const cg_page_pool* pool, int32_t* pages,
+                        int32_t max_pages, int32_t page_size, int32_t* err_flag, void* stream);
+
+/* Host only: the plan of a rotation.  Errors: CG_ERR_ARG (odd or large d_rot, unknown enum, numbers that are
+ * not finite, base or factor not positive, RAMP without train_len > 0 and low < high). */
+int32_t rope_make(const cg_rope* rope, cg_rope_plan* plan);
+
+/* Rotary positions: y = x with channels [0, d_rot) of every token turned by its position,
+ *   (x_a, x_b) -> amplitude (x_a cos - x_b sin, x_a sin + x_b cos),   angle = pos f_i
+ * (angles exact to 2^-32 turns at any position, products and sums in binary32, one rounding).  x0, y0: views
+ * [L][B][H0][T][d] of one element type; x1, y1 (both or neither): views [L][B][H1][T][d] of the same type,
+ * turned by the same launch (queries and keys).  y may be x itself (same pointer and strides), else they must
+ * not overlap.  pos: device int32 [B][T]; a token with a negative position is left as it was.
+ * inverse != 0: the transposed map (turned back, the same amplitude): the gradient with respect to x of
+ * a gradient given for y.  Errors: CG_ERR_ARG, CG_ERR_SHAPE, CG_ERR_ALIGN, CG_ERR_UNSUPPORTED (d no multiple
+ * of 8 or above 256), CG_ERR_CAPACITY (2^31 or more tokens x channels / 2), CG_ERR_DEVICE. */
+int32_t kv_rope(const cg_rope_plan* plan, const cg_kv_view* x0, const cg_kv_view* y0, const cg_kv_view* x1,
+                const cg_kv_view* y1, const int32_t* pos, int32_t inverse, void* stream);
+
+/* Encode packed tokens through their slots (section 3, Z = G X, B_c = C(Z)), keys and values in one call:
+ * token i of the views k_new, v_new [l1 - l0][1][H][N][d] (view layer j is cache layer l0 + j) goes to position
+ * slots[i] mod P of page slots[i] / P of the pools kc, vc (P = their T_cap; slots: device int32 [N], as
+ * kv_page_map writes them).  A negative slot skips its token; a page outside the pool sets CG_FLAG_POS_RANGE and
+ * skips it; of two tokens with one slot either may stay.  Block-uniform with block_t = 1, or passthrough;
+ * P a multiple of 64, pages * P below 2^31.  Errors: as kv_append_paged. */
+int32_t kv_append_slots(int32_t l0, int32_t l1, const cg_kv_view* k_new, const cg_kv_view* v_new, const int32_t* slots,
+                        const void* G_dev, cg_gauge_shape shp, const cg_codec* codec, const cg_cache* kc,
+                        const cg_cache* vc, int32_t* err_flag, void* stream);
+
+/* Workspace bytes of kv_attend_chunk_paged (0: none needed, or invalid arguments). */
+size_t attend_chunk_workspace_bytes(cg_gauge_shape shp, int32_t nl, int32_t N, int32_t B, int32_t max_q, int32_t Hq,
+                                    int32_t max_pages, int32_t page_size, int32_t window, int32_t sinks);
+
+/* Attention of new tokens over paged caches that hold them already: chunks of prompts, single tokens, or both in
+ * one batch.  q, out: views [l1 - l0][1][Hq][N][d] (bf16 or binary32) of N packed tokens; row b's are
+ * [cu[b], cu[b + 1]) (device int32 [B + 1]), at most max_q of them.  With n_b tokens and lens[b] positions held
+ * (device int32 [B], the new tokens among them), its token i sits at p = lens[b] - n_b + i and
+ *     o = softmax(scale q Khat^T) Vhat  over the positions t <= p with
+ *                                       window == 0 or t > p - window or t < sinks,
+ * Khat, Vhat as kv_decode would return them in binary32.  The first `sinks` positions stay visible behind the
+ * window; window = 0: causal (sinks unused).  bf16 outputs are computed from binary16 operands with
+ * binary32 sums, binary32 outputs from operands of 22 bits.  Positions a token does not see do not reach its
+ * output, whatever their bytes decode to.  Tokens behind the last row are left as they were.  A row whose lens is
+ * below n_b or above max_pages * page_size sets CG_FLAG_POS_RANGE and gets zeros; a row whose cu runs backwards,
+ * past N or over max_q sets it and is left as it was; a page outside the pool sets it and contributes nothing.
+ * Caches: page pools as in kv_attend_paged.  workspace: attend_chunk_workspace_bytes bytes, 16-byte aligned;
+ * calls sharing one workspace on different streams race.  Errors: as kv_attend_paged. */
+int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const int32_t* cu, int32_t B, int32_t max_q,
+                              const cg_cache* kc, const cg_cache* vc, const cg_page_table* pages, const void* G_dev,
+                              cg_gauge_shape shp, const cg_codec* codec, const int32_t* lens, float scale,
+                              int32_t window, int32_t sinks, const cg_kv_view* out, void* workspace,
+                              int32_t* err_flag, void* stream);
 
 /* Device self-test of the two binary32 steps of the quantiser the kernels compute without a
  * division (section 4.3 block range; the oracle divides): which = 0 compares the reciprocal

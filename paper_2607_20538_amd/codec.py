@@ -18,16 +18,20 @@ LIB_PATH = os.path.join(_HERE, "libcodecgauge.so")
 
 CG_OK, CG_ERR_ARG, CG_ERR_SHAPE, CG_ERR_ALIGN, CG_ERR_UNSUPPORTED, CG_ERR_NOT_ORTHOGONAL, CG_ERR_CAPACITY, \
     CG_ERR_DEVICE = range(8)
-CG_FLAG_NONFINITE, CG_FLAG_SIDE_OVERFLOW, CG_FLAG_POS_RANGE = 1, 2, 4
+CG_FLAG_NONFINITE, CG_FLAG_SIDE_OVERFLOW, CG_FLAG_POS_RANGE, CG_FLAG_POOL_EMPTY = 1, 2, 4, 8
 GAUGE_IDENTITY, GAUGE_HAAR, GAUGE_DCT2, GAUGE_HADAMARD, GAUGE_EXPM, GAUGE_USER = range(6)
 PASSTHROUGH, BLOCK_UNIFORM, KIVI, ZFP = 0, 1, 2, 3
 DTYPE_BF16, DTYPE_F32 = 0, 1
+ROPE_HALF, ROPE_PAIRS = 0, 1
+ROPE_NONE, ROPE_LINEAR, ROPE_RAMP = 0, 1, 2
 
 EXPORTS = ["cg_status_str", "gauge_device_bytes", "gauge_make", "cache_bytes", "kv_encode", "kv_decode",
            "kv_append_step", "spectral_workspace_bytes", "kv_spectral_stats", "gauge_grad_workspace_bytes",
            "kv_gauge_grad", "attend_workspace_bytes", "kv_attend",
            "kv_attend_noalloc",
-           "attend_paged_workspace_bytes", "kv_attend_paged", "kv_encode_paged", "kv_append_paged", "cg_selftest",
+           "attend_paged_workspace_bytes", "kv_attend_paged", "kv_encode_paged", "kv_append_paged",
+           "kv_page_map", "kv_page_release", "rope_make", "kv_rope", "kv_append_slots",
+           "attend_chunk_workspace_bytes", "kv_attend_chunk_paged", "cg_selftest",
            "cg_stream_probe"]
 
 
@@ -37,6 +41,21 @@ class GaugeShape(C.Structure):
 
 class PageTable(C.Structure):
     _fields_ = [("pages", C.c_void_p), ("max_pages", C.c_int32), ("page_size", C.c_int32)]
+
+
+class PagePoolStruct(C.Structure):
+    _fields_ = [("free_pages", C.c_void_p), ("free_count", C.c_void_p), ("n_pages", C.c_int32)]
+
+
+class Rope(C.Structure):
+    _fields_ = [("d_rot", C.c_int32), ("layout", C.c_int32), ("scaling", C.c_int32), ("train_len", C.c_int32),
+                ("base", C.c_double), ("factor", C.c_double), ("low", C.c_double), ("high", C.c_double),
+                ("amplitude", C.c_double)]
+
+
+class RopePlan(C.Structure):
+    _fields_ = [("d_rot", C.c_int32), ("layout", C.c_int32), ("amplitude", C.c_float), ("reserved", C.c_int32),
+                ("step", C.c_uint64 * 128)]
 
 
 class CodecStruct(C.Structure):
@@ -119,6 +138,24 @@ def lib() -> C.CDLL:
                                       GaugeShape, C.POINTER(CodecStruct), C.POINTER(CacheStruct),
                                       C.POINTER(CacheStruct), p, p]
         L.kv_append_paged.restype = i32
+        L.kv_page_map.argtypes = [p, p, i32, C.POINTER(PagePoolStruct), p, i32, i32, i32, p, p, p, p, p, p]
+        L.kv_page_map.restype = i32
+        L.kv_page_release.argtypes = [p, p, i32, C.POINTER(PagePoolStruct), p, i32, i32, p, p]
+        L.kv_page_release.restype = i32
+        L.rope_make.argtypes = [C.POINTER(Rope), C.POINTER(RopePlan)]
+        L.rope_make.restype = i32
+        L.kv_rope.argtypes = [C.POINTER(RopePlan), C.POINTER(KvView), C.POINTER(KvView), C.POINTER(KvView),
+                              C.POINTER(KvView), p, i32, p]
+        L.kv_rope.restype = i32
+        L.kv_append_slots.argtypes = [i32, i32, C.POINTER(KvView), C.POINTER(KvView), p, p, GaugeShape,
+                                      C.POINTER(CodecStruct), C.POINTER(CacheStruct), C.POINTER(CacheStruct), p, p]
+        L.kv_append_slots.restype = i32
+        L.attend_chunk_workspace_bytes.argtypes = [GaugeShape] + [i32] * 9
+        L.attend_chunk_workspace_bytes.restype = C.c_size_t
+        L.kv_attend_chunk_paged.argtypes = [i32, i32, C.POINTER(KvView), p, i32, i32, C.POINTER(CacheStruct),
+                                            C.POINTER(CacheStruct), C.POINTER(PageTable), p, GaugeShape,
+                                            C.POINTER(CodecStruct), p, C.c_float, i32, i32, C.POINTER(KvView), p, p, p]
+        L.kv_attend_chunk_paged.restype = i32
         L.cg_selftest.argtypes = [i32, p, p]
         L.cg_selftest.restype = i32
         L.cg_stream_probe.argtypes = [p, C.c_int64, p, C.c_int64, p]
@@ -377,3 +414,147 @@ def kv_append_paged(l0: int, l1: int, k_new, v_new, pos, pt: PageTable, G_dev, s
     rc = lib().kv_append_paged(l0, l1, C.byref(kn), C.byref(vn), _ptr(pos), C.byref(pt), _ptr(G_dev), shp,
                                C.byref(cs), C.byref(kcs), C.byref(vcs), _ptr(err_flag), _stream(stream))
     _check("kv_append_paged", rc)
+
+
+# ------------------------------------------------------------------------------------------
+# a serving step over paged caches: tables and slots, rotary positions, packed tokens
+# ------------------------------------------------------------------------------------------
+
+def _on_device(fn: str, **tensors):
+    """The named tensors lie on the device that is current (the library launches there); int32 ones are
+    contiguous.  None is left out."""
+    import torch
+
+    dev = None
+    for name, t in tensors.items():
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise ValueError(f"{fn}: {name} is not a GPU tensor")
+        if dev is None:
+            dev = torch.cuda.current_device()
+        if t.get_device() != dev:
+            raise ValueError(f"{fn}: {name} is on cuda:{t.get_device()}, the current device is cuda:{dev}")
+
+
+def _int32(fn: str, count: int | None = None, **tensors):
+    """The named tensors are contiguous int32 tensors of `count` elements (any number: None)."""
+    import torch
+
+    for name, t in tensors.items():
+        if t.dtype != torch.int32 or not t.is_contiguous():
+            raise ValueError(f"{fn}: {name} must be a contiguous int32 tensor")
+        if count is not None and t.numel() != count:
+            raise ValueError(f"{fn}: {name} needs {count} elements, not {t.numel()}")
+
+
+class PagePool:
+    """Free pages of a pool of n_pages pages as kv_page_map and kv_page_release keep them: a stack `free` and
+    its height `count` (device int32).  A new pool is all free, page 0 on top."""
+
+    def __init__(self, n_pages: int, device="cuda"):
+        import torch
+
+        self.n_pages = int(n_pages)
+        self.free = torch.arange(self.n_pages - 1, -1, -1, dtype=torch.int32, device=device)
+        self.count = torch.full((1,), self.n_pages, dtype=torch.int32, device=device)
+
+    def struct(self) -> PagePoolStruct:
+        return PagePoolStruct(_ptr(self.free), _ptr(self.count), self.n_pages)
+
+
+def kv_page_map(held, add, pool: PagePool, pages, page_size: int, cu, lens, pos, slots, err_flag=None, stream=None):
+    """Tables and slots of one step: row b holds held[b] positions and adds add[b] tokens (int32 [B]).  Takes the
+    new pages off `pool` into the table `pages` [B][max_pages] and writes lens [B] (may be held), cu [B + 1], and
+    for the packed tokens pos [N] and slots [N] (-1 behind the last one)."""
+    _on_device("kv_page_map", held=held, add=add, free=pool.free, count=pool.count, pages=pages, cu=cu, lens=lens,
+               pos=pos, slots=slots, err_flag=err_flag)
+    B, N = held.numel(), pos.numel()
+    if pages.dim() != 2 or pages.shape[0] != B:
+        raise ValueError("kv_page_map: pages must be [B][max_pages]")
+    _int32("kv_page_map", B, held=held, add=add, lens=lens)
+    _int32("kv_page_map", B + 1, cu=cu)
+    _int32("kv_page_map", N, pos=pos, slots=slots)
+    _int32("kv_page_map", None, pages=pages)
+    ps = pool.struct()
+    rc = lib().kv_page_map(_ptr(held), _ptr(add), B, C.byref(ps), _ptr(pages), pages.shape[1], page_size, N, _ptr(cu),
+                           _ptr(lens), _ptr(pos), _ptr(slots), _ptr(err_flag), _stream(stream))
+    _check("kv_page_map", rc)
+
+
+def kv_page_release(lens, done, pool: PagePool, pages, page_size: int, err_flag=None, stream=None):
+    """Rows with done[b] != 0 (int32 [B]) give their pages back to `pool`; their lens become 0."""
+    _on_device("kv_page_release", lens=lens, done=done, free=pool.free, count=pool.count, pages=pages,
+               err_flag=err_flag)
+    B = lens.numel()
+    if pages.dim() != 2 or pages.shape[0] != B:
+        raise ValueError("kv_page_release: pages must be [B][max_pages]")
+    _int32("kv_page_release", B, lens=lens, done=done)
+    _int32("kv_page_release", None, pages=pages)
+    ps = pool.struct()
+    rc = lib().kv_page_release(_ptr(lens), _ptr(done), B, C.byref(ps), _ptr(pages), pages.shape[1], page_size,
+                               _ptr(err_flag), _stream(stream))
+    _check("kv_page_release", rc)
+
+
+def rope_make(d_rot: int, layout: int = ROPE_HALF, base: float = 10000.0, scaling: int = ROPE_NONE, factor: float = 1.0,
+              low: float = 1.0, high: float = 4.0, train_len: int = 0, amplitude: float = 1.0) -> RopePlan:
+    """Plan of a rotation of the channels [0, d_rot): pairs (i, i + d_rot / 2) or neighbours, frequencies
+    base^(-2 i / d_rot), for long contexts divided by `factor` (ROPE_LINEAR) or by the turns that a pair makes over
+    train_len positions, from `low` turns (divided) to `high` (kept) (ROPE_RAMP)."""
+    r = Rope(d_rot, layout, scaling, train_len, base, factor, low, high, amplitude)
+    plan = RopePlan()
+    _check("rope_make", lib().rope_make(C.byref(r), C.byref(plan)))
+    return plan
+
+
+def kv_rope(plan: RopePlan, x, y, pos, x2=None, y2=None, inverse: bool = False, stream=None):
+    """y = x [L][B][H][T][d] turned by the tokens' positions pos (int32 [B][T]; negative: left as it was), x2 into
+    y2 by the same launch; y may be x.  inverse: the transposed map (the gradient with respect to x)."""
+    _on_device("kv_rope", x=x, y=y, x2=x2, y2=y2, pos=pos)
+    _int32("kv_rope", x.shape[1] * x.shape[3], pos=pos)
+    xv, yv = view(x), view(y)
+    x2v = None if x2 is None else C.byref(view(x2))
+    y2v = None if y2 is None else C.byref(view(y2))
+    rc = lib().kv_rope(C.byref(plan), C.byref(xv), C.byref(yv), x2v, y2v, _ptr(pos), int(inverse), _stream(stream))
+    _check("kv_rope", rc)
+
+
+def kv_append_slots(l0: int, l1: int, k_new, v_new, slots, G_dev, shp: GaugeShape, codec: Codec, kc: Cache, vc: Cache,
+                    err_flag=None, stream=None):
+    """Encodes packed tokens k_new, v_new [l1-l0][1][H][N][d] into the page pools kc, vc at slots (int32 [N], as
+    kv_page_map writes them; negative: skipped)."""
+    _on_device("kv_append_slots", k_new=k_new, v_new=v_new, slots=slots, G_dev=G_dev, codes=kc.codes, v_codes=vc.codes,
+               err_flag=err_flag)
+    _int32("kv_append_slots", k_new.shape[3], slots=slots)
+    kn, vn, cs, kcs, vcs = view(k_new), view(v_new), codec.struct(), kc.struct(), vc.struct()
+    rc = lib().kv_append_slots(l0, l1, C.byref(kn), C.byref(vn), _ptr(slots), _ptr(G_dev), shp, C.byref(cs),
+                               C.byref(kcs), C.byref(vcs), _ptr(err_flag), _stream(stream))
+    _check("kv_append_slots", rc)
+
+
+def attend_chunk_workspace_bytes(shp: GaugeShape, nl: int, N: int, B: int, max_q: int, Hq: int, max_pages: int,
+                                 page_size: int, window: int = 0, sinks: int = 0) -> int:
+    return int(lib().attend_chunk_workspace_bytes(shp, nl, N, B, max_q, Hq, max_pages, page_size, window, sinks))
+
+
+def kv_attend_chunk_paged(l0: int, l1: int, q, cu, max_q: int, kc: Cache, vc: Cache, pt: PageTable, G_dev,
+                          shp: GaugeShape, codec: Codec, lens, scale: float, out, window: int = 0, sinks: int = 0,
+                          workspace=None, err_flag=None, stream=None):
+    """Attention of the packed new tokens q [l1-l0][1][Hq][N][d] (row b's: cu[b] .. cu[b+1], at most max_q) over
+    page pools that hold them, causal or with a sliding window behind which the first `sinks` positions stay
+    visible; lens: int32 [B] positions held with the new tokens.  Writes out (q's shape)."""
+    _on_device("kv_attend_chunk_paged", q=q, cu=cu, codes=kc.codes, v_codes=vc.codes, G_dev=G_dev, lens=lens, out=out,
+               workspace=workspace, err_flag=err_flag)
+    B = lens.numel()
+    _int32("kv_attend_chunk_paged", B, lens=lens)
+    _int32("kv_attend_chunk_paged", B + 1, cu=cu)
+    qv, ov, cs, kcs, vcs = view(q), view(out), codec.struct(), kc.struct(), vc.struct()
+    if workspace is not None:
+        need = attend_chunk_workspace_bytes(shp, l1 - l0, qv.T, B, max_q, qv.H, pt.max_pages, pt.page_size, window, sinks)
+        if workspace.nbytes < need:
+            raise ValueError(f"kv_attend_chunk_paged: workspace of {workspace.nbytes} bytes, {need} needed")
+    rc = lib().kv_attend_chunk_paged(l0, l1, C.byref(qv), _ptr(cu), B, max_q, C.byref(kcs), C.byref(vcs), C.byref(pt),
+                                     _ptr(G_dev), shp, C.byref(cs), _ptr(lens), float(scale), window, sinks,
+                                     C.byref(ov), _ptr(workspace), _ptr(err_flag), _stream(stream))
+    _check("kv_attend_chunk_paged", rc)

@@ -26,13 +26,18 @@ struct AppendArgs {
   CodecDev c;
   int* err;
   PageDev pt;
+  bool slots;      // pos holds pool slots: page * T_cap + position, negative: no token
 };
 
 // Cache batch row and position inside it of batch row b's new token at position p of the row; false
 // (and flagged) when the position or its page is outside the cache.
 __device__ __forceinline__ bool token_slot(const AppendArgs& a, const CacheDev& k, int b, int& row, int& p) {
   row = b;
-  if (a.pt.pages) {
+  if (a.slots) {
+    if (p < 0) return false;
+    row = p / k.T_cap;
+    p -= row * k.T_cap;
+  } else if (a.pt.pages) {
     const int lp = p >= 0 ? p / a.pt.page_size : -1;
     row = lp >= 0 && lp < a.pt.max_pages ? a.pt.pages[size_t(b) * a.pt.max_pages + lp] : -1;
     p -= lp * a.pt.page_size;
@@ -240,8 +245,9 @@ __global__ __launch_bounds__(kThreads) void append_staged(AppendArgs a) {
 
 hipError_t launch_append(const ViewDev& Kn, const ViewDev& Vn, int l0, const int* pos, const GaugeDev& G,
                          const CodecDev& c, const CacheDev& kc, const CacheDev& vc, int* err, hipStream_t st,
-                         const PageDev& pt) {
+                         const PageDev& pt, bool slots) {
   AppendArgs a;
+  a.slots = slots;
   a.x[0] = Kn; a.x[1] = Vn;
   a.k[0] = kc; a.k[1] = vc;
   a.l0 = l0;

@@ -1,0 +1,35 @@
+// Kernel arguments and plan of the chunk attention.
+#pragma once
+
+#include "cg_internal.h"
+
+namespace cg {
+
+struct ChunkDev {
+  ViewDev q, o;          // [nl][1][Hq][N][d], packed tokens
+  CacheDev kc, vc;       // page pools
+  PageDev pt;
+  int l0, Hq, grp;       // cache layer of view layer 0, query heads, query heads per KV head
+  int B, N, max_q;       // batch rows, packed tokens, tokens of a row at most
+  const int* cu;         // device [B + 1] first token of every row
+  const int* lens;       // device [B] positions a row holds, its new tokens among them
+  float scale;
+  int window, sinks;
+  int cap;               // positions a row can hold
+  int waves, tq, heads, nqc, ntile, nsplit;  // the plan
+  float *part, *ml;      // splits: [nl][nsplit][N][Hq][d], [nl][nsplit][N][Hq][2] (maximum, sum)
+  int* err;
+};
+
+struct ChunkPlan {
+  int waves = 1;         // waves of 32 query rows per workgroup
+  int tq = 1, heads = 1; // tokens and query heads of a tile
+  int nqc = 1;           // chunks of a KV head's query heads
+  int ntile = 0;         // tiles at most
+  int nsplit = 1;        // parts of a tile's positions
+  size_t ws_bytes = 0;
+};
+ChunkPlan chunk_plan(int nl, int N, int B, int max_q, int H, int Hq, int d, int cap, int window, int sinks);
+hipError_t launch_chunk(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, hipStream_t st);
+
+}  // namespace cg

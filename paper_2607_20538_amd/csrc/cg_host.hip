@@ -11,6 +11,7 @@
 #include <vector>
 
 #include "cg_internal.h"
+#include "cg_chunk.h"
 
 using namespace cg;
 
@@ -352,6 +353,20 @@ CacheDev cache_dev(const cg_cache* k) {
   return d;
 }
 
+// Shared by every view of packed tokens: type, d, 16-byte rows, strides that are not negative
+int32_t check_rows(const cg_kv_view* v) {
+  if (!v || (!v->ptr && v->T != 0)) return CG_ERR_ARG;
+  if (v->dtype != CG_DTYPE_BF16 && v->dtype != CG_DTYPE_F32) return CG_ERR_ARG;
+  if (v->L <= 0 || v->B <= 0 || v->H <= 0 || v->T < 0 || v->d <= 0) return CG_ERR_SHAPE;
+  if (!aligned16(v->ptr)) return CG_ERR_ALIGN;
+  const int64_t unit = v->dtype == CG_DTYPE_BF16 ? 8 : 4;
+  if (v->stride_l % unit || v->stride_b % unit || v->stride_h % unit || v->stride_t % unit) return CG_ERR_ALIGN;
+  if (v->stride_l < 0 || v->stride_b < 0 || v->stride_h < 0 || v->stride_t < 0) return CG_ERR_ARG;
+  return CG_OK;
+}
+
+bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
 // A query or output view of kv_attend: [nl][B][Hq][1][d], Hq a multiple of the KV heads.
 int32_t check_qview(const cg_kv_view* v, const cg_gauge_shape& s, int L) {
   if (!v || !v->ptr) return CG_ERR_ARG;
@@ -392,6 +407,25 @@ hipError_t launch_decode(int s, const CacheDev& k, int l0, const GaugeDev& G, co
   if (!force_generic() && mfma_decode_supported(s, Y, G, c))
     return launch_decode_mfma(s, k, l0, G, c, t0, len, pos, pos_add, Y, err, st);
   return launch_decode_generic(s, k, l0, G, c, t0, len, pos, pos_add, Y, err, st);
+}
+
+// Packed tokens through their slots: the tokens take the place of the batch rows of a rolling append.
+static hipError_t launch_append_slots(const ViewDev& Kn, const ViewDev& Vn, int l0, const int* slots, const GaugeDev& G,
+                                      const CodecDev& c, const CacheDev& kc, const CacheDev& vc, int* err,
+                                      hipStream_t st) {
+  constexpr int kMost = 1 << 19;  // tokens of a launch (its grid holds 2^16 groups of 16)
+  for (int i0 = 0; i0 < Kn.T; i0 += kMost) {
+    ViewDev x[2] = {Kn, Vn};
+    for (ViewDev& v : x) {
+      v.ptr = static_cast<char*>(v.ptr) + int64_t(i0) * v.st * (v.bf16 ? 2 : 4);
+      v.B = std::min(kMost, v.T - i0);
+      v.sb = v.st;
+      v.T = 1;
+    }
+    const hipError_t e = launch_append(x[0], x[1], l0, slots + i0, G, c, kc, vc, err, st, PageDev(), true);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace cg
@@ -888,6 +922,199 @@ int32_t kv_append_paged(int32_t l0, int32_t l1, const cg_kv_view* k_new, const c
   pt.page_size = pages->page_size;
   hipError_t e =
       launch_append(view_dev(k_new), view_dev(v_new), l0, pos, G, c, cache_dev(kc), cache_dev(vc), err_flag, st, pt);
+  return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
+}
+
+static int32_t check_pool(const cg_page_pool* pool, const int32_t* pages, int32_t max_pages, int32_t page_size) {
+  if (!pool || !pool->free_pages || !pool->free_count || !pages || pool->n_pages <= 0 || max_pages <= 0) return CG_ERR_ARG;
+  if (!aligned4(pool->free_pages) || !aligned4(pool->free_count) || !aligned4(pages)) return CG_ERR_ALIGN;
+  if (page_size <= 0 || page_size % 64) return CG_ERR_SHAPE;
+  if (int64_t(pool->n_pages) * page_size > INT32_MAX || int64_t(max_pages) * page_size > INT32_MAX) return CG_ERR_CAPACITY;
+  return CG_OK;
+}
+
+int32_t kv_page_map(const int32_t* held, const int32_t* add, int32_t B, const cg_page_pool* pool, int32_t* pages,
+                    int32_t max_pages, int32_t page_size, int32_t N, int32_t* cu, int32_t* lens, int32_t* pos,
+                    int32_t* slots, int32_t* err_flag, void* stream) {
+  int32_t rc = check_pool(pool, pages, max_pages, page_size);
+  if (rc != CG_OK) return rc;
+  if (!held || !add || B <= 0 || N < 0 || !cu || !lens || (N && (!pos || !slots))) return CG_ERR_ARG;
+  if (!aligned4(held) || !aligned4(add) || !aligned4(cu) || !aligned4(lens) || !aligned4(pos) || !aligned4(slots) ||
+      !aligned4(err_flag))
+    return CG_ERR_ALIGN;
+  hipError_t e = launch_page_map(held, add, B, *pool, pages, max_pages, page_size, N, cu, lens, pos, slots, err_flag,
+                                 static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
+}
+
+int32_t kv_page_release(int32_t* lens, const int32_t* done, int32_t B, const cg_page_pool* pool, int32_t* pages,
+                        int32_t max_pages, int32_t page_size, int32_t* err_flag, void* stream) {
+  int32_t rc = check_pool(pool, pages, max_pages, page_size);
+  if (rc != CG_OK) return rc;
+  if (!lens || !done || B <= 0) return CG_ERR_ARG;
+  if (!aligned4(lens) || !aligned4(done) || !aligned4(err_flag)) return CG_ERR_ALIGN;
+  hipError_t e = launch_page_release(lens, done, B, *pool, pages, max_pages, page_size, err_flag,
+                                     static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
+}
+
+int32_t rope_make(const cg_rope* r, cg_rope_plan* plan) {
+  if (!r || !plan) return CG_ERR_ARG;
+  if (r->d_rot < 2 || r->d_rot > 256 || r->d_rot % 2) return CG_ERR_ARG;
+  if (r->layout != CG_ROPE_HALF && r->layout != CG_ROPE_PAIRS) return CG_ERR_ARG;
+  if (r->scaling < CG_ROPE_NONE || r->scaling > CG_ROPE_RAMP) return CG_ERR_ARG;
+  if (!isfinite(r->base) || !(r->base > 0.0) || !isfinite(float(r->amplitude))) return CG_ERR_ARG;
+  if (r->scaling != CG_ROPE_NONE && (!isfinite(r->factor) || !(r->factor > 0.0))) return CG_ERR_ARG;
+  if (r->scaling == CG_ROPE_RAMP && (r->train_len <= 0 || !isfinite(r->low) || !isfinite(r->high) || !(r->low < r->high)))
+    return CG_ERR_ARG;
+  cg_rope_plan p = {};
+  p.d_rot = r->d_rot;
+  p.layout = r->layout;
+  p.amplitude = float(r->amplitude);
+  for (int i = 0; i < r->d_rot / 2; ++i) {
+    double f = pow(r->base, -2.0 * i / r->d_rot);  // radians per position
+    if (r->scaling == CG_ROPE_LINEAR) f /= r->factor;
+    if (r->scaling == CG_ROPE_RAMP) {
+      const double w = std::min(1.0, std::max(0.0, (r->train_len * f / (2.0 * M_PI) - r->low) / (r->high - r->low)));
+      f = f * (1.0 - w) / r->factor + f * w;
+    }
+    if (!isfinite(f)) return CG_ERR_ARG;
+    const double t = f / (2.0 * M_PI), frac = t - floor(t);  // whole turns per position are none
+    const double s = ldexp(frac, 64);
+    p.step[i] = s >= 18446744073709551615.0 ? 0 : uint64_t(s);
+  }
+  *plan = p;
+  return CG_OK;
+}
+
+int32_t kv_rope(const cg_rope_plan* plan, const cg_kv_view* x0, const cg_kv_view* y0, const cg_kv_view* x1,
+                const cg_kv_view* y1, const int32_t* pos, int32_t inverse, void* stream) {
+  if (!plan || !x0 || !y0 || (x1 == nullptr) != (y1 == nullptr)) return CG_ERR_ARG;
+  if (plan->layout != CG_ROPE_HALF && plan->layout != CG_ROPE_PAIRS) return CG_ERR_ARG;
+  const cg_kv_view* vs[4] = {x0, y0, x1, y1};
+  int32_t rc;
+  for (int i = 0; i < (x1 ? 4 : 2); ++i) {
+    if ((rc = check_rows(vs[i])) != CG_OK) return rc;
+    if (vs[i]->dtype != x0->dtype || vs[i]->L != x0->L || vs[i]->B != x0->B || vs[i]->T != x0->T || vs[i]->d != x0->d)
+      return CG_ERR_SHAPE;
+    if (vs[i]->H != vs[i & 2]->H) return CG_ERR_SHAPE;
+  }
+  if (x0->d % 8 || x0->d > 256) return CG_ERR_UNSUPPORTED;
+  if (plan->d_rot < 2 || plan->d_rot % 2 || plan->d_rot > x0->d) return CG_ERR_SHAPE;
+  if (x0->T == 0) return CG_OK;
+  if (!pos) return CG_ERR_ARG;
+  if (!aligned4(pos)) return CG_ERR_ALIGN;
+  if (int64_t(x0->B) * x0->T > INT32_MAX / (x0->d / 2) - 256 || int64_t(x0->L) * (int64_t(x0->H) + (x1 ? x1->H : 0)) > 65535)
+    return CG_ERR_CAPACITY;
+  ViewDev none{};
+  hipError_t e = launch_rope(*plan, view_dev(x0), view_dev(y0), x1 ? view_dev(x1) : none, x1 ? view_dev(y1) : none, pos,
+                             inverse != 0, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
+}
+
+// the pools of packed tokens' entry points: page pools whose slots fit an int32
+static int32_t check_pools(const cg_cache* kc, const cg_cache* vc, const cg_codec* codec, const cg_gauge_shape& shp) {
+  if (!kc || !vc) return CG_ERR_ARG;
+  int32_t rc;
+  if ((rc = check_cache(kc, codec, shp, kc->B)) != CG_OK) return rc;
+  if ((rc = check_cache(vc, codec, shp, kc->B)) != CG_OK) return rc;
+  if (kc->T_cap != vc->T_cap || kc->T_cap % 64) return CG_ERR_SHAPE;
+  const bool ok = codec->backend == CG_BACKEND_PASSTHROUGH ||
+                  (codec->backend == CG_BACKEND_BLOCK_UNIFORM && codec->block_t == 1);
+  return ok ? CG_OK : CG_ERR_UNSUPPORTED;
+}
+
+int32_t kv_append_slots(int32_t l0, int32_t l1, const cg_kv_view* k_new, const cg_kv_view* v_new, const int32_t* slots,
+                        const void* G_dev, cg_gauge_shape shp, const cg_codec* codec, const cg_cache* kc,
+                        const cg_cache* vc, int32_t* err_flag, void* stream) {
+  int32_t rc = check_shape(shp);
+  if (rc != CG_OK) return rc;
+  if (!G_dev || l0 < 0 || l1 <= l0 || l1 > shp.L) return CG_ERR_ARG;
+  if (!aligned16(G_dev)) return CG_ERR_ALIGN;
+  if ((rc = check_codec(codec, shp.d)) != CG_OK) return rc;
+  const int nl = l1 - l0;
+  if ((rc = check_view(k_new, shp, nl)) != CG_OK) return rc;
+  if ((rc = check_view(v_new, shp, nl)) != CG_OK) return rc;
+  if (k_new->B != 1 || v_new->B != 1 || v_new->T != k_new->T) return CG_ERR_SHAPE;
+  if ((rc = check_pools(kc, vc, codec, shp)) != CG_OK) return rc;
+  if (int64_t(kc->B) * kc->T_cap > INT32_MAX) return CG_ERR_CAPACITY;
+  if (k_new->T == 0) return CG_OK;
+  if (!slots) return CG_ERR_ARG;
+  if (!aligned4(slots) || !aligned4(err_flag)) return CG_ERR_ALIGN;
+  hipError_t e = launch_append_slots(view_dev(k_new), view_dev(v_new), l0, slots, gauge_dev(G_dev, shp), codec_dev(codec),
+                                     cache_dev(kc), cache_dev(vc), err_flag, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
+}
+
+static int32_t check_chunk(int32_t nl, int32_t N, int32_t B, int32_t max_q, int32_t Hq, int32_t max_pages, int32_t page_size,
+                           int32_t window, int32_t sinks, const cg_gauge_shape& shp) {
+  if (nl <= 0 || N < 0 || B <= 0 || max_q <= 0 || window < 0 || sinks < 0 || max_pages <= 0) return CG_ERR_ARG;
+  if (Hq < shp.H || Hq % shp.H || page_size <= 0 || page_size % 64) return CG_ERR_SHAPE;
+  if (int64_t(max_pages) * page_size > INT32_MAX) return CG_ERR_CAPACITY;
+  return CG_OK;
+}
+
+size_t attend_chunk_workspace_bytes(cg_gauge_shape shp, int32_t nl, int32_t N, int32_t B, int32_t max_q, int32_t Hq,
+                                    int32_t max_pages, int32_t page_size, int32_t window, int32_t sinks) {
+  if (check_shape(shp) != CG_OK || check_chunk(nl, N, B, max_q, Hq, max_pages, page_size, window, sinks, shp) != CG_OK || N == 0)
+    return 0;
+  return chunk_plan(nl, N, B, max_q, shp.H, Hq, shp.d, max_pages * page_size, window, sinks).ws_bytes;
+}
+
+int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const int32_t* cu, int32_t B, int32_t max_q,
+                              const cg_cache* kc, const cg_cache* vc, const cg_page_table* pages, const void* G_dev,
+                              cg_gauge_shape shp, const cg_codec* codec, const int32_t* lens, float scale,
+                              int32_t window, int32_t sinks, const cg_kv_view* out, void* workspace,
+                              int32_t* err_flag, void* stream) {
+  int32_t rc = check_shape(shp);
+  if (rc != CG_OK) return rc;
+  if (!G_dev || !cu || !lens || l0 < 0 || l1 <= l0 || l1 > shp.L || !isfinite(scale)) return CG_ERR_ARG;
+  if (!aligned16(G_dev)) return CG_ERR_ALIGN;
+  if (!aligned4(cu) || !aligned4(lens) || !aligned4(err_flag)) return CG_ERR_ALIGN;
+  if ((rc = check_codec(codec, shp.d)) != CG_OK) return rc;
+  const int nl = l1 - l0;
+  if ((rc = check_rows(q)) != CG_OK) return rc;
+  if ((rc = check_rows(out)) != CG_OK) return rc;
+  if (q->L != nl || q->B != 1 || q->d != shp.d) return CG_ERR_SHAPE;
+  if (out->L != nl || out->B != 1 || out->d != shp.d || out->H != q->H || out->T != q->T) return CG_ERR_SHAPE;
+  if ((rc = check_pools(kc, vc, codec, shp)) != CG_OK) return rc;
+  if ((rc = check_pages(pages, codec, kc)) != CG_OK) return rc;
+  if ((rc = check_chunk(nl, q->T, B, max_q, q->H, pages->max_pages, pages->page_size, window, sinks, shp)) != CG_OK) return rc;
+  if (q->T == 0) return CG_OK;
+  const int cap = pages->max_pages * pages->page_size;
+  const ChunkPlan p = chunk_plan(nl, q->T, B, max_q, shp.H, q->H, shp.d, cap, window, sinks);
+  if (p.ws_bytes && (!workspace || !aligned16(workspace))) return workspace ? CG_ERR_ALIGN : CG_ERR_ARG;
+  if (int64_t(nl) * shp.H * p.nqc * p.ntile * p.nsplit > INT32_MAX) return CG_ERR_CAPACITY;
+  ChunkDev a;
+  a.q = view_dev(q);
+  a.o = view_dev(out);
+  a.kc = cache_dev(kc);
+  a.vc = cache_dev(vc);
+  a.pt.pages = pages->pages;
+  a.pt.max_pages = pages->max_pages;
+  a.pt.page_size = pages->page_size;
+  a.l0 = l0;
+  a.Hq = q->H;
+  a.grp = q->H / shp.H;
+  a.B = B;
+  a.N = q->T;
+  a.max_q = max_q;
+  a.cu = cu;
+  a.lens = lens;
+  a.scale = scale;
+  a.window = window;
+  a.sinks = sinks;
+  a.cap = cap;
+  a.waves = p.waves;
+  a.tq = p.tq;
+  a.heads = p.heads;
+  a.nqc = p.nqc;
+  a.ntile = p.ntile;
+  a.nsplit = p.nsplit;
+  a.part = static_cast<float*>(workspace);
+  a.ml = a.part ? a.part + size_t(nl) * p.nsplit * q->T * q->H * shp.d : nullptr;
+  a.err = err_flag;
+  hipError_t e = launch_chunk(a, gauge_dev(G_dev, shp), codec_dev(codec), static_cast<hipStream_t>(stream));
   return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
 }
 

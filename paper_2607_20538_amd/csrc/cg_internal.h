@@ -173,6 +173,14 @@ hipError_t launch_attend(const AttendDev& a, const GaugeDev& G, const CodecDev& 
 size_t attend_scratch_bytes();
 hipError_t attend_scratch(void** ptr);
 
+// Rotary positions of one or two views (x1.H == 0: one), tables and slots of a serving step.
+hipError_t launch_rope(const cg_rope_plan& plan, const ViewDev& x0, const ViewDev& y0, const ViewDev& x1,
+                       const ViewDev& y1, const int* pos, bool inverse, hipStream_t st);
+hipError_t launch_page_map(const int* held, const int* add, int B, const cg_page_pool& pool, int* pages, int max_pages,
+                           int P, int N, int* cu, int* lens, int* pos, int* slots, int* err, hipStream_t st);
+hipError_t launch_page_release(int* lens, const int* done, int B, const cg_page_pool& pool, int* pages, int max_pages,
+                               int P, int* err, hipStream_t st);
+
 // HBM streaming probe (read_bytes a multiple of 8 KB, write_bytes of 16 bytes).
 hipError_t launch_stream_probe(const void* src, int64_t read_bytes, void* dst, int64_t write_bytes, hipStream_t st);
 
@@ -192,9 +200,10 @@ hipError_t launch_encode(int s, const ViewDev& X, int l0, const GaugeDev& G, con
 hipError_t launch_decode(int s, const CacheDev& k, int l0, const GaugeDev& G, const CodecDev& c, int t0, int len,
                          const int* pos, int pos_add, const ViewDev& Y, int* err, hipStream_t st);
 // Rolling append of one key and one value token per (layer, b, h) at pos[b], in one launch (layer l of
-// the views is cache layer l + l0).
+// the views is cache layer l + l0).  slots: pos holds pool slots (page * T_cap + position; negative:
+// nothing to append) instead of row positions.
 hipError_t launch_append(const ViewDev& Kn, const ViewDev& Vn, int l0, const int* pos, const GaugeDev& G,
                          const CodecDev& c, const CacheDev& kc, const CacheDev& vc, int* err, hipStream_t st,
-                         const PageDev& pt = PageDev());
+                         const PageDev& pt = PageDev(), bool slots = false);
 
 }  // namespace cg
