@@ -20,6 +20,7 @@
 // infinities and NaN make a step "odd": it is summed position by position in binary32, where a masked
 // position is left out instead of being multiplied by zero.
 #include <algorithm>
+#include <type_traits>
 
 #include "cg_internal.h"
 #include "cg_device.h"
@@ -225,7 +226,7 @@ struct ChunkShape {
   static constexpr int bytes = plane * PL * buffers;
 };
 
-template <int D, int PL, int NW>
+template <int D, int PL, int NW, bool WIDE>
 __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_attend(ChunkDev a, GaugeDev G, CodecDev c) {
   using SH = ChunkShape<D, PL>;
   constexpr int NT = 64 * NW, KK = D / 16, CT = D / 32, RUNS = D / 32;
@@ -285,13 +286,12 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
   const size_t qoff = size_t(lv) * a.q.sl + size_t(h * a.grp + j0 + jj) * a.q.sh + size_t(qt.tok0 + qt.i0 + tok) * a.q.st;
 
   // ---- loads of a step: page, then this thread's runs
-  constexpr bool AHEAD = IT <= 4;  // a step's codes wait in registers while the step before is computed
+  constexpr bool AHEAD = WIDE && IT * D <= 512;  // a step's codes wait in registers while the step before is computed
   Raw32 raw[AHEAD ? IT : 1];
   size_t srow = 0;       // cache row of the step's first position
   bool have = false;     // the step's page is inside the pool
-  const bool pass = c.backend == CG_BACKEND_PASSTHROUGH;
-  const bool wide = !pass && c.n % 32 == 0 && d % 32 == 0;  // one side word per run
-  const int words = pass ? 0 : d * c.bits / 32;
+  const bool pass = !WIDE && c.backend == CG_BACKEND_PASSTHROUGH;
+  const int words = d * c.bits / 32;
   auto item = [&](int i, bool& val, int& pos, int& run) {
     const int x = i * NT + tid;
     val = x >= ITEMS / 2;
@@ -311,26 +311,35 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
     }
     const CacheDev& k = val ? a.vc : a.kc;
     const uint32_t* src = reinterpret_cast<const uint32_t*>(k.codes) + (srow + pos) * words + run * c.bits;
-    if (c.bits == 4) {
-      const u32x4_t u = *reinterpret_cast<const u32x4_t*>(src);
+    auto words_at = [&](auto width, int i0) {  // `width` words from word i0 on, in one load
+      constexpr int W = decltype(width)::value;
+      typedef uint32_t vec_t __attribute__((ext_vector_type(W), aligned(W == 3 ? 4 : 4 * W)));
+      const vec_t u = *reinterpret_cast<const vec_t*>(src + i0);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o.w[e] = u[e];
-    } else if (c.bits == 8) {
-      const u32x4_t u = *reinterpret_cast<const u32x4_t*>(src), u2 = *reinterpret_cast<const u32x4_t*>(src + 4);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        o.w[e] = u[e];
-        o.w[4 + e] = u2[e];
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 6; ++e) o.w[e] = e < c.bits ? src[e] : 0u;
+      for (int e = 0; e < W; ++e) o.w[i0 + e] = u[e];
+    };
+    switch (c.bits) {  // rows of whole runs: every run starts on a multiple of its load's width
+      case 4: words_at(std::integral_constant<int, 4>(), 0); break;
+      case 8:
+        words_at(std::integral_constant<int, 4>(), 0);
+        words_at(std::integral_constant<int, 4>(), 4);
+        break;
+      case 2: words_at(std::integral_constant<int, 2>(), 0); break;
+      case 3: words_at(std::integral_constant<int, 3>(), 0); break;
+      default:
+        words_at(std::integral_constant<int, 2>(), 0);
+        words_at(std::integral_constant<int, 2>(), 2);
+        words_at(std::integral_constant<int, 2>(), 4);
     }
     o.side = k.side[(srow + pos) * (d / c.n) + 32 * run / c.n];
   };
+  const int* table = a.pt.pages + size_t(qt.b) * a.pt.max_pages;
+  auto page_of = [&](int v) { return v < v1 ? table[step_pos(v) / a.pt.page_size] : -1; };
+  int page = page_of(v0);  // of the step fetched next, looked up a step ahead
   auto fetch = [&](int v) {
     const int t0 = step_pos(v), lp = t0 / a.pt.page_size;
-    const int pg = __builtin_amdgcn_readfirstlane(a.pt.pages[size_t(qt.b) * a.pt.max_pages + lp]);
+    const int pg = __builtin_amdgcn_readfirstlane(page);
+    page = page_of(v + 1);
     have = pg >= 0 && pg < a.kc.B;
     if (!have) {
       if (tid == 0 && a.err) atomicOr(a.err, CG_FLAG_POS_RANGE);
@@ -338,7 +347,6 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
     }
     srow = ((size_t(l) * a.kc.B + pg) * H + h) * a.kc.T_cap + (t0 - lp * a.pt.page_size);
     if constexpr (AHEAD) {
-      if (!wide) return;
 #pragma unroll
       for (int i = 0; i < IT; ++i) load_run(raw[i], i);
     }
@@ -367,7 +375,7 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
           lo = pk_h(z0 - h_lo(hi), z1 - h_hi(hi));
         }
       };
-      if (wide) {
+      if constexpr (WIDE) {
         const uint32_t s = live ? rw.side : 0u;
         const float mnf = f16_bits_to_f32(s & 0xffffu), top = fmaf(float((1 << c.bits) - 1), f16_bits_to_f32(s >> 16), mnf);
         if (!(fabsf(top) <= 65504.0f && fabsf(mnf) <= 65504.0f)) st |= kOver;
@@ -433,7 +441,7 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
     } else {
 #pragma unroll 1
       for (int i = 0; i < IT; ++i) {
-        if (wide) load_run(raw[0], i);
+        if constexpr (WIDE) load_run(raw[0], i);
         one(i, raw[0]);
       }
     }
@@ -584,13 +592,18 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
           const float* vr = rows32 + SUB * D + u * D + 4 * hc;
           float s = 0.0f;
 #pragma unroll
-          for (int kk = 0; kk < KK; ++kk)
+          for (int kk = 0; kk < KK; ++kk) {
+            // (opaque: the queries in binary32 would otherwise be kept for this rare path, in registers
+            // that the others need)
+            u32x4_t qa = __builtin_bit_cast(u32x4_t, Q[0][kk]), qb = __builtin_bit_cast(u32x4_t, Q[PL - 1][kk]);
+            asm volatile("" : "+v"(qa), "+v"(qb));
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              float q = (float)Q[0][kk][e];
-              if constexpr (PL == 2) q += (float)Q[PL - 1][kk][e];
+              float q = (e & 1) ? h_hi(qa[e >> 1]) : h_lo(qa[e >> 1]);
+              if constexpr (PL == 2) q += (e & 1) ? h_hi(qb[e >> 1]) : h_lo(qb[e >> 1]);
               s = fmaf(q, kr[16 * kk + e], s);
             }
+          }
           s = halves_sum(s);
           const float mn = seen ? fmaxf(m, s) : m;
           const float al = m == mn ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * cs);
@@ -614,19 +627,36 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
     f32x16_t S[2];
     S[0] = f32x16_t{};
     S[1] = f32x16_t{};
+    // operands two K-steps ahead of the products
+    const uint8_t* kb = buf + n * SH::KP + 16 * hc;
+    f16x8_t kf[2][2][2][PL];  // buffer, K-step, positions, plane
+    auto kload = [&](int s, int k2) {
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk)
+      for (int i = 0; i < 2; ++i)
 #pragma unroll
-      for (int ps = 0; ps < 2; ++ps) {
-        const uint8_t* src = buf + (32 * ps + n) * SH::KP + 32 * kk + 16 * hc;
-        const f16x8_t k0 = as_f16x8(*reinterpret_cast<const u32x4_t*>(src));
-        S[ps] = mfma_h(k0, Q[0][kk], S[ps]);
-        if constexpr (PL == 2) {
-          const f16x8_t k1 = as_f16x8(*reinterpret_cast<const u32x4_t*>(src + SH::plane));
-          S[ps] = mfma_h(k0, Q[PL - 1][kk], S[ps]);
-          S[ps] = mfma_h(k1, Q[0][kk], S[ps]);
+        for (int ps = 0; ps < 2; ++ps)
+#pragma unroll
+          for (int p = 0; p < PL; ++p)
+            kf[s][i][ps][p] = as_f16x8(*reinterpret_cast<const u32x4_t*>(kb + 32 * ps * SH::KP + 32 * (2 * k2 + i) + p * SH::plane));
+    };
+    kload(0, 0);
+#pragma unroll
+    for (int k2 = 0; k2 < KK / 2; ++k2) {
+      if (k2 + 1 < KK / 2) kload((k2 + 1) & 1, k2 + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int ps = 0; ps < 2; ++ps) {
+          const int kk = 2 * k2 + i;
+          S[ps] = mfma_h(kf[k2 & 1][i][ps][0], Q[0][kk], S[ps]);
+          if constexpr (PL == 2) {
+            S[ps] = mfma_h(kf[k2 & 1][i][ps][0], Q[PL - 1][kk], S[ps]);
+            S[ps] = mfma_h(kf[k2 & 1][i][ps][PL - 1], Q[0][kk], S[ps]);
+          }
         }
-      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
     // hidden positions: after the lane's token, or before its window and no sink
     const bool whole = t0 + kStep - 1 <= wlo && (a.window == 0 || t0 > whi - a.window || t0 + kStep <= a.sinks);
     if (!whole) {
@@ -658,10 +688,19 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
         for (int e = 0; e < 16; ++e) O[ct][e] *= al;
     }
     const float off = kPBias - (m == -INFINITY ? 0.0f : m * cs);
-    f16x8_t P[PL][4];
     float ls[2] = {0.0f, 0.0f};
-#pragma unroll
-    for (int kp = 0; kp < 4; ++kp) {
+    // values: element e of the lane's operand is position 16 kp + 8 (e / 4) + 4 hc + e % 4
+    const uint8_t* vb = buf + kStep * SH::KP + (4 * hc + ((lane >> 2) & 3)) * SH::VP + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+    auto vfrag = [&](int plane, int ct, int kp) {
+      typedef __attribute__((address_space(3))) s16x4_t* lds4;
+      const uint8_t* src = vb + plane * SH::plane + 16 * kp * SH::VP + 64 * ct;
+      const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(src));
+      const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(src + 8 * SH::VP));
+      return __builtin_bit_cast(f16x8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    // probabilities of K-step kp, operands in P
+    f16x8_t P[2][PL];
+    auto weights = [&](int s, int kp) {
       u32x4_t hi, lo;
 #pragma unroll
       for (int e2 = 0; e2 < 4; ++e2) {
@@ -673,31 +712,45 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
         hi[e2] = pk_h(p0, p1);
         if constexpr (PL == 2) lo[e2] = pk_h(p0 - h_lo(hi[e2]), p1 - h_hi(hi[e2]));
       }
-      P[0][kp] = as_f16x8(hi);
-      if constexpr (PL == 2) P[PL - 1][kp] = as_f16x8(lo);
-    }
-    lsum += ls[0] + ls[1];
-    // values: element e of the lane's operand is position 16 kp + 8 (e / 4) + 4 hc + e % 4
-    const uint8_t* vb = buf + kStep * SH::KP + (4 * hc + ((lane >> 2) & 3)) * SH::VP + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
-    auto vfrag = [&](int plane, int ct, int kp) {
-      typedef __attribute__((address_space(3))) s16x4_t* lds4;
-      const uint8_t* src = vb + plane * SH::plane + 16 * kp * SH::VP + 64 * ct;
-      const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(src));
-      const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(src + 8 * SH::VP));
-      return __builtin_bit_cast(f16x8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+      P[s][0] = as_f16x8(hi);
+      if constexpr (PL == 2) P[s][PL - 1] = as_f16x8(lo);
     };
+    // the products of K-step kp run while the probabilities of the next are computed
+    constexpr int CB = CT < 4 ? CT : 4;  // channel tiles whose operands are loaded together
+    f16x8_t vf[2][CB][PL];
+    auto vload = [&](int s, int x) {  // batch x: K-step x / (CT / CB), channel tiles CB (x % (CT / CB)) ..
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
+      for (int i = 0; i < CB; ++i)
 #pragma unroll
-      for (int kp = 0; kp < 4; ++kp) {
-        const f16x8_t x0 = vfrag(0, ct, kp);
-        O[ct] = mfma_h(x0, P[0][kp], O[ct]);
+        for (int p = 0; p < PL; ++p) vf[s][i][p] = vfrag(p, CB * (x % (CT / CB)) + i, x / (CT / CB));
+    };
+    constexpr int NB = 4 * (CT / CB);
+    vload(0, 0);
+    weights(0, 0);
+#pragma unroll
+    for (int x = 0; x < NB; ++x) {
+      const int kp = x / (CT / CB), c0 = CB * (x % (CT / CB));
+      if (x + 1 < NB) vload((x + 1) & 1, x + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < CB; ++i) {
+        O[c0 + i] = mfma_h(vf[x & 1][i][0], P[kp & 1][0], O[c0 + i]);
         if constexpr (PL == 2) {
-          const f16x8_t x1 = vfrag(1, ct, kp);
-          O[ct] = mfma_h(x0, P[PL - 1][kp], O[ct]);
-          O[ct] = mfma_h(x1, P[0][kp], O[ct]);
+          O[c0 + i] = mfma_h(vf[x & 1][i][0], P[kp & 1][PL - 1], O[c0 + i]);
+          O[c0 + i] = mfma_h(vf[x & 1][i][PL - 1], P[kp & 1][0], O[c0 + i]);
         }
       }
+      if (c0 == 0 && kp + 1 < 4) weights((kp + 1) & 1, kp + 1);
+      if (x + 1 < NB) {
+#pragma unroll
+        for (int i = 0; i < CB * (PL == 2 ? 3 : 1); ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x402, 9, 0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    lsum += ls[0] + ls[1];
   }
   // ---- o = G_V^T (sums / normaliser): the sums are the B operand as they lie
   const float lall = halves_sum(lsum), inv = lall == 0.0f ? 0.0f : 1.0f / lall;  // nothing visible: zeros
@@ -811,7 +864,10 @@ __global__ __launch_bounds__(256) void chunk_join(ChunkDev a) {
 
 template <int D, int PL, int NW>
 hipError_t run_chunk(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st) {
-  const void* fn = reinterpret_cast<const void*>(chunk_attend<D, PL, NW>);
+  // runs of 32 channels with one side word each; everything else four channels at a time
+  const bool wide = c.backend == CG_BACKEND_BLOCK_UNIFORM && c.n % 32 == 0 && a.q.d % 32 == 0;
+  const void* fn = wide ? reinterpret_cast<const void*>(chunk_attend<D, PL, NW, true>)
+                        : reinterpret_cast<const void*>(chunk_attend<D, PL, NW, false>);
   const int smem = ChunkShape<D, PL>::bytes;
   if (smem > 65536) {
     const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
