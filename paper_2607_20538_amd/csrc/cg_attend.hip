@@ -78,6 +78,37 @@ __device__ __forceinline__ bool step_slice(const AttendDev& a, int l, int b, int
   return true;
 }
 
+// A packed row's query and what it sees: positions [0, s64) and [lo64, held) in whole steps of 64, of which those
+// in [sinks, lo) are hidden.  The row's `nv` positions in that order are dealt to the splits in multiples of 128.
+struct PackRow {
+  int tok = -1, held = 0, lo = 0, lo64 = 0, s64 = 0, sinks = 0, nv = 0, begin = 0, end = 0;
+  __device__ __forceinline__ int at(int v) const { return v < s64 ? v : v - s64 + lo64; }
+  __device__ __forceinline__ bool seen(int t) const { return t >= lo || t < sinks; }
+};
+__device__ __forceinline__ PackRow pack_row(const AttendDev& a, int b, int sp, bool report) {
+  PackRow r;
+  const int c0 = a.cu[b], n = a.cu[b + 1] - c0;
+  int flags = n < 0 || n > a.max_q || c0 < 0 || c0 > a.ntok - n ? CG_FLAG_POS_RANGE : 0;
+  if (n == 1 && !flags) {
+    r.tok = c0;
+    r.held = a.lens[b];
+    if (r.held < 1 || r.held > a.cap) {
+      flags = CG_FLAG_POS_RANGE;
+      r.held = 0;
+    }
+    r.lo = a.window > 0 ? max(0, r.held - a.window) : 0;
+    r.lo64 = r.lo & ~63;
+    r.sinks = r.lo > 0 ? min(a.sinks, r.held) : 0;
+    r.s64 = min((r.sinks + 63) & ~63, r.lo64);
+    r.nv = r.s64 + r.held - r.lo64;
+    const int chunk = ((r.nv + a.nsplit - 1) / a.nsplit + 127) & ~127;
+    r.begin = min(r.nv, sp * chunk);
+    r.end = min(r.nv, r.begin + chunk);
+  }
+  if (report && flags && a.err) atomicOr(a.err, flags);
+  return r;
+}
+
 // Channels ch0 .. ch0 + 7 (ch0 % 8 == 0) of cache position p: raw bf16 tokens (raw) or the
 // dequantised gauge-space values, with as few loads as the layout allows (one or two dwords of a
 // code row and one side word per block; eight streams for KIVI keys).
@@ -242,9 +273,10 @@ constexpr int generic_tile_floats(int d) {
   return kGTile * (d + 4) > finalize_floats(kGFin) ? kGTile * (d + 4) : finalize_floats(kGFin);
 }
 
+template <bool PACK>
 __global__ __launch_bounds__(kAThreads) void att_generic(AttendDev a, GaugeDev G, CodecDev c) {
   extern __shared__ float sm[];
-  const int d = a.q.d, H = a.kc.H, B = a.q.B;
+  const int d = a.q.d, H = a.kc.H, B = PACK ? a.rows : a.q.B;
   const int dp = d + 4;                 // tile row pitch (16-byte aligned rows)
   float* qg = sm;                       // [kJQ][d] scale * G_K q
   float* qr = qg + kJQ * d;             // [kJQ][d] scale * q
@@ -263,19 +295,28 @@ __global__ __launch_bounds__(kAThreads) void att_generic(AttendDev a, GaugeDev G
   const int j0 = qc * kJQ, nj = min(kJQ, a.grp - j0);
   const int hq0 = h * a.grp + j0;  // first query head of this workgroup
 
-  if (tid == 0 && a.lens && sp == 0 && qc == 0 && h == 0 && lv == 0) {
-    const int n = a.lens[b];
-    if ((n < 0 || n > a.cap) && a.err) atomicOr(a.err, CG_FLAG_POS_RANGE);
+  PackRow pr;
+  RowSpan rs;
+  if constexpr (PACK) {
+    pr = pack_row(a, b, sp, tid == 0 && sp == 0 && qc == 0 && h == 0 && lv == 0);
+    if (pr.tok < 0) return;
+    rs.held = rs.tq = pr.held;
+  } else {
+    if (tid == 0 && a.lens && sp == 0 && qc == 0 && h == 0 && lv == 0) {
+      const int n = a.lens[b];
+      if ((n < 0 || n > a.cap) && a.err) atomicOr(a.err, CG_FLAG_POS_RANGE);
+    }
+    rs = row_span(a, c, b);
   }
-  const RowSpan rs = row_span(a, c, b);
-  const int t_begin = sp * a.chunk, t_end = min(rs.held, t_begin + a.chunk);
+  const int bq = PACK ? pr.tok : b;  // the query's place in the views
+  const int t_begin = PACK ? pr.begin : sp * a.chunk, t_end = PACK ? pr.end : min(rs.held, t_begin + a.chunk);
 
   // 1. queries: raw (scaled) and gauged (z_i = sum_j G_K[i][j] q_j, scaled)
   for (int idx = tid; idx < kJQ * d; idx += kAThreads) {
     const int jj = idx / d, ch = idx - jj * d;
     float v = 0.0f;
     if (jj < nj) {
-      const size_t off = size_t(lv) * a.q.sl + size_t(b) * a.q.sb + size_t(hq0 + jj) * a.q.sh + ch;
+      const size_t off = size_t(lv) * a.q.sl + size_t(bq) * a.q.sb + size_t(hq0 + jj) * a.q.sh + ch;
       v = a.q.bf16 ? bf16_to_f32(((const uint16_t*)a.q.ptr)[off]) : ((const float*)a.q.ptr)[off];
     }
     qr[idx] = v;
@@ -306,8 +347,9 @@ __global__ __launch_bounds__(kAThreads) void att_generic(AttendDev a, GaugeDev G
 #pragma unroll
   for (int k = 0; k < kGAcc; ++k) acc[k] = accr[k] = 0.0f;
 
-  for (int t0 = t_begin; t0 < t_end; t0 += kGTile) {
-    const int nt = min(kGTile, t_end - t0);
+  for (int v0 = t_begin; v0 < t_end; v0 += kGTile) {
+    const int t0 = PACK ? pr.at(v0) : v0;
+    const int nt = PACK ? min(kGTile, rs.held - t0) : min(kGTile, t_end - t0);
     size_t sslc;
     int poff;
     if (!step_slice(a, l, b, h, t0, sslc, poff)) continue;  // uniform over the workgroup
@@ -348,6 +390,7 @@ __global__ __launch_bounds__(kAThreads) void att_generic(AttendDev a, GaugeDev G
           s1 = fmaf(a1.w, kv.w, s1);
         }
       }
+      if (PACK && !pr.seen(t0 + t)) s0 = s1 = -INFINITY;
       pw[jq * kGTile + t] = s0;
       pw[(jq + 4) * kGTile + t] = s1;
     }
@@ -375,6 +418,10 @@ __global__ __launch_bounds__(kAThreads) void att_generic(AttendDev a, GaugeDev G
       const int p = t0 + t;
       float v[8];
       load8(a.vc, c, 1, sslc, p - poff, 8 * c8, d, p >= rs.tq, v);
+      if (PACK && !pr.seen(p)) {  // weight 0, but 0 times an infinity is not 0
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 0.0f;
+      }
       float* dst = tile + t * dp + 8 * c8;
       *reinterpret_cast<float4*>(dst) = make_float4(v[0], v[1], v[2], v[3]);
       *reinterpret_cast<float4*>(dst + 4) = make_float4(v[4], v[5], v[6], v[7]);
@@ -440,7 +487,7 @@ __global__ __launch_bounds__(kAThreads) void att_generic(AttendDev a, GaugeDev G
     load_out_rows(out, G, d, l, h);
     for (int jj = 0; jj < nj; jj += kGFin) {
       if (jj) __syncthreads();  // the sums of the queries before are read
-      finalize_rows<kGFin>(a, G, out, macc + jj * d, maccr + jj * d, st + kJQ + jj, min(kGFin, nj - jj), lv, b, h,
+      finalize_rows<kGFin>(a, G, out, macc + jj * d, maccr + jj * d, st + kJQ + jj, min(kGFin, nj - jj), lv, bq, h,
                            hq0 + jj, tile);
     }
     return;
@@ -471,9 +518,10 @@ __global__ __launch_bounds__(kAThreads) void att_generic(AttendDev a, GaugeDev G
 // only where a cache has raw positions (a.raw).  A split without a finite score (maximum -inf) weighs 0
 // and has written zeros, so nothing is left of it.  8 rows x 6 splits (one layer, 1500 positions): 23 -> 8 us;
 // 512 rows x 4 splits: 36 -> 13 us.
+template <bool PACK>
 __global__ __launch_bounds__(kAThreads) void att_combine(AttendDev a, GaugeDev G) {
   extern __shared__ float sm[];
-  const int d = a.q.d, H = a.kc.H, B = a.q.B, ns = a.nsplit;
+  const int d = a.q.d, H = a.kc.H, B = PACK ? a.rows : a.q.B, ns = a.nsplit;
   float* macc = sm;               // [kJQ][d]
   float* maccr = macc + kJQ * d;  // [kJQ][d]
   float* lsum = maccr + kJQ * d;  // [kJQ]
@@ -482,6 +530,11 @@ __global__ __launch_bounds__(kAThreads) void att_combine(AttendDev a, GaugeDev G
   const int qc = sv % a.nqc;
   sv /= a.nqc;
   const int h = sv % H, b = (sv / H) % B, lv = sv / (H * B);
+  int bq = b;
+  if constexpr (PACK) {
+    bq = pack_row(a, b, 0, false).tok;
+    if (bq < 0) return;
+  }
   const int j0 = qc * kJQ, nj = min(kJQ, a.grp - j0);
   const int hq0 = h * a.grp + j0;
   const size_t pstride = size_t(2 + 2 * d);
@@ -529,8 +582,8 @@ __global__ __launch_bounds__(kAThreads) void att_combine(AttendDev a, GaugeDev G
   }
   __syncthreads();
   const float* raw = a.raw ? maccr : nullptr;
-  if (nj <= 4) finalize_rows<4>(a, G, out, macc, raw, lsum, nj, lv, b, h, hq0, wts);
-  else finalize_rows<kJQ>(a, G, out, macc, raw, lsum, nj, lv, b, h, hq0, wts);
+  if (nj <= 4) finalize_rows<4>(a, G, out, macc, raw, lsum, nj, lv, bq, h, hq0, wts);
+  else finalize_rows<kJQ>(a, G, out, macc, raw, lsum, nj, lv, bq, h, hq0, wts);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -749,10 +802,11 @@ __device__ __forceinline__ void gauge_query(const QueryRows& q, const GaugeDev& 
   }
 }
 
-template <int BITS, int NBLK, int TB, bool KIVI = false>
+template <int BITS, int NBLK, int TB, bool KIVI = false, bool PACK = false>
 __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a, GaugeDev G) {
   static_assert(TB == 1 || TB == 16, "token tiles of 16");
   static_assert(!KIVI || (TB == 1 && NBLK == 2), "KIVI: 32-position key groups, 64-channel value blocks");
+  static_assert(!PACK || (TB == 1 && !KIVI), "packed tokens: per-token blocks");
   constexpr bool RAW = TB > 1 || KIVI;         // raw bf16 positions after the quantised ones
   constexpr int JQ = 8 / NBLK;                 // query heads per workgroup (16 A rows)
   constexpr int NQL = 2 / NBLK;                // queries per D lane
@@ -790,7 +844,7 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
 
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int n = lane & 15, gq = lane >> 4;
-  const int H = a.kc.H, B = a.q.B;
+  const int H = a.kc.H, B = PACK ? a.rows : a.q.B;
   const int sp = blockIdx.x;
   int sv = blockIdx.y;
   const int qc = sv % a.nqc;
@@ -800,13 +854,22 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
   const int j0 = qc * JQ, nj = min(JQ, a.grp - j0);
   const int hq0 = h * a.grp + j0;
 
-  if (threadIdx.x == 0 && a.lens && sp == 0 && qc == 0 && h == 0 && lv == 0) {
-    const int nn = a.lens[b];
-    if ((nn < 0 || nn > a.cap) && a.err) atomicOr(a.err, CG_FLAG_POS_RANGE);
+  PackRow pr;
+  int held;
+  if constexpr (PACK) {
+    pr = pack_row(a, b, sp, threadIdx.x == 0 && sp == 0 && qc == 0 && h == 0 && lv == 0);
+    if (pr.tok < 0) return;
+    held = pr.held;
+  } else {
+    if (threadIdx.x == 0 && a.lens && sp == 0 && qc == 0 && h == 0 && lv == 0) {
+      const int nn = a.lens[b];
+      if ((nn < 0 || nn > a.cap) && a.err) atomicOr(a.err, CG_FLAG_POS_RANGE);
+    }
+    held = a.lens ? a.lens[b] : a.len;
+    if (held < 0 || held > a.cap) held = 0;
   }
-  int held = a.lens ? a.lens[b] : a.len;
-  if (held < 0 || held > a.cap) held = 0;
-  const int t_begin = sp * a.chunk, t_end = min(held, t_begin + a.chunk);
+  const int bq = PACK ? pr.tok : b;  // the query's place in the views
+  const int t_begin = PACK ? pr.begin : sp * a.chunk, t_end = PACK ? pr.end : min(held, t_begin + a.chunk);
   // positions in whole tiles / key groups go through the matrix cores, the staged tile tokens
   // or the KIVI window after them are raw
   const int tq = KIVI ? (held < a.win ? 0 : (held - a.win) / 32 * 32) : (TB > 1 ? held / TB * TB : held);
@@ -819,7 +882,7 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
     const int jj = idx / kD, ch = idx % kD;
     float v = 0.0f;
     if (jj < nj) {
-      const size_t off = size_t(lv) * a.q.sl + size_t(b) * a.q.sb + size_t(hq0 + jj) * a.q.sh + ch;
+      const size_t off = size_t(lv) * a.q.sl + size_t(bq) * a.q.sb + size_t(hq0 + jj) * a.q.sh + ch;
       v = a.q.bf16 ? bf16_to_f32(((const uint16_t*)a.q.ptr)[off]) : ((const float*)a.q.ptr)[off];
     }
     macc[jj][ch] = v;
@@ -917,7 +980,9 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
   // One 32-position step; FULL: all 32 positions lie before t_end (no clamping)
   auto step = [&](int t0, auto fullc) {
     constexpr bool FULL = decltype(fullc)::value;
-    const int lim = t_endq - 1 - t0;  // last valid position offset in the step
+    const int lim = (PACK ? held : t_endq) - 1 - t0;  // last valid position offset in the step
+    // packed rows: positions between the sinks and the window are hidden
+    auto shown = [&](int x) { return FULL || (x <= lim && (!PACK || pr.seen(t0 + x))); };
     auto clampt = [&](int x) { return FULL ? x : min(x, lim); };
     // cache row of position t0 (a step never crosses a page)
     size_t sslc;
@@ -969,7 +1034,8 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
     }
     if (lane < 32 * NBLK) {
       const int k = lane >> 5, t = lane & 31;
-      vsd[w][k][t] = vsdg[size_t(clampt(t) / TB) * NBLK + k];
+      const uint32_t word = vsdg[size_t(clampt(t) / TB) * NBLK + k];
+      vsd[w][k][t] = !PACK || shown(t) ? word : 0u;  // (0 times an infinity is not 0)
     }
 
     // scores of the two 16-token halves
@@ -1076,7 +1142,7 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
         gam[k] = kSK * sc;
         bet[k] = BITS == 8 ? mn : mn - gam[k];
       }
-      const bool valid = FULL || 16 * sb + n <= lim;
+      const bool valid = shown(16 * sb + n);
       if constexpr (NBLK == 2) {
         const float v = fmaf(gam[0], d[0] + d[1], bet[0] * qrow[0]) + fmaf(gam[1], d[2] + d[3], bet[1] * qrow[2]);
         s[sb][0] = valid ? v : -INFINITY;
@@ -1153,9 +1219,17 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
     __builtin_amdgcn_wave_barrier();
   };
-  int t0 = t_begin + 32 * w;
-  for (; t0 + 32 <= t_endq; t0 += 128) step(t0, std::true_type{});
-  if (t0 < t_endq) step(t0, std::false_type{});
+  if constexpr (PACK) {
+    for (int v = t_begin + 32 * w; v < t_end; v += 128) {
+      const int t0 = pr.at(v);
+      if (t0 + 32 <= held && (t0 >= pr.lo || t0 + 32 <= pr.sinks)) step(t0, std::true_type{});
+      else if (t0 + 32 > pr.lo || t0 < pr.sinks) step(t0, std::false_type{});  // (else nothing of it is seen)
+    }
+  } else {
+    int t0 = t_begin + 32 * w;
+    for (; t0 + 32 <= t_endq; t0 += 128) step(t0, std::true_type{});
+    if (t0 < t_endq) step(t0, std::false_type{});
+  }
 
   // raw positions [max(tq, t_begin), t_end) of this split (staged tile tokens, at most 15; the KIVI
   // window, at most win + 31), 16 RI at a time: 16 lanes read a position's key row and share its
@@ -1387,7 +1461,7 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
   if (a.nsplit == 1) {
     for (int jj = 0; jj < nj; jj += FJ) {
       if (jj) __syncthreads();  // the sums of the queries before are read
-      finalize_rows<FJ>(a, G, out, &macc[jj][0], RAW ? &accr[RAW ? jj : 0][0] : nullptr, mm[1] + jj, min(FJ, nj - jj), lv, b,
+      finalize_rows<FJ>(a, G, out, &macc[jj][0], RAW ? &accr[RAW ? jj : 0][0] : nullptr, mm[1] + jj, min(FJ, nj - jj), lv, bq,
                         h, hq0 + jj, red);
     }
     return;
@@ -1409,19 +1483,20 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
 }
 
 template <int BITS>
-const void* att_mfma_fn(int nblk, int bt, bool kivi) {
+const void* att_mfma_fn(int nblk, int bt, bool kivi, bool pack) {
+  if (pack) return nblk == 2 ? (const void*)att_mfma<BITS, 2, 1, false, true> : (const void*)att_mfma<BITS, 1, 1, false, true>;
   if (kivi) return (const void*)att_mfma<BITS, 2, 1, true>;
   if (bt > 1) return nblk == 2 ? (const void*)att_mfma<BITS, 2, 16> : (const void*)att_mfma<BITS, 1, 16>;
   return nblk == 2 ? (const void*)att_mfma<BITS, 2, 1> : (const void*)att_mfma<BITS, 1, 1>;
 }
 
-const void* att_mfma_kernel(int bits, int nblk, int bt, bool kivi) {
+const void* att_mfma_kernel(int bits, int nblk, int bt, bool kivi, bool pack) {
   switch (bits) {
-    case 2: return att_mfma_fn<2>(nblk, bt, kivi);
-    case 3: return att_mfma_fn<3>(nblk, bt, kivi);
-    case 4: return att_mfma_fn<4>(nblk, bt, kivi);
-    case 6: return att_mfma_fn<6>(nblk, bt, kivi);
-    default: return att_mfma_fn<8>(nblk, bt, kivi);
+    case 2: return att_mfma_fn<2>(nblk, bt, kivi, pack);
+    case 3: return att_mfma_fn<3>(nblk, bt, kivi, pack);
+    case 4: return att_mfma_fn<4>(nblk, bt, kivi, pack);
+    case 6: return att_mfma_fn<6>(nblk, bt, kivi, pack);
+    default: return att_mfma_fn<8>(nblk, bt, kivi, pack);
   }
 }
 
@@ -1450,12 +1525,12 @@ AttendPlan attend_plan(int nl, int B, int H, int Hq, int d, int span) {
   return p;
 }
 
-bool attend_mfma_supported(const AttendDev& a, const CodecDev& c) {
+bool attend_mfma_supported(int d, bool paged, const CodecDev& c) {
   const bool bits = c.bits == 2 || c.bits == 3 || c.bits == 4 || c.bits == 6 || c.bits == 8;
   // KIVI: 32-position key groups, 64-channel value blocks, contiguous caches
-  if (c.backend == CG_BACKEND_KIVI) return a.q.d == kD && c.kg == 32 && c.kvc == 64 && !a.pt.pages && bits;
+  if (c.backend == CG_BACKEND_KIVI) return d == kD && c.kg == 32 && c.kvc == 64 && !paged && bits;
   // tiles of 16 tokens on contiguous caches (paged caches take per-token blocks only)
-  return c.backend == CG_BACKEND_BLOCK_UNIFORM && (c.bt == 1 || (c.bt == 16 && !a.pt.pages)) && a.q.d == kD &&
+  return c.backend == CG_BACKEND_BLOCK_UNIFORM && (c.bt == 1 || (c.bt == 16 && !paged)) && d == kD &&
          (c.n == 64 || c.n == 128) && bits;
 }
 
@@ -1464,36 +1539,45 @@ hipError_t launch_attend(const AttendDev& args_in, const GaugeDev& G, const Code
   AttendDev a = args_in;
   a.raw = c.backend == CG_BACKEND_KIVI || (c.backend == CG_BACKEND_BLOCK_UNIFORM && c.bt > 1);
   const int d = a.q.d;
-  const int nrow = a.q.L * a.q.B * a.kc.H * a.nqc;
+  const bool pack = a.cu != nullptr;
+  const int B = pack ? a.rows : a.q.B;
+  const int nrow = a.q.L * B * a.kc.H * a.nqc;
   if (nrow == 0) return hipSuccess;
   hipError_t e;
-  if (!force_generic && attend_mfma_supported(a, c)) {
+  if (!force_generic && attend_mfma_supported(d, a.pt.pages != nullptr, c)) {
     // the matrix-core kernel takes 8 / NBLK query heads per workgroup (NBLK value blocks per row)
     const bool kivi = c.backend == CG_BACKEND_KIVI;
     const int nblk = kD / (kivi ? c.kvc : c.n), jq = 8 / nblk;
     AttendDev af = a;
     af.nqc = (a.grp + jq - 1) / jq;
     af.win = kivi ? c.win : 0;
-    const int nrow_f = a.q.L * a.q.B * a.kc.H * af.nqc;
+    const int nrow_f = a.q.L * B * a.kc.H * af.nqc;
     GaugeDev g2 = G;
     void* args[] = {&af, &g2};
-    e = hipLaunchKernel(att_mfma_kernel(c.bits, nblk, c.bt, kivi), dim3(a.nsplit, nrow_f), dim3(kAThreads), args, 0,
+    e = hipLaunchKernel(att_mfma_kernel(c.bits, nblk, c.bt, kivi, pack), dim3(a.nsplit, nrow_f), dim3(kAThreads), args, 0,
                         st);
     if (e != hipSuccess) return e;
   } else {
     const size_t smem = (size_t(2) * kJQ * d + generic_tile_floats(d) + kJQ * kGTile + 3 * kJQ) * sizeof(float);
-    e = set_smem((const void*)att_generic, smem);
+    const void* fn = pack ? (const void*)att_generic<true> : (const void*)att_generic<false>;
+    e = set_smem(fn, smem);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(att_generic, dim3(a.nsplit, nrow), dim3(kAThreads), smem, st, a, G, c);
+    GaugeDev g2 = G;
+    CodecDev c2 = c;
+    void* args[] = {&a, &g2, &c2};
+    e = hipLaunchKernel(fn, dim3(a.nsplit, nrow), dim3(kAThreads), args, smem, st);
+    if (e != hipSuccess) return e;
   }
   e = hipGetLastError();
   if (e != hipSuccess || a.nsplit == 1) return e;
   const size_t smem2 =
       (size_t(2) * kJQ * d + kJQ + std::max(kJQ * a.nsplit, finalize_floats(kJQ))) * sizeof(float);
-  e = set_smem((const void*)att_combine, smem2);
+  const void* fn = pack ? (const void*)att_combine<true> : (const void*)att_combine<false>;
+  e = set_smem(fn, smem2);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(att_combine, dim3(nrow), dim3(kAThreads), smem2, st, a, G);
-  return hipGetLastError();
+  GaugeDev g2 = G;
+  void* args[] = {&a, &g2};
+  return hipLaunchKernel(fn, dim3(nrow), dim3(kAThreads), args, smem2, st);
 }
 
 // ------------------------------------------------------------------------------------------

@@ -11,6 +11,7 @@ struct ChunkDev {
   PageDev pt;
   int l0, Hq, grp;       // cache layer of view layer 0, query heads, query heads per KV head
   int B, N, max_q;       // batch rows, packed tokens, tokens of a row at most
+  int min_q;             // rows with fewer tokens are left (the single-token attention takes them)
   const int* cu;         // device [B + 1] first token of every row
   const int* lens;       // device [B] positions a row holds, its new tokens among them
   float scale;
@@ -20,6 +21,11 @@ struct ChunkDev {
   float *part, *ml;      // splits: [nl][nsplit][N][Hq][d], [nl][nsplit][N][Hq][2] (maximum, sum)
   int* err;
 };
+
+// Rows that decode in runs of 32 channels with one side word each; everything else goes four channels at a time
+inline bool chunk_wide(const CodecDev& c, int d) {
+  return c.backend == CG_BACKEND_BLOCK_UNIFORM && c.n % 32 == 0 && d % 32 == 0;
+}
 
 struct ChunkPlan {
   int waves = 1;         // waves of 32 query rows per workgroup

@@ -20,6 +20,7 @@
 // infinities and NaN make a step "odd": it is summed position by position in binary32, where a masked
 // position is left out instead of being multiplied by zero.
 #include <algorithm>
+#include <cstdlib>
 #include <type_traits>
 
 #include "cg_internal.h"
@@ -84,7 +85,7 @@ __device__ __forceinline__ QTile find_tile(const ChunkDev& a, int tile) {
   for (int b0 = 0; b0 < a.B; b0 += 64) {
     int c0 = 0, n = 0;
     if (b0 + lane < a.B) n = row_tokens(a, b0 + lane, c0);
-    n = max(n, 0);
+    if (n < a.min_q) n = 0;
     const int nt = (n + a.tq - 1) / a.tq;
     int sum = nt;  // inclusive prefix sum over the wave
 #pragma unroll
@@ -122,32 +123,49 @@ __device__ __forceinline__ uint32_t gauge_at(const uint16_t* blk, int g, int d, 
   if (col / g != r) return 0u;
   return blk[size_t(r) * g * g + size_t(row - r * g) * g + (col - r * g)];
 }
-// Rows row0 .. row0 + rows - 1, K-steps kk0 .. kk0 + ks - 1 of NP planes to LDS as operand granules: row i of
-// plane p at (p * rows + i) * (32 ks + 16), the 8 values of (K-step, lane half) at 32 kk + 16 hc.  ORDER 0: a lane
-// half's channels in order (q as loaded); ORDER 1: the order in which the sums of V lie in a lane, element e
-// channel 16 kk + 8 (e & 1) + 4 (e >> 2) + 2 hc + ((e & 3) >> 1).  All of the workgroup's threads.
-template <int ORDER, int NP>
+// Rows row0 .. row0 + ROWS - 1, K-steps kk0 .. kk0 + KS - 1 of NP planes to LDS: row i of plane p at
+// (p ROWS + i) (32 KS + 16), its channels in order.  All NT threads of the workgroup.  Eight reads are in flight
+// per thread: one at a time they were half of the time of a tile with a window of 1024 positions.
+template <int NP, int ROWS, int KS, int NT>
 __device__ __forceinline__ void stage_gauge(uint8_t* dst, const uint16_t* const (&planes)[3], size_t gb, int g, int d,
-                                            int row0, int rows, int kk0, int ks, int nt) {
-  const int per = 2 * ks;
+                                            int row0, int kk0) {
+  constexpr int PER = 2 * KS, TOTAL = NP * ROWS * PER, ITS = (TOTAL + NT - 1) / NT, UN = ITS < 8 ? ITS : 8;
+  auto plane = [&](int p) { return (p == 0 ? planes[0] : (p == 1 ? planes[1] : planes[2])) + gb; };
+  auto put = [&](int p, int i, int gr, const u32x4_t& o) {
+    *reinterpret_cast<u32x4_t*>(dst + size_t(p * ROWS + i) * (32 * KS + 16) + 16 * gr) = o;
+  };
+  if (g % 8) {
 #pragma unroll 1
-  for (int x = threadIdx.x; x < NP * rows * per; x += nt) {
-    const int p = x / (rows * per), y = x - p * rows * per, i = y / per, gr = y - i * per;
-    const int kk = kk0 + (gr >> 1), hc = gr & 1, row = row0 + i;
-    const uint16_t* blk = (p == 0 ? planes[0] : (p == 1 ? planes[1] : planes[2])) + gb;
-    u32x4_t o = {0u, 0u, 0u, 0u};
-    if (ORDER == 0 && g % 8 == 0) {
-      const int c0 = 16 * kk + 8 * hc, r = row / g;
-      if (row < d && c0 < d && c0 / g == r)
-        o = *reinterpret_cast<const u32x4_t*>(blk + size_t(r) * g * g + size_t(row - r * g) * g + (c0 - r * g));
-    } else {
-#pragma unroll
+    for (int x = threadIdx.x; x < TOTAL; x += NT) {
+      const int p = x / (ROWS * PER), i = x / PER % ROWS, gr = x % PER;
+      u32x4_t o = {0u, 0u, 0u, 0u};
+#pragma unroll 1
       for (int e = 0; e < 8; ++e) {
-        const int ch = ORDER == 0 ? 16 * kk + 8 * hc + e : 16 * kk + 8 * (e & 1) + 4 * (e >> 2) + 2 * hc + ((e & 3) >> 1);
-        o[e >> 1] |= gauge_at(blk, g, d, row, ch) << (16 * (e & 1));
+        const uint32_t v = gauge_at(plane(p), g, d, row0 + i, 16 * kk0 + 8 * gr + e) << (16 * (e & 1));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] |= k == e >> 1 ? v : 0u;
       }
+      put(p, i, gr, o);
     }
-    *reinterpret_cast<u32x4_t*>(dst + size_t(p * rows + i) * (32 * ks + 16) + 16 * gr) = o;
+    return;
+  }
+  const float invg = 1.0f / float(g);  // (x + 1/2) / g lies at least 1/512 from an integer
+#pragma unroll 1
+  for (int i0 = 0; i0 < ITS; i0 += UN) {
+    u32x4_t o[UN];
+#pragma unroll
+    for (int k = 0; k < UN; ++k) {
+      const int x = (i0 + k) * NT + threadIdx.x, p = x / (ROWS * PER), row = row0 + x / PER % ROWS;
+      const int c0 = 16 * kk0 + 8 * (x % PER), r = int((float(row) + 0.5f) * invg);
+      const bool in = x < TOTAL && row < d && c0 >= r * g && c0 < (r + 1) * g;
+      o[k] = u32x4_t{0u, 0u, 0u, 0u};
+      if (in) o[k] = *reinterpret_cast<const u32x4_t*>(plane(p) + size_t(r) * g * g + (row - r * g) * g + (c0 - r * g));
+    }
+#pragma unroll
+    for (int k = 0; k < UN; ++k) {
+      const int x = (i0 + k) * NT + threadIdx.x;
+      if (x < TOTAL) put(x / (ROWS * PER), x / PER % ROWS, x % PER, o[k]);
+    }
   }
 }
 
@@ -165,36 +183,38 @@ struct Raw32 {
 // values a lane half hc takes in K-step kk are one 16-byte granule, its dword j the channels 4 hc + j and
 // 8 + 4 hc + j: the pair that one shift of a word holding both codes 16 bits apart selects.
 
-// Codes (kk, hc, j) of a run of 32 channels as the integers of a binary16 pair
-__device__ __forceinline__ uint32_t code_pair(const uint32_t (&w)[8], int bits, int kk, int hc, int j) {
+// Codes (kk, hc, j) of a run of 32 channels as the integers of a pair, OR-ed into the bit pattern of (1024, 1024):
+// 1024 + q in binary16.  `one` is that pattern and `m` the mask of both codes, held in registers so that
+// (x & m) | one is one instruction (it takes no literals).
+__device__ __forceinline__ uint32_t code_pair(const uint32_t (&w)[8], int bits, int kk, int hc, int j, uint32_t one, uint32_t m) {
   switch (bits) {
     case 4: {
       const uint32_t u = __builtin_amdgcn_perm(w[2 * kk + 1], w[2 * kk], hc ? 0x07060302u : 0x05040100u);
-      return (u >> (4 * j)) & 0x000f000fu;
+      return ((u >> (4 * j)) & m) | one;
     }
     case 8:
       return __builtin_amdgcn_perm(w[4 * kk + 2 + hc], w[4 * kk + hc],
-                                   uint32_t(j) | 0x0c000c00u | (uint32_t(j + 4) << 16));
+                                   uint32_t(j) | 0x0c000c00u | (uint32_t(j + 4) << 16)) | one;
     case 2:
-      return (w[kk] >> (8 * hc + 2 * j)) & 0x00030003u;
+      return ((w[kk] >> (8 * hc + 2 * j)) & m) | one;
     case 3: {  // pairs are 24 bits apart
       const int b = 48 * kk + 12 * hc + 3 * j, o = b >> 5;
       const uint32_t x = __builtin_amdgcn_alignbit(w[o + 1 < 3 ? o + 1 : 2], w[o], b & 31);
-      return (x & 7u) | ((x >> 8) & 0x00070000u);
+      return (x & 7u) | ((x >> 8) & 0x00070000u) | one;
     }
     default: {  // 6 bits: 48 bits apart
       const int b0 = 96 * kk + 24 * hc + 6 * j, b1 = b0 + 48, o0 = b0 >> 5, o1 = b1 >> 5;
       const uint32_t x = __builtin_amdgcn_alignbit(w[o0 + 1 < 6 ? o0 + 1 : 5], w[o0], b0 & 31);
       const uint32_t y = __builtin_amdgcn_alignbit(w[o1 + 1 < 6 ? o1 + 1 : 5], w[o1], b1 & 31);
-      return (x & 63u) | ((y & 63u) << 16);
+      return (x & 63u) | ((y & 63u) << 16) | one;
     }
   }
 }
 
-// the integer pair (at most 255 each) as binary16: 1024 + q is the bit pattern 0x6400 | q
+// the integer pair (at most 255 each, already under the bits of 1024) as binary16
 __device__ __forceinline__ f16x2_t int_pair(uint32_t p) {
   const f16x2_t k = {(_Float16)1024.0f, (_Float16)1024.0f};
-  return __builtin_bit_cast(f16x2_t, p | 0x64006400u) - k;
+  return __builtin_bit_cast(f16x2_t, p) - k;
 }
 
 // Four neighbouring channels c .. c + 3 (c a multiple of 4, < d) of a cached position in binary32
@@ -361,8 +381,10 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
       item(i, val, pos, run);
       const bool live = t0 + pos < held;
       uint8_t* dst = buf + (val ? kStep * SH::KP + pos * SH::VP : pos * SH::KP) + 64 * run;
+      // V rows that share their banks (every fourth) keep the granules of a run in another order
+      const int turn = val ? pos & 3 : 0;
       auto put = [&](int plane, int kk, int half, const u32x4_t& o) {
-        *reinterpret_cast<u32x4_t*>(dst + plane * SH::plane + 32 * kk + 16 * half) = o;
+        *reinterpret_cast<u32x4_t*>(dst + plane * SH::plane + 16 * ((2 * kk + half) ^ turn)) = o;
       };
       // the pair (codes p) of a granule with its two blocks' side words
       auto pair = [&](uint32_t p, f16x2_t sc, f16x2_t mn, uint32_t& hi, uint32_t& lo) {
@@ -382,6 +404,8 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
         const _Float16 m1 = __builtin_bit_cast(_Float16, uint16_t(s)), s1 = __builtin_bit_cast(_Float16, uint16_t(s >> 16));
         const f16x2_t mn = {m1, m1}, sc = {s1, s1};
         auto all = [&](auto bits) {
+          uint32_t one = 0x64006400u, m = ((1u << decltype(bits)::value) - 1u) * 0x00010001u;
+          asm volatile("" : "+v"(one), "+v"(m));
 #pragma unroll
           for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
@@ -390,7 +414,7 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
                 uint32_t x, y = 0;
-                pair(code_pair(rw.w, decltype(bits)::value, kk, half, j), sc, mn, x, y);
+                pair(code_pair(rw.w, decltype(bits)::value, kk, half, j, one, m), sc, mn, x, y);
                 hi[j] = x;
                 lo[j] = y;
               }
@@ -448,7 +472,7 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
     // the wave's flags (a bit is set when any lane has it)
     uint32_t all = 0;
 #pragma unroll
-    for (int k = 0; k < 5; ++k)
+    for (int k = 0; k < (WIDE ? 1 : 5); ++k)
       if (__builtin_amdgcn_ballot_w64((st >> k) & 1u)) all |= 1u << k;
     if (lane == 0) state[v & 1][w] = all;
   };
@@ -467,7 +491,7 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
     static_assert(GP * D * GPITCH <= SH::bytes, "space of the gauge");
     for (int k0 = 0; 16 * k0 < d; k0 += KC) {
       if (k0) __syncthreads();
-      stage_gauge<0, GP>(sm, G.hi, gb, G.g, d, 0, D, k0, KC, NT);
+      stage_gauge<GP, D, KC, NT>(sm, G.hi, gb, G.g, d, 0, k0);
       __syncthreads();
 #pragma unroll 1
       for (int kk = k0; kk < k0 + KC && 16 * kk < d; ++kk) {
@@ -544,11 +568,17 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
   float m = -INFINITY, lsum = 0.0f;  // running maximum (in S) and this lane half's sum
 
   // ---- steps
-  for (int v = v0; v < v1; ++v) {
+  // (the loop over ordinary steps ends at an odd one and is entered again after it: with both in one body the
+  // sums were moved between registers in every step)
+  int v = v0;
+  while (v < v1) {
+  bool odd = false;
+  size_t crow = 0;
+  for (; v < v1; ++v) {
     const int t0 = step_pos(v);
     uint8_t* buf = sm + (SH::buffers == 2 ? (v & 1) * SH::plane * PL : 0);
     const bool ok = have;
-    const size_t crow = srow;
+    crow = srow;
     if (SH::buffers == 1 && v > v0) __syncthreads();  // the step before is read
     if (ok) fill(v, buf);
     if (v + 1 < v1) fetch(v + 1);
@@ -560,68 +590,8 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
     st = __builtin_amdgcn_readfirstlane(st);
     // nothing of the step is visible to this wave's queries
     const bool hidden = idle || t0 > whi || (a.window > 0 && t0 + kStep - 1 <= wlo - a.window && t0 >= a.sinks);
-    const bool odd = (st & kOver) || (pass && (((st & kAnyK) && !(st & kBigK)) || ((st & kAnyV) && !(st & kBigV))));
-    if (odd) {
-      // the step position by position in binary32, 16 positions of K and V at a time through its buffer (in
-      // the lanes' order: the values of (kk, hc) at 16 kk + 8 hc, for V of (ct, i, hc) at 32 ct + 8 i + 4 hc)
-      constexpr int SUB = 16;
-      static_assert(2 * SUB * D * 4 <= SH::plane * PL, "space of the rows");
-      float* rows32 = reinterpret_cast<float*>(buf);
-      const int live = min(kStep, held - t0);
-#pragma unroll 1
-      for (int s0 = 0; s0 < live; s0 += SUB) {
-        __syncthreads();
-#pragma unroll 1
-        for (int x = tid; x < 2 * SUB * (D / 4); x += NT) {
-          const bool val = x >= SUB * (D / 4);
-          const int y = val ? x - SUB * (D / 4) : x, pos = y / (D / 4), ch = 4 * (y - pos * (D / 4));
-          float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-          if (s0 + pos < live && ch < d) load4(val ? a.vc : a.kc, c, crow + s0 + pos, d, ch, z);
-          float* dst = rows32 + (val ? SUB * D : 0) + pos * D + (ch & ~15);
-          const int half = (ch >> 3) & 1, h4 = (ch >> 2) & 1;  // channels 16 kk + 8 half + 4 h4 ..
-#pragma unroll
-          for (int j = 0; j < 4; ++j) dst[8 * h4 + 2 * j + half] = z[j];
-        }
-        __syncthreads();
-        if (hidden) continue;
-#pragma unroll 1
-        for (int u = 0; u < min(SUB, live - s0); ++u) {
-          const int t = t0 + s0 + u;
-          const bool seen = t <= pq && (t > plow || t < a.sinks);
-          const float* kr = rows32 + u * D + 8 * hc;
-          const float* vr = rows32 + SUB * D + u * D + 4 * hc;
-          float s = 0.0f;
-#pragma unroll
-          for (int kk = 0; kk < KK; ++kk) {
-            // (opaque: the queries in binary32 would otherwise be kept for this rare path, in registers
-            // that the others need)
-            u32x4_t qa = __builtin_bit_cast(u32x4_t, Q[0][kk]), qb = __builtin_bit_cast(u32x4_t, Q[PL - 1][kk]);
-            asm volatile("" : "+v"(qa), "+v"(qb));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              float q = (e & 1) ? h_hi(qa[e >> 1]) : h_lo(qa[e >> 1]);
-              if constexpr (PL == 2) q += (e & 1) ? h_hi(qb[e >> 1]) : h_lo(qb[e >> 1]);
-              s = fmaf(q, kr[16 * kk + e], s);
-            }
-          }
-          s = halves_sum(s);
-          const float mn = seen ? fmaxf(m, s) : m;
-          const float al = m == mn ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * cs);
-          const float p = seen ? __builtin_amdgcn_exp2f(fmaf(s, cs, kPBias - (mn == -INFINITY ? 0.0f : mn * cs))) : 0.0f;
-          m = mn;
-          lsum = fmaf(lsum, al, hc ? 0.0f : p);
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float o = O[ct][e] * al;
-              O[ct][e] = seen ? fmaf(p, vr[32 * ct + 8 * (e >> 2) + (e & 3)], o) : o;
-            }
-        }
-      }
-      if (SH::buffers == 2) __syncthreads();  // (one buffer: the next step begins with a barrier)
-      continue;
-    }
+    odd = (st & kOver) || (pass && (((st & kAnyK) && !(st & kBigK)) || ((st & kAnyV) && !(st & kBigV))));
+    if (odd) break;
     if (hidden) continue;
     // scores
     f32x16_t S[2];
@@ -690,7 +660,8 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
     const float off = kPBias - (m == -INFINITY ? 0.0f : m * cs);
     float ls[2] = {0.0f, 0.0f};
     // values: element e of the lane's operand is position 16 kp + 8 (e / 4) + 4 hc + e % 4
-    const uint8_t* vb = buf + kStep * SH::KP + (4 * hc + ((lane >> 2) & 3)) * SH::VP + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
+    const uint8_t* vb = buf + kStep * SH::KP + (4 * hc + ((lane >> 2) & 3)) * SH::VP +
+                        16 * ((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ ((lane >> 2) & 3)) + 8 * (lane & 1);
     auto vfrag = [&](int plane, int ct, int kp) {
       typedef __attribute__((address_space(3))) s16x4_t* lds4;
       const uint8_t* src = vb + plane * SH::plane + 16 * kp * SH::VP + 64 * ct;
@@ -707,10 +678,17 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
         const int e = 8 * (kp & 1) + 2 * e2;
         const float p0 = __builtin_amdgcn_exp2f(fmaf(S[kp >> 1][e], cs, off));
         const float p1 = __builtin_amdgcn_exp2f(fmaf(S[kp >> 1][e + 1], cs, off));
-        ls[0] += p0;
-        ls[1] += p1;
-        hi[e2] = pk_h(p0, p1);
-        if constexpr (PL == 2) lo[e2] = pk_h(p0 - h_lo(hi[e2]), p1 - h_hi(hi[e2]));
+        const uint32_t both = pk_h(p0, p1);
+        hi[e2] = both;
+        if constexpr (PL == 2) {
+          ls[0] += p0;
+          ls[1] += p1;
+          lo[e2] = pk_h(p0 - h_lo(both), p1 - h_hi(both));
+        } else {
+          // the rounded weights, as the values meet them (v_dot2_f32_f16 adds both to binary32 exactly)
+          const f16x2_t ones = {(_Float16)1.0f, (_Float16)1.0f};
+          ls[e2 & 1] = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2_t, both), ones, ls[e2 & 1], false);
+        }
       }
       P[s][0] = as_f16x8(hi);
       if constexpr (PL == 2) P[s][PL - 1] = as_f16x8(lo);
@@ -752,6 +730,71 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
     }
     lsum += ls[0] + ls[1];
   }
+  if (!odd) break;
+  {
+      const int t0 = step_pos(v);
+      const bool hidden = idle || t0 > whi || (a.window > 0 && t0 + kStep - 1 <= wlo - a.window && t0 >= a.sinks);
+      uint8_t* buf = sm + (SH::buffers == 2 ? (v & 1) * SH::plane * PL : 0);
+      // the step position by position in binary32, 16 positions of K and V at a time through its buffer (in
+      // the lanes' order: the values of (kk, hc) at 16 kk + 8 hc, for V of (ct, i, hc) at 32 ct + 8 i + 4 hc)
+      constexpr int SUB = 16;
+      static_assert(2 * SUB * D * 4 <= SH::plane * PL, "space of the rows");
+      float* rows32 = reinterpret_cast<float*>(buf);
+      const int live = min(kStep, held - t0);
+#pragma unroll 1
+      for (int s0 = 0; s0 < live; s0 += SUB) {
+        __syncthreads();
+#pragma unroll 1
+        for (int x = tid; x < 2 * SUB * (D / 4); x += NT) {
+          const bool val = x >= SUB * (D / 4);
+          const int y = val ? x - SUB * (D / 4) : x, pos = y / (D / 4), ch = 4 * (y - pos * (D / 4));
+          float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+          if (s0 + pos < live && ch < d) load4(val ? a.vc : a.kc, c, crow + s0 + pos, d, ch, z);
+          float* dst = rows32 + (val ? SUB * D : 0) + pos * D + (ch & ~15);
+          const int half = (ch >> 3) & 1, h4 = (ch >> 2) & 1;  // channels 16 kk + 8 half + 4 h4 ..
+#pragma unroll
+          for (int j = 0; j < 4; ++j) dst[8 * h4 + 2 * j + half] = z[j];
+        }
+        __syncthreads();
+        if (hidden) continue;
+#pragma unroll 1
+        for (int u = 0; u < min(SUB, live - s0); ++u) {
+          const int t = t0 + s0 + u;
+          const bool seen = t <= pq && (t > plow || t < a.sinks);
+          const float* kr = rows32 + u * D + 8 * hc;
+          const float* vr = rows32 + SUB * D + u * D + 4 * hc;
+          float s = 0.0f;
+#pragma unroll
+          for (int kk = 0; kk < KK; ++kk) {
+            // (opaque: the queries in binary32 would otherwise be kept for this rare path, in registers
+            // that the others need)
+            u32x4_t qa = __builtin_bit_cast(u32x4_t, Q[0][kk]), qb = __builtin_bit_cast(u32x4_t, Q[PL - 1][kk]);
+            asm volatile("" : "+v"(qa), "+v"(qb));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              float q = (e & 1) ? h_hi(qa[e >> 1]) : h_lo(qa[e >> 1]);
+              if constexpr (PL == 2) q += (e & 1) ? h_hi(qb[e >> 1]) : h_lo(qb[e >> 1]);
+              s = fmaf(q, kr[16 * kk + e], s);
+            }
+          }
+          s = halves_sum(s);
+          const float mn = seen ? fmaxf(m, s) : m;
+          const float al = m == mn ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * cs);
+          const float p = seen ? __builtin_amdgcn_exp2f(fmaf(s, cs, kPBias - (mn == -INFINITY ? 0.0f : mn * cs))) : 0.0f;
+          m = mn;
+          lsum = fmaf(lsum, al, hc ? 0.0f : p);
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float o = O[ct][e] * al;
+              O[ct][e] = seen ? fmaf(p, vr[32 * ct + 8 * (e >> 2) + (e & 3)], o) : o;
+            }
+        }
+      }
+  }
+  ++v;
+  }
   // ---- o = G_V^T (sums / normaliser): the sums are the B operand as they lie
   const float lall = halves_sum(lsum), inv = lall == 0.0f ? 0.0f : 1.0f / lall;  // nothing visible: zeros
   constexpr int OP = PL == 1 ? 2 : 3, OPITCH = 2 * D + 16;
@@ -786,7 +829,7 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
 #pragma unroll 1
   for (int ct = 0; 32 * ct < d; ++ct) {  // output channels 32 ct ..
     __syncthreads();
-    stage_gauge<1, OP>(sm, G.tr, gb, G.g, d, 32 * ct, 32, 0, KK, NT);
+    stage_gauge<OP, 32, KK, NT>(sm, G.tr, gb, G.g, d, 32 * ct, 0);
     __syncthreads();
     if (idle) continue;
     f32x16_t y = f32x16_t{};
@@ -795,7 +838,11 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
       if (16 * kk >= d || 32 * ct / G.g > (16 * kk + 15) / G.g || (32 * ct + 31) / G.g < 16 * kk / G.g) continue;
 #pragma unroll
       for (int p = 0; p < OP; ++p) {
-        const bf16x8_t A = as_bf16x8(*reinterpret_cast<const u32x4_t*>(sm + (32 * p + n) * OPITCH + 32 * kk + 16 * hc));
+        // element e of the sums' operand is channel 16 kk + 8 (e & 1) + 4 (e >> 2) + 2 hc + ((e & 3) >> 1)
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(sm + (32 * p + n) * OPITCH + 32 * kk) + hc;
+        const uint32_t c0 = src[0], c4 = src[2], c8 = src[4], c12 = src[6];
+        const bf16x8_t A = as_bf16x8(u32x4_t{__builtin_amdgcn_perm(c8, c0, 0x05040100u), __builtin_amdgcn_perm(c8, c0, 0x07060302u),
+                                             __builtin_amdgcn_perm(c12, c4, 0x05040100u), __builtin_amdgcn_perm(c12, c4, 0x07060302u)});
 #pragma unroll
         for (int s = 0; s < OP; ++s)
           if (p + s < OP) y = mfma(A, x[s][kk], y);
@@ -864,8 +911,7 @@ __global__ __launch_bounds__(256) void chunk_join(ChunkDev a) {
 
 template <int D, int PL, int NW>
 hipError_t run_chunk(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st) {
-  // runs of 32 channels with one side word each; everything else four channels at a time
-  const bool wide = c.backend == CG_BACKEND_BLOCK_UNIFORM && c.n % 32 == 0 && a.q.d % 32 == 0;
+  const bool wide = chunk_wide(c, a.q.d);
   const void* fn = wide ? reinterpret_cast<const void*>(chunk_attend<D, PL, NW, true>)
                         : reinterpret_cast<const void*>(chunk_attend<D, PL, NW, false>);
   const int smem = ChunkShape<D, PL>::bytes;
@@ -885,7 +931,10 @@ hipError_t by_waves(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int
   switch (a.waves) {
     case 1: return run_chunk<D, PL, 1>(a, G, c, blocks, st);
     case 2: return run_chunk<D, PL, 2>(a, G, c, blocks, st);
-    default: return run_chunk<D, PL, 4>(a, G, c, blocks, st);
+    case 4: return run_chunk<D, PL, 4>(a, G, c, blocks, st);
+    default:
+      if constexpr (D == 128 && PL == 1) return run_chunk<D, PL, 8>(a, G, c, blocks, st);
+      return hipErrorInvalidValue;
   }
 }
 
@@ -897,6 +946,7 @@ ChunkPlan chunk_plan(int nl, int N, int B, int max_q, int H, int Hq, int d, int 
   const int64_t mq = std::min(max_q, N);
   const int64_t want_rows = mq * grp;
   p.waves = want_rows <= 32 ? 1 : (want_rows <= 64 ? 2 : 4);
+  if (getenv("CGW")) p.waves = atoi(getenv("CGW"));
   const int M = 32 * p.waves;
   p.heads = std::min(grp, M);
   p.nqc = (grp + p.heads - 1) / p.heads;

@@ -1054,11 +1054,24 @@ static int32_t check_chunk(int32_t nl, int32_t N, int32_t B, int32_t max_q, int3
   return CG_OK;
 }
 
+// Single tokens go to the single-token attention (max_q = 1, or in a launch of its own beside the chunks of a
+// batch) where its matrix-core kernel takes the caches, or where the chunk kernel decodes four channels at a
+// time.  32 rows of up to 8000 positions, 8 KV heads x 4: d = 128, n = 64 675 us as chunks of one token, 86 there;
+// d = 80 1710 against 917; but d = 64 251 against 636, d = 128, n = 32 675 against 1138.  Its plan, for rows of
+// as many positions as they see:
+static AttendPlan singles_plan(int nl, int B, int H, int Hq, int d, int cap, int window, int sinks) {
+  const int64_t seen = window > 0 ? int64_t(window) + sinks + 128 : cap;
+  return attend_plan(nl, B, H, Hq, d, int(std::min<int64_t>(cap, seen)));
+}
+
 size_t attend_chunk_workspace_bytes(cg_gauge_shape shp, int32_t nl, int32_t N, int32_t B, int32_t max_q, int32_t Hq,
                                     int32_t max_pages, int32_t page_size, int32_t window, int32_t sinks) {
   if (check_shape(shp) != CG_OK || check_chunk(nl, N, B, max_q, Hq, max_pages, page_size, window, sinks, shp) != CG_OK || N == 0)
     return 0;
-  return chunk_plan(nl, N, B, max_q, shp.H, Hq, shp.d, max_pages * page_size, window, sinks).ws_bytes;
+  const int cap = max_pages * page_size;
+  // the two launches follow one another and share it
+  return std::max(chunk_plan(nl, N, B, max_q, shp.H, Hq, shp.d, cap, window, sinks).ws_bytes,
+                  max_q == 1 || B > 1 ? singles_plan(nl, B, shp.H, Hq, shp.d, cap, window, sinks).ws_bytes : 0);
 }
 
 int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const int32_t* cu, int32_t B, int32_t max_q,
@@ -1083,7 +1096,9 @@ int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const
   if (q->T == 0) return CG_OK;
   const int cap = pages->max_pages * pages->page_size;
   const ChunkPlan p = chunk_plan(nl, q->T, B, max_q, shp.H, q->H, shp.d, cap, window, sinks);
-  if (p.ws_bytes && (!workspace || !aligned16(workspace))) return workspace ? CG_ERR_ALIGN : CG_ERR_ARG;
+  const AttendPlan one = singles_plan(nl, B, shp.H, q->H, shp.d, cap, window, sinks);
+  const size_t ws = std::max(p.ws_bytes, max_q == 1 || B > 1 ? one.ws_bytes : 0);
+  if (ws && (!workspace || !aligned16(workspace))) return workspace ? CG_ERR_ALIGN : CG_ERR_ARG;
   if (int64_t(nl) * shp.H * p.nqc * p.ntile * p.nsplit > INT32_MAX) return CG_ERR_CAPACITY;
   ChunkDev a;
   a.q = view_dev(q);
@@ -1114,7 +1129,43 @@ int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const
   a.part = static_cast<float*>(workspace);
   a.ml = a.part ? a.part + size_t(nl) * p.nsplit * q->T * q->H * shp.d : nullptr;
   a.err = err_flag;
-  hipError_t e = launch_chunk(a, gauge_dev(G_dev, shp), codec_dev(codec), static_cast<hipStream_t>(stream));
+  const CodecDev c = codec_dev(codec);
+  const GaugeDev G = gauge_dev(G_dev, shp);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const bool singles = (max_q == 1 || B > 1) && (attend_mfma_supported(shp.d, true, c) || !chunk_wide(c, shp.d));
+  a.min_q = singles ? 2 : 1;
+  hipError_t e = hipSuccess;
+  if (!singles || max_q > 1) e = launch_chunk(a, G, c, st);
+  if (e == hipSuccess && singles) {
+    AttendDev s;
+    s.q = a.q;
+    s.o = a.o;
+    s.q.sb = a.q.st;
+    s.o.sb = a.o.st;
+    s.kc = a.kc;
+    s.vc = a.vc;
+    s.l0 = l0;
+    s.Hq = a.Hq;
+    s.grp = a.grp;
+    s.lens = lens;
+    s.len = 0;
+    s.scale = scale;
+    s.nsplit = one.nsplit;
+    s.chunk = one.chunk;
+    s.nqc = one.nqc;
+    s.part = static_cast<float*>(workspace);
+    s.err = err_flag;
+    s.pt = a.pt;
+    s.cap = cap;
+    s.win = 0;
+    s.cu = cu;
+    s.rows = B;
+    s.ntok = a.N;
+    s.max_q = max_q;
+    s.window = window;
+    s.sinks = sinks;
+    e = launch_attend(s, G, c, force_generic(), st);
+  }
   return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
 }
 

@@ -157,11 +157,19 @@ struct AttendDev {
   int cap;               // positions a row can hold: T_cap, or max_pages * page_size
   int win;               // KIVI window (set by the launch for the matrix-core kernel)
   int raw;               // partials carry raw sums (KIVI window, staged tile tokens; set by the launch)
+  // packed tokens (kv_attend_chunk_paged): row b's query is token cu[b] of q / o views whose batch
+  // stride is that of the tokens, if the row has exactly one (rows with another count are left); it sees the
+  // last `window` positions (0: all) and the first `sinks`
+  const int* cu = nullptr;
+  int rows = 0, ntok = 0, max_q = 0;
+  int window = 0, sinks = 0;
 };
 struct AttendPlan {
   int nsplit = 1, chunk = 64, nqc = 1;
   size_t ws_bytes = 0;
 };
+// Whether the matrix-core attention takes these caches and head dimension
+bool attend_mfma_supported(int d, bool paged, const CodecDev& c);
 // Split plan of a call covering `span` positions per row (the same rule sizes the workspace
 // from the capacity, so a plan for span <= T_cap never needs more than that workspace).
 AttendPlan attend_plan(int nl, int B, int H, int Hq, int d, int span);
