@@ -36,6 +36,11 @@ struct ChunkPlan {
   size_t ws_bytes = 0;
 };
 ChunkPlan chunk_plan(int nl, int N, int B, int max_q, int H, int Hq, int d, int cap, int window, int sinks);
+// The kernels by rounded row width and result type
+hipError_t run_chunk_64(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st);
+hipError_t run_chunk_128(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st);
+hipError_t run_chunk_256(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st);
+hipError_t run_chunk_f32(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st);
 hipError_t launch_chunk(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, hipStream_t st);
 
 }  // namespace cg

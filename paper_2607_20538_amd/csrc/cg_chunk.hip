@@ -1,870 +1,13 @@
-// Attention of a chunk of new tokens over paged, gauge-coded caches: causal, or with a sliding window and
-// first positions that stay visible.
-//
-// Token i of batch row b (n_b new tokens, lens[b] positions held with them) sits at p = lens[b] - n_b + i and
-//   o = softmax(scale q Khat^T) Vhat   over t <= p with (window == 0 or t > p - window or t < sinks).
-// As in the single-token attention the gauge stays out of the loop over positions: with q' = G_K q and Khat =
-// G_K^T zhat^K the scores are q' . zhat^K_t, and o = G_V^T sum_t p_t zhat^V_t, so it is applied once to the
-// queries of a tile and once to their sums, on the bf16 matrix cores (split planes of G).
-//
-// A workgroup takes 32 NW query rows (tokens x query heads of one KV head) of one batch row and walks their
-// visible positions 64 at a time.  The codes of a step become binary16 zhat = fma(q, sc, mn) in LDS once per
-// workgroup; both products run on v_mfma_f32_32x32x16_f16 with the queries as columns:
-//   S^T = K Q'^T   (lane: one query, half of the 64 positions)  -> softmax without crossing lanes but for one
-//                                                                   swap of the halves per step
-//   O^T += V^T P^T (the lane's own probabilities are its B operand: the order of the contraction is free, so
-//                   V is read in the order that S^T left the positions in, by transposing LDS reads)
-// Binary16 and not bf16: codes are exact in both, zhat, q' (scaled by a power of two to at most 1) and p then
-// carry 11 bits, four times finer than the result's own rounding.  Binary32 results take every operand in
-// two binary16 planes (22 bits, three products).  zhat beyond binary16 (the side information allows 2^24),
-// infinities and NaN make a step "odd": it is summed position by position in binary32, where a masked
-// position is left out instead of being multiplied by zero.
+// Chunk attention: plan, launch, and the joining of splits (the kernel: cg_chunk_kernel.h).
 #include <algorithm>
-#include <cstdlib>
-#include <type_traits>
 
-#include "cg_internal.h"
-#include "cg_device.h"
 #include "cg_chunk.h"
-#include "cg_mfma_util.h"
+#include "cg_chunk_rows.h"
+#include "cg_device.h"
 
 namespace cg {
 
 namespace {
-
-typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x4_t __attribute__((ext_vector_type(4)));
-typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
-typedef float f32x2_t __attribute__((ext_vector_type(2)));
-typedef short s16x4_t __attribute__((ext_vector_type(4)));
-
-constexpr int kStep = 64;  // positions per step
-constexpr float kLog2e = 1.44269504088896340736f;
-// Probabilities are kept times 2^6: with a maximum that lags by at most 2^8 they stay below 2^14, and what is
-// lost below binary16's subnormals is 2^-31 of the largest.
-constexpr float kPBias = 6.0f, kLag = 8.0f;
-
-__device__ __forceinline__ f32x16_t mfma_h(const f16x8_t& a, const f16x8_t& b, const f32x16_t& c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ uint32_t pk_h(float a, float b) {
-  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), f16x2_t));
-}
-__device__ __forceinline__ float h_lo(uint32_t w) { return (float)__builtin_bit_cast(f16x2_t, w)[0]; }
-__device__ __forceinline__ float h_hi(uint32_t w) { return (float)__builtin_bit_cast(f16x2_t, w)[1]; }
-__device__ __forceinline__ f16x8_t as_f16x8(const u32x4_t& v) { return __builtin_bit_cast(f16x8_t, v); }
-
-// the lane's value and that of the lane 32 away
-__device__ __forceinline__ float halves_max(float v) {
-  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-}
-__device__ __forceinline__ float halves_sum(float v) {
-  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(a[0]) + __uint_as_float(a[1]);
-}
-
-// ------------------------------------------------------------------------------------------
-// rows of the batch
-// ------------------------------------------------------------------------------------------
-
-// The tile-th query tile of the batch: its row, the row's tokens and which of them the tile takes.  Every row
-// brings ceil(n_b / tq) tiles, in order; within a row the last tile (which sees the most) comes first.
-struct QTile {
-  int b = -1, tok0 = 0, n = 0, i0 = 0;  // row (-1: past the last tile), first packed token, tokens, first of the tile
-};
-__device__ __forceinline__ int row_tokens(const ChunkDev& a, int b, int& c0) {
-  c0 = a.cu[b];
-  const int n = a.cu[b + 1] - c0;
-  return c0 < 0 || n < 0 || c0 > a.N - n || n > a.max_q ? -1 : n;
-}
-__device__ __forceinline__ QTile find_tile(const ChunkDev& a, int tile) {
-  const int lane = threadIdx.x & 63;
-  int before = 0;
-  QTile r;
-  for (int b0 = 0; b0 < a.B; b0 += 64) {
-    int c0 = 0, n = 0;
-    if (b0 + lane < a.B) n = row_tokens(a, b0 + lane, c0);
-    if (n < a.min_q) n = 0;
-    const int nt = (n + a.tq - 1) / a.tq;
-    int sum = nt;  // inclusive prefix sum over the wave
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const int v = __shfl_up(sum, o);
-      if (lane >= o) sum += v;
-    }
-    const uint64_t hit = __builtin_amdgcn_ballot_w64(tile < before + sum);
-    if (hit) {
-      const int src = __builtin_ctzll(hit);
-      const int first = before + __shfl(sum, src) - __shfl(nt, src);
-      r.b = b0 + src;
-      r.tok0 = __shfl(c0, src);
-      r.n = __shfl(n, src);
-      r.i0 = (__shfl(nt, src) - 1 - (tile - first)) * a.tq;
-      break;
-    }
-    before += __shfl(sum, 63);
-  }
-  r.b = __builtin_amdgcn_readfirstlane(r.b);
-  r.tok0 = __builtin_amdgcn_readfirstlane(r.tok0);
-  r.n = __builtin_amdgcn_readfirstlane(r.n);
-  r.i0 = __builtin_amdgcn_readfirstlane(r.i0);
-  return r;
-}
-
-// ------------------------------------------------------------------------------------------
-// the gauge operands
-// ------------------------------------------------------------------------------------------
-
-// Element (row, col) of a head's block-diagonal matrix out of one bf16 plane (G or G^T); zero outside
-__device__ __forceinline__ uint32_t gauge_at(const uint16_t* blk, int g, int d, int row, int col) {
-  if (row >= d || col >= d) return 0u;
-  const int r = row / g;
-  if (col / g != r) return 0u;
-  return blk[size_t(r) * g * g + size_t(row - r * g) * g + (col - r * g)];
-}
-// Rows row0 .. row0 + ROWS - 1, K-steps kk0 .. kk0 + KS - 1 of NP planes to LDS: row i of plane p at
-// (p ROWS + i) (32 KS + 16), its channels in order.  All NT threads of the workgroup.  Eight reads are in flight
-// per thread: one at a time they were half of the time of a tile with a window of 1024 positions.
-template <int NP, int ROWS, int KS, int NT>
-__device__ __forceinline__ void stage_gauge(uint8_t* dst, const uint16_t* const (&planes)[3], size_t gb, int g, int d,
-                                            int row0, int kk0) {
-  constexpr int PER = 2 * KS, TOTAL = NP * ROWS * PER, ITS = (TOTAL + NT - 1) / NT, UN = ITS < 8 ? ITS : 8;
-  auto plane = [&](int p) { return (p == 0 ? planes[0] : (p == 1 ? planes[1] : planes[2])) + gb; };
-  auto put = [&](int p, int i, int gr, const u32x4_t& o) {
-    *reinterpret_cast<u32x4_t*>(dst + size_t(p * ROWS + i) * (32 * KS + 16) + 16 * gr) = o;
-  };
-  if (g % 8) {
-#pragma unroll 1
-    for (int x = threadIdx.x; x < TOTAL; x += NT) {
-      const int p = x / (ROWS * PER), i = x / PER % ROWS, gr = x % PER;
-      u32x4_t o = {0u, 0u, 0u, 0u};
-#pragma unroll 1
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t v = gauge_at(plane(p), g, d, row0 + i, 16 * kk0 + 8 * gr + e) << (16 * (e & 1));
-#pragma unroll
-        for (int k = 0; k < 4; ++k) o[k] |= k == e >> 1 ? v : 0u;
-      }
-      put(p, i, gr, o);
-    }
-    return;
-  }
-  const float invg = 1.0f / float(g);  // (x + 1/2) / g lies at least 1/512 from an integer
-#pragma unroll 1
-  for (int i0 = 0; i0 < ITS; i0 += UN) {
-    u32x4_t o[UN];
-#pragma unroll
-    for (int k = 0; k < UN; ++k) {
-      const int x = (i0 + k) * NT + threadIdx.x, p = x / (ROWS * PER), row = row0 + x / PER % ROWS;
-      const int c0 = 16 * kk0 + 8 * (x % PER), r = int((float(row) + 0.5f) * invg);
-      const bool in = x < TOTAL && row < d && c0 >= r * g && c0 < (r + 1) * g;
-      o[k] = u32x4_t{0u, 0u, 0u, 0u};
-      if (in) o[k] = *reinterpret_cast<const u32x4_t*>(plane(p) + size_t(r) * g * g + (row - r * g) * g + (c0 - r * g));
-    }
-#pragma unroll
-    for (int k = 0; k < UN; ++k) {
-      const int x = (i0 + k) * NT + threadIdx.x;
-      if (x < TOTAL) put(x / (ROWS * PER), x / PER % ROWS, x % PER, o[k]);
-    }
-  }
-}
-
-// ------------------------------------------------------------------------------------------
-// codes to binary16
-// ------------------------------------------------------------------------------------------
-
-// What a thread holds of 32 neighbouring channels of one position before they go to LDS: the packed words and
-// (blocks of whole runs of 32 channels) their side word.
-struct Raw32 {
-  uint32_t w[8], side;
-};
-
-// Stored order of a row: channels 16 kk + 8 half + 4 hc + j sit at 16 kk + 8 hc + 2 j + half, so that the 8
-// values a lane half hc takes in K-step kk are one 16-byte granule, its dword j the channels 4 hc + j and
-// 8 + 4 hc + j: the pair that one shift of a word holding both codes 16 bits apart selects.
-
-// Codes (kk, hc, j) of a run of 32 channels as the integers of a pair, OR-ed into the bit pattern of (1024, 1024):
-// 1024 + q in binary16.  `one` is that pattern and `m` the mask of both codes, held in registers so that
-// (x & m) | one is one instruction (it takes no literals).
-__device__ __forceinline__ uint32_t code_pair(const uint32_t (&w)[8], int bits, int kk, int hc, int j, uint32_t one, uint32_t m) {
-  switch (bits) {
-    case 4: {
-      const uint32_t u = __builtin_amdgcn_perm(w[2 * kk + 1], w[2 * kk], hc ? 0x07060302u : 0x05040100u);
-      return ((u >> (4 * j)) & m) | one;
-    }
-    case 8:
-      return __builtin_amdgcn_perm(w[4 * kk + 2 + hc], w[4 * kk + hc],
-                                   uint32_t(j) | 0x0c000c00u | (uint32_t(j + 4) << 16)) | one;
-    case 2:
-      return ((w[kk] >> (8 * hc + 2 * j)) & m) | one;
-    case 3: {  // pairs are 24 bits apart
-      const int b = 48 * kk + 12 * hc + 3 * j, o = b >> 5;
-      const uint32_t x = __builtin_amdgcn_alignbit(w[o + 1 < 3 ? o + 1 : 2], w[o], b & 31);
-      return (x & 7u) | ((x >> 8) & 0x00070000u) | one;
-    }
-    default: {  // 6 bits: 48 bits apart
-      const int b0 = 96 * kk + 24 * hc + 6 * j, b1 = b0 + 48, o0 = b0 >> 5, o1 = b1 >> 5;
-      const uint32_t x = __builtin_amdgcn_alignbit(w[o0 + 1 < 6 ? o0 + 1 : 5], w[o0], b0 & 31);
-      const uint32_t y = __builtin_amdgcn_alignbit(w[o1 + 1 < 6 ? o1 + 1 : 5], w[o1], b1 & 31);
-      return (x & 63u) | ((y & 63u) << 16) | one;
-    }
-  }
-}
-
-// the integer pair (at most 255 each, already under the bits of 1024) as binary16
-__device__ __forceinline__ f16x2_t int_pair(uint32_t p) {
-  const f16x2_t k = {(_Float16)1024.0f, (_Float16)1024.0f};
-  return __builtin_bit_cast(f16x2_t, p) - k;
-}
-
-// Four neighbouring channels c .. c + 3 (c a multiple of 4, < d) of a cached position in binary32
-__device__ __forceinline__ void load4(const CacheDev& k, const CodecDev& c, size_t row, int d, int ch, float (&out)[4]) {
-  if (c.backend == CG_BACKEND_PASSTHROUGH) {
-    const float4 v = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(k.codes) + row * d + ch);
-    out[0] = v.x; out[1] = v.y; out[2] = v.z; out[3] = v.w;
-    return;
-  }
-  const uint32_t* w = reinterpret_cast<const uint32_t*>(k.codes) + row * size_t(d * c.bits / 32);
-  const int bit = ch * c.bits, o = bit >> 5, last = d * c.bits / 32 - 1;
-  const uint64_t v = ((uint64_t(w[min(o + 1, last)]) << 32) | w[o]) >> (bit & 31);
-  const uint32_t s = k.side[row * size_t(d / c.n) + ch / c.n];
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    out[e] = dequantize(uint32_t(v >> (c.bits * e)) & ((1u << c.bits) - 1u), f16_bits_to_f32(s & 0xffffu), f16_bits_to_f32(s >> 16));
-}
-
-// ------------------------------------------------------------------------------------------
-// the kernel
-// ------------------------------------------------------------------------------------------
-// D: channels of a row rounded up (zeros past d); PL: binary16 planes of an operand; NW: waves.
-template <int D, int PL>
-struct ChunkShape {
-  static constexpr int KP = 2 * D + 16;                          // bytes between K rows: an odd number of granules
-  static constexpr int VP = 2 * D + (D % 64 == 32 ? 0 : 64);     // V rows: 4 of them cover all banks once (64 mod 128)
-  static constexpr int plane = kStep * (KP + VP);
-  static constexpr int buffers = PL == 1 && D <= 128 ? 2 : 1;
-  static constexpr int bytes = plane * PL * buffers;
-};
-
-template <int D, int PL, int NW, bool WIDE>
-__global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_attend(ChunkDev a, GaugeDev G, CodecDev c) {
-  using SH = ChunkShape<D, PL>;
-  constexpr int NT = 64 * NW, KK = D / 16, CT = D / 32, RUNS = D / 32;
-  constexpr int ITEMS = 2 * kStep * RUNS, IT = (ITEMS + NT - 1) / NT;  // (position, run) of K, then of V
-  static_assert(ITEMS % NT == 0, "items per thread");
-  extern __shared__ __attribute__((aligned(16))) uint8_t sm[];
-  __shared__ uint32_t state[2][NW];  // per step parity and wave: what its items hold (kOver ...)
-  constexpr uint32_t kOver = 1, kBigK = 2, kBigV = 4, kAnyK = 8, kAnyV = 16;
-
-  const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, hc = lane >> 5;
-  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int H = a.kc.H, d = a.q.d, inner = H * a.nqc;
-  int bid = blockIdx.x;
-  const int hq = bid % inner;
-  bid /= inner;
-  const int sp = bid % a.nsplit;
-  bid /= a.nsplit;
-  const int tile = bid % a.ntile, lv = bid / a.ntile;
-  const int h = hq / a.nqc, qc = hq - h * a.nqc, l = lv + a.l0;
-  if (blockIdx.x == 0 && a.err) {  // rows that cannot be taken
-    for (int b = tid; b < a.B; b += NT) {
-      int c0;
-      if (row_tokens(a, b, c0) < 0) atomicOr(a.err, CG_FLAG_POS_RANGE);
-    }
-  }
-  const QTile qt = find_tile(a, tile);
-  if (qt.b < 0) return;
-  const int ntok = min(a.tq, qt.n - qt.i0);
-  const int j0 = qc * a.heads, nh = min(a.heads, a.grp - j0), rows = ntok * nh;
-  int held = a.lens[qt.b];
-  const bool bad_row = held < qt.n || held > a.cap;
-  if (bad_row) {
-    if (tid == 0 && a.err) atomicOr(a.err, CG_FLAG_POS_RANGE);
-    held = 0;
-  }
-  const int pa = held - qt.n + qt.i0, pb = pa + ntok - 1;  // positions of the tile's tokens
-  // steps: those that hold sinks before the window, then from the window's first position to the last token
-  int lo_t = 0, sink_t = 0, nstep = 0;
-  if (!bad_row) {
-    if (a.window > 0) {
-      lo_t = max(0, pa - a.window + 1) / kStep;
-      sink_t = min((min(a.sinks, pb + 1) + kStep - 1) / kStep, lo_t);
-    }
-    nstep = sink_t + pb / kStep - lo_t + 1;
-  }
-  const int per = (nstep + a.nsplit - 1) / a.nsplit, v0 = min(nstep, sp * per), v1 = min(nstep, v0 + per);
-  auto step_pos = [&](int v) { return kStep * (v < sink_t ? v : lo_t + v - sink_t); };
-
-  // this lane's query (columns past the tile repeat its last one and are not stored)
-  const int r = min(32 * w + n, rows - 1);
-  const int tok = r / nh, jj = r - tok * nh;
-  const int pq = pa + tok;
-  const int plow = a.window > 0 ? pq - a.window : -1;   // positions up to here are hidden unless a sink
-  // the first and last position of the wave's queries
-  const int wlo = pa + min(32 * w, rows - 1) / nh, whi = pa + min(32 * w + 31, rows - 1) / nh;
-  const bool idle = 32 * w >= rows;                     // a wave without queries only moves codes and gauges
-  const size_t qoff = size_t(lv) * a.q.sl + size_t(h * a.grp + j0 + jj) * a.q.sh + size_t(qt.tok0 + qt.i0 + tok) * a.q.st;
-
-  // ---- loads of a step: page, then this thread's runs
-  constexpr bool AHEAD = WIDE && IT * D <= 512;  // a step's codes wait in registers while the step before is computed
-  Raw32 raw[AHEAD ? IT : 1];
-  size_t srow = 0;       // cache row of the step's first position
-  bool have = false;     // the step's page is inside the pool
-  const bool pass = !WIDE && c.backend == CG_BACKEND_PASSTHROUGH;
-  const int words = d * c.bits / 32;
-  auto item = [&](int i, bool& val, int& pos, int& run) {
-    const int x = i * NT + tid;
-    val = x >= ITEMS / 2;
-    const int y = val ? x - ITEMS / 2 : x;
-    pos = y / RUNS;
-    run = y % RUNS;
-  };
-  auto load_run = [&](Raw32& o, int i) {
-    bool val;
-    int pos, run;
-    item(i, val, pos, run);
-    if (32 * run >= d) {  // channels past the row: zeros
-#pragma unroll
-      for (int e = 0; e < 8; ++e) o.w[e] = 0u;
-      o.side = 0u;
-      return;
-    }
-    const CacheDev& k = val ? a.vc : a.kc;
-    const uint32_t* src = reinterpret_cast<const uint32_t*>(k.codes) + (srow + pos) * words + run * c.bits;
-    auto words_at = [&](auto width, int i0) {  // `width` words from word i0 on, in one load
-      constexpr int W = decltype(width)::value;
-      typedef uint32_t vec_t __attribute__((ext_vector_type(W), aligned(W == 3 ? 4 : 4 * W)));
-      const vec_t u = *reinterpret_cast<const vec_t*>(src + i0);
-#pragma unroll
-      for (int e = 0; e < W; ++e) o.w[i0 + e] = u[e];
-    };
-    switch (c.bits) {  // rows of whole runs: every run starts on a multiple of its load's width
-      case 4: words_at(std::integral_constant<int, 4>(), 0); break;
-      case 8:
-        words_at(std::integral_constant<int, 4>(), 0);
-        words_at(std::integral_constant<int, 4>(), 4);
-        break;
-      case 2: words_at(std::integral_constant<int, 2>(), 0); break;
-      case 3: words_at(std::integral_constant<int, 3>(), 0); break;
-      default:
-        words_at(std::integral_constant<int, 2>(), 0);
-        words_at(std::integral_constant<int, 2>(), 2);
-        words_at(std::integral_constant<int, 2>(), 4);
-    }
-    o.side = k.side[(srow + pos) * (d / c.n) + 32 * run / c.n];
-  };
-  const int* table = a.pt.pages + size_t(qt.b) * a.pt.max_pages;
-  auto page_of = [&](int v) { return v < v1 ? table[step_pos(v) / a.pt.page_size] : -1; };
-  int page = page_of(v0);  // of the step fetched next, looked up a step ahead
-  auto fetch = [&](int v) {
-    const int t0 = step_pos(v), lp = t0 / a.pt.page_size;
-    const int pg = __builtin_amdgcn_readfirstlane(page);
-    page = page_of(v + 1);
-    have = pg >= 0 && pg < a.kc.B;
-    if (!have) {
-      if (tid == 0 && a.err) atomicOr(a.err, CG_FLAG_POS_RANGE);
-      return;
-    }
-    srow = ((size_t(l) * a.kc.B + pg) * H + h) * a.kc.T_cap + (t0 - lp * a.pt.page_size);
-    if constexpr (AHEAD) {
-#pragma unroll
-      for (int i = 0; i < IT; ++i) load_run(raw[i], i);
-    }
-  };
-  // codes -> binary16 rows in LDS; positions from `held` on become zeros (their bytes may hold anything)
-  auto fill = [&](int v, uint8_t* buf) {
-    const int t0 = step_pos(v);
-    uint32_t st = 0;
-    auto one = [&](int i, Raw32& rw) {
-      bool val;
-      int pos, run;
-      item(i, val, pos, run);
-      const bool live = t0 + pos < held;
-      uint8_t* dst = buf + (val ? kStep * SH::KP + pos * SH::VP : pos * SH::KP) + 64 * run;
-      // V rows that share their banks (every fourth) keep the granules of a run in another order
-      const int turn = val ? pos & 3 : 0;
-      auto put = [&](int plane, int kk, int half, const u32x4_t& o) {
-        *reinterpret_cast<u32x4_t*>(dst + plane * SH::plane + 16 * ((2 * kk + half) ^ turn)) = o;
-      };
-      // the pair (codes p) of a granule with its two blocks' side words
-      auto pair = [&](uint32_t p, f16x2_t sc, f16x2_t mn, uint32_t& hi, uint32_t& lo) {
-        const f16x2_t q = int_pair(p);
-        if constexpr (PL == 1) {
-          hi = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(q, sc, mn));
-        } else {
-          const float z0 = fmaf((float)q[0], (float)sc[0], (float)mn[0]), z1 = fmaf((float)q[1], (float)sc[1], (float)mn[1]);
-          hi = pk_h(z0, z1);
-          lo = pk_h(z0 - h_lo(hi), z1 - h_hi(hi));
-        }
-      };
-      if constexpr (WIDE) {
-        const uint32_t s = live ? rw.side : 0u;
-        const float mnf = f16_bits_to_f32(s & 0xffffu), top = fmaf(float((1 << c.bits) - 1), f16_bits_to_f32(s >> 16), mnf);
-        if (!(fabsf(top) <= 65504.0f && fabsf(mnf) <= 65504.0f)) st |= kOver;
-        const _Float16 m1 = __builtin_bit_cast(_Float16, uint16_t(s)), s1 = __builtin_bit_cast(_Float16, uint16_t(s >> 16));
-        const f16x2_t mn = {m1, m1}, sc = {s1, s1};
-        auto all = [&](auto bits) {
-          uint32_t one = 0x64006400u, m = ((1u << decltype(bits)::value) - 1u) * 0x00010001u;
-          asm volatile("" : "+v"(one), "+v"(m));
-#pragma unroll
-          for (int kk = 0; kk < 2; ++kk)
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              u32x4_t hi, lo;
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                uint32_t x, y = 0;
-                pair(code_pair(rw.w, decltype(bits)::value, kk, half, j, one, m), sc, mn, x, y);
-                hi[j] = x;
-                lo[j] = y;
-              }
-              put(0, kk, half, hi);
-              if constexpr (PL == 2) put(1, kk, half, lo);
-            }
-        };
-        switch (c.bits) {
-          case 4: all(std::integral_constant<int, 4>()); break;
-          case 8: all(std::integral_constant<int, 8>()); break;
-          case 2: all(std::integral_constant<int, 2>()); break;
-          case 3: all(std::integral_constant<int, 3>()); break;
-          default: all(std::integral_constant<int, 6>()); break;
-        }
-      } else {
-        // any block width, row width, or the error-free backend: four channels at a time in binary32
-#pragma unroll 1
-        for (int g4 = 0; g4 < 4; ++g4) {
-          float z[2][4];
-#pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            const int ch = 32 * run + 16 * (g4 >> 1) + 8 * q + 4 * (g4 & 1);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) z[q][e] = 0.0f;
-            if (live && ch < d) load4(val ? a.vc : a.kc, c, srow + pos, d, ch, z[q]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float m = fabsf(z[q][e]);
-              if (!(m <= 65504.0f)) st |= kOver;
-              if (m != 0.0f) st |= val ? kAnyV : kAnyK;
-              if (m >= 0.015625f) st |= val ? kBigV : kBigK;
-            }
-          }
-          u32x4_t hi, lo;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            hi[j] = pk_h(z[0][j], z[1][j]);
-            lo[j] = pk_h(z[0][j] - h_lo(hi[j]), z[1][j] - h_hi(hi[j]));
-          }
-          put(0, g4 >> 1, g4 & 1, hi);
-          if constexpr (PL == 2) put(1, g4 >> 1, g4 & 1, lo);
-        }
-      }
-    };
-    if constexpr (AHEAD) {
-#pragma unroll
-      for (int i = 0; i < IT; ++i) one(i, raw[i]);
-    } else {
-#pragma unroll 1
-      for (int i = 0; i < IT; ++i) {
-        if constexpr (WIDE) load_run(raw[0], i);
-        one(i, raw[0]);
-      }
-    }
-    // the wave's flags (a bit is set when any lane has it)
-    uint32_t all = 0;
-#pragma unroll
-    for (int k = 0; k < (WIDE ? 1 : 5); ++k)
-      if (__builtin_amdgcn_ballot_w64((st >> k) & 1u)) all |= 1u << k;
-    if (lane == 0) state[v & 1][w] = all;
-  };
-
-  if (v0 < v1) fetch(v0);
-
-  // ---- the queries: q' = G_K q for this lane's column, binary16 B operands
-  f16x8_t Q[PL][KK];
-  float cs = 0.0f;  // score = S cs, in powers of two
-  {
-    f32x16_t z[CT];
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) z[ct] = f32x16_t{};
-    const size_t gb = ((size_t(l) * 2 + 0) * G.H + h) * G.R * size_t(G.g) * G.g;
-    constexpr int GP = PL == 1 ? 2 : 3, KC = D == 256 && PL == 1 ? 2 : 4, GPITCH = 32 * KC + 16;
-    static_assert(GP * D * GPITCH <= SH::bytes, "space of the gauge");
-    for (int k0 = 0; 16 * k0 < d; k0 += KC) {
-      if (k0) __syncthreads();
-      stage_gauge<GP, D, KC, NT>(sm, G.hi, gb, G.g, d, 0, k0);
-      __syncthreads();
-#pragma unroll 1
-      for (int kk = k0; kk < k0 + KC && 16 * kk < d; ++kk) {
-        const int ch = 16 * kk + 8 * hc;
-        u32x4_t x[3];
-#pragma unroll
-        for (int p = 0; p < 3; ++p) x[p] = u32x4_t{0u, 0u, 0u, 0u};
-        int np = 1;
-        if (a.q.bf16) {
-          if (ch < d) x[0] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(a.q.ptr) + qoff + ch);
-        } else {
-          np = 3;
-          if (ch < d) {
-            const float* src = static_cast<const float*>(a.q.ptr) + qoff + ch;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              float v[2] = {src[2 * e], src[2 * e + 1]};
-#pragma unroll
-              for (int p = 0; p < 3; ++p) {
-                const uint32_t b0 = f32_to_bf16_rne(v[0]), b1 = f32_to_bf16_rne(v[1]);
-                x[p][e] = b0 | (b1 << 16);
-                // the rest of an infinity is nothing
-                v[0] = fabsf(v[0]) < INFINITY ? v[0] - bf16_to_f32(b0) : 0.0f;
-                v[1] = fabsf(v[1]) < INFINITY ? v[1] - bf16_to_f32(b1) : 0.0f;
-              }
-            }
-          }
-        }
-        const uint8_t* src = sm + n * GPITCH + 32 * (kk - k0) + 16 * hc;
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-          // rows of this channel tile that no group of the K-step's channels reaches add nothing
-          if (32 * ct / G.g > (16 * kk + 15) / G.g || (32 * ct + 31) / G.g < 16 * kk / G.g) continue;
-          bf16x8_t A[GP];
-#pragma unroll
-          for (int p = 0; p < GP; ++p) A[p] = as_bf16x8(*reinterpret_cast<const u32x4_t*>(src + (p * D + 32 * ct) * GPITCH));
-#pragma unroll
-          for (int s = 0; s < 3; ++s)
-            if (s < np)
-#pragma unroll
-              for (int p = 0; p < GP; ++p)
-                if (p + s < 3) z[ct] = mfma(A[p], as_bf16x8(x[s]), z[ct]);
-        }
-      }
-    }
-    __syncthreads();  // the gauge is read
-    float mx = 0.0f;
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, fabsf(z[ct][e]));
-    mx = halves_max(mx);
-    const int ex = mx > 0.0f && mx < INFINITY ? __builtin_amdgcn_frexp_expf(mx) : 0;
-    const float sign = a.scale < 0.0f ? -1.0f : (a.scale > 0.0f ? 1.0f : 0.0f);
-    cs = a.scale == 0.0f ? 1.0f : __builtin_amdgcn_ldexpf(fabsf(a.scale) * kLog2e, ex);
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      u32x4_t hi, lo;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const float x0 = sign * __builtin_amdgcn_ldexpf(z[kk >> 1][8 * (kk & 1) + j], -ex);
-        const float x1 = sign * __builtin_amdgcn_ldexpf(z[kk >> 1][8 * (kk & 1) + 4 + j], -ex);
-        hi[j] = pk_h(x0, x1);
-        lo[j] = pk_h(x0 - h_lo(hi[j]), x1 - h_hi(hi[j]));
-      }
-      Q[0][kk] = as_f16x8(hi);
-      if constexpr (PL == 2) Q[PL - 1][kk] = as_f16x8(lo);
-    }
-  }
-
-  f32x16_t O[CT];
-#pragma unroll
-  for (int ct = 0; ct < CT; ++ct) O[ct] = f32x16_t{};
-  float m = -INFINITY, lsum = 0.0f;  // running maximum (in S) and this lane half's sum
-
-  // ---- steps
-  // (the loop over ordinary steps ends at an odd one and is entered again after it: with both in one body the
-  // sums were moved between registers in every step)
-  int v = v0;
-  while (v < v1) {
-  bool odd = false;
-  size_t crow = 0;
-  for (; v < v1; ++v) {
-    const int t0 = step_pos(v);
-    uint8_t* buf = sm + (SH::buffers == 2 ? (v & 1) * SH::plane * PL : 0);
-    const bool ok = have;
-    crow = srow;
-    if (SH::buffers == 1 && v > v0) __syncthreads();  // the step before is read
-    if (ok) fill(v, buf);
-    if (v + 1 < v1) fetch(v + 1);
-    __syncthreads();
-    if (!ok) continue;
-    uint32_t st = 0;
-#pragma unroll
-    for (int i = 0; i < NW; ++i) st |= state[v & 1][i];
-    st = __builtin_amdgcn_readfirstlane(st);
-    // nothing of the step is visible to this wave's queries
-    const bool hidden = idle || t0 > whi || (a.window > 0 && t0 + kStep - 1 <= wlo - a.window && t0 >= a.sinks);
-    odd = (st & kOver) || (pass && (((st & kAnyK) && !(st & kBigK)) || ((st & kAnyV) && !(st & kBigV))));
-    if (odd) break;
-    if (hidden) continue;
-    // scores
-    f32x16_t S[2];
-    S[0] = f32x16_t{};
-    S[1] = f32x16_t{};
-    // operands two K-steps ahead of the products
-    const uint8_t* kb = buf + n * SH::KP + 16 * hc;
-    f16x8_t kf[2][2][2][PL];  // buffer, K-step, positions, plane
-    auto kload = [&](int s, int k2) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int ps = 0; ps < 2; ++ps)
-#pragma unroll
-          for (int p = 0; p < PL; ++p)
-            kf[s][i][ps][p] = as_f16x8(*reinterpret_cast<const u32x4_t*>(kb + 32 * ps * SH::KP + 32 * (2 * k2 + i) + p * SH::plane));
-    };
-    kload(0, 0);
-#pragma unroll
-    for (int k2 = 0; k2 < KK / 2; ++k2) {
-      if (k2 + 1 < KK / 2) kload((k2 + 1) & 1, k2 + 1);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int ps = 0; ps < 2; ++ps) {
-          const int kk = 2 * k2 + i;
-          S[ps] = mfma_h(kf[k2 & 1][i][ps][0], Q[0][kk], S[ps]);
-          if constexpr (PL == 2) {
-            S[ps] = mfma_h(kf[k2 & 1][i][ps][0], Q[PL - 1][kk], S[ps]);
-            S[ps] = mfma_h(kf[k2 & 1][i][ps][PL - 1], Q[0][kk], S[ps]);
-          }
-        }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    // hidden positions: after the lane's token, or before its window and no sink
-    const bool whole = t0 + kStep - 1 <= wlo && (a.window == 0 || t0 > whi - a.window || t0 + kStep <= a.sinks);
-    if (!whole) {
-#pragma unroll
-      for (int ps = 0; ps < 2; ++ps)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int t = t0 + 32 * ps + 8 * (e >> 2) + 4 * hc + (e & 3);
-          const bool seen = t <= pq && (t > plow || t < a.sinks);
-          S[ps][e] = seen ? S[ps][e] : -INFINITY;
-        }
-    }
-    float mx = S[0][0];
-#pragma unroll
-    for (int ps = 0; ps < 2; ++ps)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, S[ps][e]);
-    mx = halves_max(mx);
-    // the maximum moves only when a score passes it by 2^kLag: the sums are seldom rescaled
-    const bool lift = mx > m && (m == -INFINITY || (mx - m) * cs > kLag);
-    if (__builtin_amdgcn_ballot_w64(lift)) {
-      const float mn = fmaxf(m, mx);
-      const float al = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * cs);
-      m = mn;
-      lsum *= al;
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) O[ct][e] *= al;
-    }
-    const float off = kPBias - (m == -INFINITY ? 0.0f : m * cs);
-    float ls[2] = {0.0f, 0.0f};
-    // values: element e of the lane's operand is position 16 kp + 8 (e / 4) + 4 hc + e % 4
-    const uint8_t* vb = buf + kStep * SH::KP + (4 * hc + ((lane >> 2) & 3)) * SH::VP +
-                        16 * ((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ ((lane >> 2) & 3)) + 8 * (lane & 1);
-    auto vfrag = [&](int plane, int ct, int kp) {
-      typedef __attribute__((address_space(3))) s16x4_t* lds4;
-      const uint8_t* src = vb + plane * SH::plane + 16 * kp * SH::VP + 64 * ct;
-      const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(src));
-      const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(src + 8 * SH::VP));
-      return __builtin_bit_cast(f16x8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-    };
-    // probabilities of K-step kp, operands in P
-    f16x8_t P[2][PL];
-    auto weights = [&](int s, int kp) {
-      u32x4_t hi, lo;
-#pragma unroll
-      for (int e2 = 0; e2 < 4; ++e2) {
-        const int e = 8 * (kp & 1) + 2 * e2;
-        const float p0 = __builtin_amdgcn_exp2f(fmaf(S[kp >> 1][e], cs, off));
-        const float p1 = __builtin_amdgcn_exp2f(fmaf(S[kp >> 1][e + 1], cs, off));
-        const uint32_t both = pk_h(p0, p1);
-        hi[e2] = both;
-        if constexpr (PL == 2) {
-          ls[0] += p0;
-          ls[1] += p1;
-          lo[e2] = pk_h(p0 - h_lo(both), p1 - h_hi(both));
-        } else {
-          // the rounded weights, as the values meet them (v_dot2_f32_f16 adds both to binary32 exactly)
-          const f16x2_t ones = {(_Float16)1.0f, (_Float16)1.0f};
-          ls[e2 & 1] = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2_t, both), ones, ls[e2 & 1], false);
-        }
-      }
-      P[s][0] = as_f16x8(hi);
-      if constexpr (PL == 2) P[s][PL - 1] = as_f16x8(lo);
-    };
-    // the products of K-step kp run while the probabilities of the next are computed
-    constexpr int CB = CT < 4 ? CT : 4;  // channel tiles whose operands are loaded together
-    f16x8_t vf[2][CB][PL];
-    auto vload = [&](int s, int x) {  // batch x: K-step x / (CT / CB), channel tiles CB (x % (CT / CB)) ..
-#pragma unroll
-      for (int i = 0; i < CB; ++i)
-#pragma unroll
-        for (int p = 0; p < PL; ++p) vf[s][i][p] = vfrag(p, CB * (x % (CT / CB)) + i, x / (CT / CB));
-    };
-    constexpr int NB = 4 * (CT / CB);
-    vload(0, 0);
-    weights(0, 0);
-#pragma unroll
-    for (int x = 0; x < NB; ++x) {
-      const int kp = x / (CT / CB), c0 = CB * (x % (CT / CB));
-      if (x + 1 < NB) vload((x + 1) & 1, x + 1);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int i = 0; i < CB; ++i) {
-        O[c0 + i] = mfma_h(vf[x & 1][i][0], P[kp & 1][0], O[c0 + i]);
-        if constexpr (PL == 2) {
-          O[c0 + i] = mfma_h(vf[x & 1][i][0], P[kp & 1][PL - 1], O[c0 + i]);
-          O[c0 + i] = mfma_h(vf[x & 1][i][PL - 1], P[kp & 1][0], O[c0 + i]);
-        }
-      }
-      if (c0 == 0 && kp + 1 < 4) weights((kp + 1) & 1, kp + 1);
-      if (x + 1 < NB) {
-#pragma unroll
-        for (int i = 0; i < CB * (PL == 2 ? 3 : 1); ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x402, 9, 0);
-        }
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    lsum += ls[0] + ls[1];
-  }
-  if (!odd) break;
-  {
-      const int t0 = step_pos(v);
-      const bool hidden = idle || t0 > whi || (a.window > 0 && t0 + kStep - 1 <= wlo - a.window && t0 >= a.sinks);
-      uint8_t* buf = sm + (SH::buffers == 2 ? (v & 1) * SH::plane * PL : 0);
-      // the step position by position in binary32, 16 positions of K and V at a time through its buffer (in
-      // the lanes' order: the values of (kk, hc) at 16 kk + 8 hc, for V of (ct, i, hc) at 32 ct + 8 i + 4 hc)
-      constexpr int SUB = 16;
-      static_assert(2 * SUB * D * 4 <= SH::plane * PL, "space of the rows");
-      float* rows32 = reinterpret_cast<float*>(buf);
-      const int live = min(kStep, held - t0);
-#pragma unroll 1
-      for (int s0 = 0; s0 < live; s0 += SUB) {
-        __syncthreads();
-#pragma unroll 1
-        for (int x = tid; x < 2 * SUB * (D / 4); x += NT) {
-          const bool val = x >= SUB * (D / 4);
-          const int y = val ? x - SUB * (D / 4) : x, pos = y / (D / 4), ch = 4 * (y - pos * (D / 4));
-          float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-          if (s0 + pos < live && ch < d) load4(val ? a.vc : a.kc, c, crow + s0 + pos, d, ch, z);
-          float* dst = rows32 + (val ? SUB * D : 0) + pos * D + (ch & ~15);
-          const int half = (ch >> 3) & 1, h4 = (ch >> 2) & 1;  // channels 16 kk + 8 half + 4 h4 ..
-#pragma unroll
-          for (int j = 0; j < 4; ++j) dst[8 * h4 + 2 * j + half] = z[j];
-        }
-        __syncthreads();
-        if (hidden) continue;
-#pragma unroll 1
-        for (int u = 0; u < min(SUB, live - s0); ++u) {
-          const int t = t0 + s0 + u;
-          const bool seen = t <= pq && (t > plow || t < a.sinks);
-          const float* kr = rows32 + u * D + 8 * hc;
-          const float* vr = rows32 + SUB * D + u * D + 4 * hc;
-          float s = 0.0f;
-#pragma unroll
-          for (int kk = 0; kk < KK; ++kk) {
-            // (opaque: the queries in binary32 would otherwise be kept for this rare path, in registers
-            // that the others need)
-            u32x4_t qa = __builtin_bit_cast(u32x4_t, Q[0][kk]), qb = __builtin_bit_cast(u32x4_t, Q[PL - 1][kk]);
-            asm volatile("" : "+v"(qa), "+v"(qb));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              float q = (e & 1) ? h_hi(qa[e >> 1]) : h_lo(qa[e >> 1]);
-              if constexpr (PL == 2) q += (e & 1) ? h_hi(qb[e >> 1]) : h_lo(qb[e >> 1]);
-              s = fmaf(q, kr[16 * kk + e], s);
-            }
-          }
-          s = halves_sum(s);
-          const float mn = seen ? fmaxf(m, s) : m;
-          const float al = m == mn ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * cs);
-          const float p = seen ? __builtin_amdgcn_exp2f(fmaf(s, cs, kPBias - (mn == -INFINITY ? 0.0f : mn * cs))) : 0.0f;
-          m = mn;
-          lsum = fmaf(lsum, al, hc ? 0.0f : p);
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float o = O[ct][e] * al;
-              O[ct][e] = seen ? fmaf(p, vr[32 * ct + 8 * (e >> 2) + (e & 3)], o) : o;
-            }
-        }
-      }
-  }
-  ++v;
-  }
-  // ---- o = G_V^T (sums / normaliser): the sums are the B operand as they lie
-  const float lall = halves_sum(lsum), inv = lall == 0.0f ? 0.0f : 1.0f / lall;  // nothing visible: zeros
-  constexpr int OP = PL == 1 ? 2 : 3, OPITCH = 2 * D + 16;
-  static_assert(OP * 32 * OPITCH <= SH::bytes, "space of the gauge");
-  const size_t gb = ((size_t(l) * 2 + 1) * G.H + h) * G.R * size_t(G.g) * G.g;
-  const bool mine = 32 * w + n < rows;
-  const size_t orow = (size_t(lv) * a.nsplit + sp) * a.N + (qt.tok0 + qt.i0 + tok);
-  const size_t phead = orow * a.Hq + h * a.grp + j0 + jj;  // this lane's partial row
-  const size_t ooff = size_t(lv) * a.o.sl + size_t(h * a.grp + j0 + jj) * a.o.sh + size_t(qt.tok0 + qt.i0 + tok) * a.o.st;
-  if (a.nsplit > 1 && mine && hc == 0) {
-    a.ml[2 * phead] = m == -INFINITY ? -INFINITY : m * cs;
-    a.ml[2 * phead + 1] = lall;
-  }
-  bf16x8_t x[OP][KK];
-#pragma unroll
-  for (int kk = 0; kk < KK; ++kk) {
-    u32x4_t t[OP];
-#pragma unroll
-    for (int e2 = 0; e2 < 4; ++e2) {
-      float x0 = O[kk >> 1][8 * (kk & 1) + 2 * e2] * inv, x1 = O[kk >> 1][8 * (kk & 1) + 2 * e2 + 1] * inv;
-#pragma unroll
-      for (int p = 0; p < OP; ++p) {
-        const uint32_t b0 = f32_to_bf16_rne(x0), b1 = f32_to_bf16_rne(x1);
-        t[p][e2] = b0 | (b1 << 16);
-        x0 = fabsf(x0) < INFINITY ? x0 - bf16_to_f32(b0) : 0.0f;
-        x1 = fabsf(x1) < INFINITY ? x1 - bf16_to_f32(b1) : 0.0f;
-      }
-    }
-#pragma unroll
-    for (int p = 0; p < OP; ++p) x[p][kk] = as_bf16x8(t[p]);
-  }
-#pragma unroll 1
-  for (int ct = 0; 32 * ct < d; ++ct) {  // output channels 32 ct ..
-    __syncthreads();
-    stage_gauge<OP, 32, KK, NT>(sm, G.tr, gb, G.g, d, 32 * ct, 0);
-    __syncthreads();
-    if (idle) continue;
-    f32x16_t y = f32x16_t{};
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      if (16 * kk >= d || 32 * ct / G.g > (16 * kk + 15) / G.g || (32 * ct + 31) / G.g < 16 * kk / G.g) continue;
-#pragma unroll
-      for (int p = 0; p < OP; ++p) {
-        // element e of the sums' operand is channel 16 kk + 8 (e & 1) + 4 (e >> 2) + 2 hc + ((e & 3) >> 1)
-        const uint32_t* src = reinterpret_cast<const uint32_t*>(sm + (32 * p + n) * OPITCH + 32 * kk) + hc;
-        const uint32_t c0 = src[0], c4 = src[2], c8 = src[4], c12 = src[6];
-        const bf16x8_t A = as_bf16x8(u32x4_t{__builtin_amdgcn_perm(c8, c0, 0x05040100u), __builtin_amdgcn_perm(c8, c0, 0x07060302u),
-                                             __builtin_amdgcn_perm(c12, c4, 0x05040100u), __builtin_amdgcn_perm(c12, c4, 0x07060302u)});
-#pragma unroll
-        for (int s = 0; s < OP; ++s)
-          if (p + s < OP) y = mfma(A, x[s][kk], y);
-      }
-    }
-    // lane (n, hc): channels 32 ct + 8 i + 4 hc + j of its query
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int ch = 32 * ct + 8 * i + 4 * hc;
-      if (!mine || ch >= d) continue;
-      const float4 o = make_float4(y[4 * i], y[4 * i + 1], y[4 * i + 2], y[4 * i + 3]);
-      if (a.nsplit > 1) {
-        *reinterpret_cast<float4*>(a.part + phead * d + ch) = o;
-      } else if (a.o.bf16) {
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.o.ptr) + ooff + ch) =
-            make_uint2(f32_to_bf16_rne(o.x) | (f32_to_bf16_rne(o.y) << 16), f32_to_bf16_rne(o.z) | (f32_to_bf16_rne(o.w) << 16));
-      } else {
-        *reinterpret_cast<float4*>(static_cast<float*>(a.o.ptr) + ooff + ch) = o;
-      }
-    }
-  }
-}
 
 // Splits of a tile's steps joined: out = sum_s w_s o_s / sum_s w_s, w_s = l_s 2^(m_s - max m).  One wave per
 // (token, query head); a split that saw nothing has l = 0 and its sums are zeros.
@@ -909,35 +52,6 @@ __global__ __launch_bounds__(256) void chunk_join(ChunkDev a) {
   }
 }
 
-template <int D, int PL, int NW>
-hipError_t run_chunk(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st) {
-  const bool wide = chunk_wide(c, a.q.d);
-  const void* fn = wide ? reinterpret_cast<const void*>(chunk_attend<D, PL, NW, true>)
-                        : reinterpret_cast<const void*>(chunk_attend<D, PL, NW, false>);
-  const int smem = ChunkShape<D, PL>::bytes;
-  if (smem > 65536) {
-    const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e != hipSuccess) return e;
-  }
-  ChunkDev av = a;
-  GaugeDev gv = G;
-  CodecDev cv = c;
-  void* args[] = {&av, &gv, &cv};
-  return hipLaunchKernel(fn, dim3(blocks), dim3(64 * NW), args, smem, st);
-}
-
-template <int D, int PL>
-hipError_t by_waves(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st) {
-  switch (a.waves) {
-    case 1: return run_chunk<D, PL, 1>(a, G, c, blocks, st);
-    case 2: return run_chunk<D, PL, 2>(a, G, c, blocks, st);
-    case 4: return run_chunk<D, PL, 4>(a, G, c, blocks, st);
-    default:
-      if constexpr (D == 128 && PL == 1) return run_chunk<D, PL, 8>(a, G, c, blocks, st);
-      return hipErrorInvalidValue;
-  }
-}
-
 }  // namespace
 
 ChunkPlan chunk_plan(int nl, int N, int B, int max_q, int H, int Hq, int d, int cap, int window, int sinks) {
@@ -946,7 +60,6 @@ ChunkPlan chunk_plan(int nl, int N, int B, int max_q, int H, int Hq, int d, int 
   const int64_t mq = std::min(max_q, N);
   const int64_t want_rows = mq * grp;
   p.waves = want_rows <= 32 ? 1 : (want_rows <= 64 ? 2 : 4);
-  if (getenv("CGW")) p.waves = atoi(getenv("CGW"));
   const int M = 32 * p.waves;
   p.heads = std::min(grp, M);
   p.nqc = (grp + p.heads - 1) / p.heads;
@@ -971,9 +84,10 @@ hipError_t launch_chunk(const ChunkDev& a, const GaugeDev& G, const CodecDev& c,
   const int d = a.q.d;
   const bool wide = !a.o.bf16;  // binary32 results
   hipError_t e;
-  if (d <= 64) e = wide ? by_waves<64, 2>(a, G, c, int(blocks), st) : by_waves<64, 1>(a, G, c, int(blocks), st);
-  else if (d <= 128) e = wide ? by_waves<128, 2>(a, G, c, int(blocks), st) : by_waves<128, 1>(a, G, c, int(blocks), st);
-  else e = wide ? by_waves<256, 2>(a, G, c, int(blocks), st) : by_waves<256, 1>(a, G, c, int(blocks), st);
+  if (wide) e = run_chunk_f32(a, G, c, int(blocks), st);
+  else if (d <= 64) e = run_chunk_64(a, G, c, int(blocks), st);
+  else if (d <= 128) e = run_chunk_128(a, G, c, int(blocks), st);
+  else e = run_chunk_256(a, G, c, int(blocks), st);
   if (e != hipSuccess || a.nsplit == 1) return e;
   const int per = std::min(16, (a.tq * a.Hq + 3) / 4);
   hipLaunchKernelGGL(chunk_join, dim3(a.ntile * a.q.L, per), dim3(256), 0, st, a);
