@@ -50,6 +50,20 @@ __device__ __forceinline__ f32x16_t mfma_h(const f16x8_t& a, const f16x8_t& b, c
 __device__ __forceinline__ uint32_t pk_h(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), f16x2_t));
 }
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pk_b(float a, float b) {  // bf16 pair, round to nearest even
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
+}
+// planes p = 0 .. NP - 1 of a pair: every one the bf16 of what the ones before leave (of an infinity: nothing)
+template <int NP>
+__device__ __forceinline__ void split_b(float a, float b, uint32_t (&o)[NP]) {
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    o[p] = pk_b(a, b);
+    a = fabsf(a) < INFINITY ? a - __uint_as_float(o[p] << 16) : 0.0f;
+    b = fabsf(b) < INFINITY ? b - __uint_as_float(o[p] & 0xffff0000u) : 0.0f;
+  }
+}
 __device__ __forceinline__ float h_lo(uint32_t w) { return (float)__builtin_bit_cast(f16x2_t, w)[0]; }
 __device__ __forceinline__ float h_hi(uint32_t w) { return (float)__builtin_bit_cast(f16x2_t, w)[1]; }
 __device__ __forceinline__ f16x8_t as_f16x8(const u32x4_t& v) { return __builtin_bit_cast(f16x8_t, v); }
@@ -194,6 +208,7 @@ __device__ __forceinline__ void load4(const CacheDev& k, const CodecDev& c, size
 // compiler took 2088 -> 1850 us (4096 tokens at 20000 positions, 4 bits): the branches over widths, twice a step, and
 // the registers of all of them.
 constexpr int kAnyLayout = -1;
+constexpr int kFillOps = 11;  // vector instructions of the next step's codes beside each product of the scores
 
 template <int D, int PL>
 struct ChunkShape {
@@ -202,6 +217,7 @@ struct ChunkShape {
   static constexpr int plane = kStep * (KP + VP);
   static constexpr int buffers = PL == 1 && D <= 128 ? 2 : 1;
   static constexpr int bytes = plane * PL * buffers;
+  static_assert(VP % 64 == 0 && kStep * KP % 64 == 0, "V runs on multiples of 64 bytes");
 };
 
 template <int D, int PL, int NW, int BITS>
@@ -212,7 +228,7 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
   constexpr int NT = 64 * NW, KK = D / 16, CT = D / 32, RUNS = D / 32;
   constexpr int ITEMS = 2 * kStep * RUNS, IT = (ITEMS + NT - 1) / NT;  // (position, run) of K, then of V
   static_assert(ITEMS % NT == 0, "items per thread");
-  extern __shared__ __attribute__((aligned(16))) uint8_t sm[];
+  extern __shared__ __attribute__((aligned(64))) uint8_t sm[];
   __shared__ uint32_t state[2][NW];  // per step parity and wave: what its items hold (kOver ...)
   constexpr uint32_t kOver = 1, kBigK = 2, kBigV = 4, kAnyK = 8, kAnyV = 16;
 
@@ -266,36 +282,47 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
   const size_t qoff = size_t(lv) * a.q.sl + size_t(h * a.grp + j0 + jj) * a.q.sh + size_t(qt.tok0 + qt.i0 + tok) * a.q.st;
 
   // ---- loads of a step: page, then this thread's runs
-  constexpr bool AHEAD = WIDE && IT * D <= 512;  // a step's codes wait in registers while the step before is computed
-  Raw32 raw[AHEAD ? IT : 1];
+  constexpr bool AHEAD = WIDE && IT * D <= 256;  // a step's codes wait in registers while the step before is computed
+  Raw32 raw[AHEAD ? IT : 1] = {};
   size_t srow = 0;       // cache row of the step's first position
   bool have = false;     // the step's page is inside the pool
   const bool pass = !WIDE && c.backend == CG_BACKEND_PASSTHROUGH;
   const int words = d * bits / 32, nblk = WIDE ? d / c.n : 1;  // words and side words of a row
   auto item = [&](int i, bool& val, int& pos, int& run) {
-    const int x = i * NT + tid;
-    val = x >= ITEMS / 2;
-    const int y = val ? x - ITEMS / 2 : x;
+    const int x0 = i * NT + 64 * w;  // the same side for a whole wave
+    val = x0 >= ITEMS / 2;
+    const int y = (val ? x0 - ITEMS / 2 : x0) + lane;
     pos = y / RUNS;
     run = y % RUNS;
+  };
+  // Buffer loads: the step's rows are the buffer, in scalar registers, and a thread keeps a 32-bit offset (as
+  // 64-bit addresses the offsets took registers enough to spill)
+  auto rows_at = [&](const void* p, int bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, kStep * bytes, 0x00027000);
   };
   auto load_run = [&](Raw32& o, int i) {
     bool val;
     int pos, run;
     item(i, val, pos, run);
-    if (32 * run >= d) {  // channels past the row: zeros
-#pragma unroll
-      for (int e = 0; e < 8; ++e) o.w[e] = 0u;
-      o.side = 0u;
-      return;
-    }
     // a base that the workgroup shares and an offset that the thread keeps
     const CacheDev& k = val ? a.vc : a.kc;
-    const uint32_t* src = reinterpret_cast<const uint32_t*>(k.codes + srow * (4 * words) + uint32_t(4 * (pos * words + run * bits)));
+    const auto rows = rows_at(k.codes + srow * (4 * words), 4 * words);
+    // (channels past the row: offsets past the buffer, which read as zeros)
+    const bool none = 32 * run >= d;
+    const int at = none ? kStep * 4 * words : 4 * (pos * words + run * bits);
     auto words_at = [&](auto width, int i0) {  // `width` words from word i0 on, in one load
       constexpr int W = decltype(width)::value;
-      typedef uint32_t vec_t __attribute__((ext_vector_type(W), aligned(W == 3 ? 4 : 4 * W)));
-      const vec_t u = *reinterpret_cast<const vec_t*>(src + i0);
+      uint32_t u[W];
+      if constexpr (W == 2) {
+        const auto x = __builtin_amdgcn_raw_buffer_load_b64(rows, at + 4 * i0, 0, 0);
+        u[0] = x[0], u[1] = x[1];
+      } else if constexpr (W == 3) {
+        const auto x = __builtin_amdgcn_raw_buffer_load_b96(rows, at + 4 * i0, 0, 0);
+        u[0] = x[0], u[1] = x[1], u[2] = x[2];
+      } else {
+        const auto x = __builtin_amdgcn_raw_buffer_load_b128(rows, at + 4 * i0, 0, 0);
+        u[0] = x[0], u[1] = x[1], u[2] = x[2], u[3] = x[3];
+      }
 #pragma unroll
       for (int e = 0; e < W; ++e) o.w[i0 + e] = u[e];
     };
@@ -312,7 +339,7 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
         words_at(std::integral_constant<int, 2>(), 2);
         words_at(std::integral_constant<int, 2>(), 4);
     }
-    o.side = (k.side + srow * nblk)[uint32_t(pos * nblk + 32 * run / c.n)];
+    o.side = __builtin_amdgcn_raw_buffer_load_b32(rows_at(k.side + srow * nblk, 4 * nblk), none ? kStep * 4 * nblk : 4 * (pos * nblk + 32 * run / c.n), 0, 0);
   };
   // pages are looked up a step ahead of the fetch; the next look: step, page of the row, position in it
   const int* table = a.pt.pages + size_t(qt.b) * a.pt.max_pages;
@@ -356,12 +383,13 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
       bool val;
       int pos, run;
       item(i, val, pos, run);
-      const bool live = t0 + pos < held;
-      uint8_t* dst = buf + (val ? kStep * SH::KP + pos * SH::VP : pos * SH::KP) + 64 * run;
-      // V rows that share their banks (every fourth) keep the granules of a run in another order
-      const int turn = val ? pos & 3 : 0;
+      const bool live = have && t0 + pos < held;  // (nothing of a page outside the pool)
+      // V rows that share their banks (every fourth) keep the granules of a run in another order; their runs
+      // start on multiples of 64 bytes, so granule g of one is at its first one's address ^ 16 g
+      const uint32_t dst = uint32_t(buf - sm) + 64 * run + (val ? kStep * SH::KP + pos * SH::VP + 16 * (pos & 3) : pos * SH::KP);
       auto put = [&](int plane, int kk, int half, const u32x4_t& o) {
-        *reinterpret_cast<u32x4_t*>(dst + plane * SH::plane + 16 * ((2 * kk + half) ^ turn)) = o;
+        const uint32_t g = 16 * (2 * kk + half);
+        *reinterpret_cast<u32x4_t*>(sm + (val ? dst ^ g : dst + g) + plane * SH::plane) = o;
       };
       // the pair (codes p) of a granule with its two blocks' side words
       auto pair = [&](uint32_t p, f16x2_t sc, f16x2_t mn, uint32_t& hi, uint32_t& lo) {
@@ -451,7 +479,7 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
 #pragma unroll
     for (int k = 0; k < (WIDE ? 1 : 5); ++k)
       if (__builtin_amdgcn_ballot_w64((st >> k) & 1u)) all |= 1u << k;
-    if (lane == 0) state[v & 1][w] = all;
+    state[v & 1][w] = all;
   };
 
   if (v0 < v1) fetch();
@@ -485,15 +513,10 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
             const float* src = static_cast<const float*>(a.q.ptr) + qoff + ch;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              float v[2] = {src[2 * e], src[2 * e + 1]};
+              uint32_t o[3];
+              split_b<3>(src[2 * e], src[2 * e + 1], o);
 #pragma unroll
-              for (int p = 0; p < 3; ++p) {
-                const uint32_t b0 = f32_to_bf16_rne(v[0]), b1 = f32_to_bf16_rne(v[1]);
-                x[p][e] = b0 | (b1 << 16);
-                // the rest of an infinity is nothing
-                v[0] = fabsf(v[0]) < INFINITY ? v[0] - bf16_to_f32(b0) : 0.0f;
-                v[1] = fabsf(v[1]) < INFINITY ? v[1] - bf16_to_f32(b1) : 0.0f;
-              }
+              for (int p = 0; p < 3; ++p) x[p][e] = o[p];
             }
           }
         }
@@ -523,7 +546,7 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
     mx = halves_max(mx);
     const int ex = mx > 0.0f && mx < INFINITY ? __builtin_amdgcn_frexp_expf(mx) : 0;
     const float sign = a.scale < 0.0f ? -1.0f : (a.scale > 0.0f ? 1.0f : 0.0f);
-    cs = a.scale == 0.0f ? 1.0f : __builtin_amdgcn_ldexpf(fabsf(a.scale) * kLog2e, ex);
+    cs = a.scale == 0.0f ? 1.0f : fmaxf(__builtin_amdgcn_ldexpf(fabsf(a.scale) * kLog2e, ex), 1e-37f);  // (not 0: 0 times a hidden score)
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
       u32x4_t hi, lo;
@@ -545,74 +568,171 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
   float m = -INFINITY, lsum = 0.0f;  // running maximum (in S) and this lane half's sum
 
   // ---- steps
-  // (the loop over ordinary steps ends at an odd one and is entered again after it: with both in one body the
-  // sums were moved between registers in every step)
+  // FUSED: with two buffers the next step's codes are decoded while this one's scores are on the matrix cores (16
+  // products leave room for about ten vector instructions each), with one barrier a step; else before them.
+  // The body is one path whatever the step: where it is not, the sums are moved between registers in every step (64
+  // moves of a wave's 340 vector instructions).  So an odd step leaves the loop, which is entered again after it, and a step that
+  // a wave sees nothing of runs with every weight 0; a wave without queries has a loop of its own.
+  constexpr bool FUSED = AHEAD && SH::buffers == 2;
+  auto buf_of = [&](int v) { return sm + (SH::buffers == 2 ? (v & 1) * SH::plane * PL : 0); };
   int v = v0;
-  while (v < v1) {
-  bool odd = false;
-  size_t crow = 0;
-  for (; v < v1; ++v) {
-    const int t0 = step_pos(v);
-    uint8_t* buf = sm + (SH::buffers == 2 ? (v & 1) * SH::plane * PL : 0);
-    const bool ok = have;
+  size_t crow = 0;    // cache row of step v's first position
+  bool ok = false;    // its page is inside the pool
+  bool skip = false;  // (FUSED) the odd step v is summed: what is left of it is to decode the next one's codes
+  auto advance = [&]() {  // what was fetched is step v, the one after it is fetched
+    ok = have;
     crow = srow;
-    if (SH::buffers == 1 && v > v0) __syncthreads();  // the step before is read
-    if (ok) fill(v, buf);
+  };
+  if (FUSED && v < v1) {
+    advance();
+    fill(v, buf_of(v));
     if (v + 1 < v1) fetch();
     __syncthreads();
-    if (!ok) continue;
+  }
+  // whether step v, in its buffer, is odd
+  auto odd_step = [&]() {
     uint32_t st = 0;
 #pragma unroll
     for (int i = 0; i < NW; ++i) st |= state[v & 1][i];
     st = __builtin_amdgcn_readfirstlane(st);
-    // nothing of the step is visible to this wave's queries
-    const bool hidden = idle || t0 > whi || (a.window > 0 && t0 + kStep - 1 <= wlo - a.window && t0 >= a.sinks);
-    odd = (st & kOver) || (pass && (((st & kAnyK) && !(st & kBigK)) || ((st & kAnyV) && !(st & kBigV))));
+    return ok && !skip &&
+           ((st & kOver) || (pass && (((st & kAnyK) && !(st & kBigK)) || ((st & kAnyV) && !(st & kBigV)))));
+  };
+  // An odd step: its positions in binary32, 16 of K and V at a time through its buffer (in the lanes' order: the
+  // values of (kk, hc) at 16 kk + 8 hc, for V of (ct, i, hc) at 32 ct + 8 i + 4 hc), each given to `take`
+  auto odd_rows = [&](auto take) {
+    constexpr int SUB = 16;
+    static_assert(2 * SUB * D * 4 <= SH::plane * PL, "space of the rows");
+    float* rows32 = reinterpret_cast<float*>(buf_of(v));
+    const int live = min(kStep, held - step_pos(v));
+#pragma unroll 1
+    for (int s0 = 0; s0 < live; s0 += SUB) {
+      __syncthreads();
+#pragma unroll 1
+      for (int x = tid; x < 2 * SUB * (D / 4); x += NT) {
+        const bool val = x >= SUB * (D / 4);
+        const int y = val ? x - SUB * (D / 4) : x, pos = y / (D / 4), ch = 4 * (y - pos * (D / 4));
+        float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (s0 + pos < live && ch < d) load4(val ? a.vc : a.kc, c, crow + s0 + pos, d, ch, z);
+        float* dst = rows32 + (val ? SUB * D : 0) + pos * D + (ch & ~15);
+        const int half = (ch >> 3) & 1, h4 = (ch >> 2) & 1;  // channels 16 kk + 8 half + 4 h4 ..
+#pragma unroll
+        for (int j = 0; j < 4; ++j) dst[8 * h4 + 2 * j + half] = z[j];
+      }
+      __syncthreads();
+      take(s0, min(SUB, live - s0), rows32 + 8 * hc, rows32 + SUB * D + 4 * hc);
+    }
+    if constexpr (FUSED) {
+      // the step's products are formed once more, with weights 0: of zeros
+      __syncthreads();
+      for (int x = tid; x < SH::plane / 16; x += NT) reinterpret_cast<u32x4_t*>(rows32)[x] = u32x4_t{0u, 0u, 0u, 0u};
+      __syncthreads();
+      skip = true;
+    } else {
+      ++v;
+    }
+  };
+  // the start of a step that is not FUSED
+  auto begin = [&]() {
+    advance();
+    if (SH::buffers == 1 && v > v0) __syncthreads();  // the step before is read
+    fill(v, buf_of(v));
+    if (v + 1 < v1) fetch();
+    __syncthreads();
+  };
+  // the end of the scores of a FUSED one
+  auto turn = [&]() {
+    advance();
+    if (v + 2 < v1) fetch();
+  };
+  if (idle) {
+    while (v < v1) {
+      if constexpr (!FUSED) begin();
+      if (odd_step()) {
+        odd_rows([](int, int, const float*, const float*) {});
+        continue;
+      }
+      skip = false;
+      if constexpr (FUSED) {
+        fill(v + 1, buf_of(v + 1));
+        turn();
+        __syncthreads();
+      }
+      ++v;
+    }
+  }
+  while (v < v1) {
+  bool odd = false;
+  for (; v < v1; ++v) {
+    const int t0 = step_pos(v);
+    const uint8_t* buf = buf_of(v);
+    if constexpr (!FUSED) begin();
+    odd = odd_step();
     if (odd) break;
-    if (hidden) continue;
-    // scores
+    // nothing of the step is visible to this wave's queries, or it holds nothing
+    const bool blank = !ok || skip;
+    skip = false;
+    // scores; operands KB K-steps ahead of the products
     f32x16_t S[2];
     S[0] = f32x16_t{};
     S[1] = f32x16_t{};
-    // operands two K-steps ahead of the products
+    constexpr int KB = FUSED ? 1 : 2;
     const uint8_t* kb = buf + n * SH::KP + 16 * hc;
-    f16x8_t kf[2][2][2][PL];  // buffer, K-step, positions, plane
+    f16x8_t kf[2][KB][2][PL];  // buffer, K-step, positions, plane
     auto kload = [&](int s, int k2) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < KB; ++i)
 #pragma unroll
         for (int ps = 0; ps < 2; ++ps)
 #pragma unroll
           for (int p = 0; p < PL; ++p)
-            kf[s][i][ps][p] = as_f16x8(*reinterpret_cast<const u32x4_t*>(kb + 32 * ps * SH::KP + 32 * (2 * k2 + i) + p * SH::plane));
+            kf[s][i][ps][p] = as_f16x8(*reinterpret_cast<const u32x4_t*>(kb + 32 * ps * SH::KP + 32 * (KB * k2 + i) + p * SH::plane));
     };
+    __builtin_amdgcn_sched_barrier(0);
     kload(0, 0);
 #pragma unroll
-    for (int k2 = 0; k2 < KK / 2; ++k2) {
-      if (k2 + 1 < KK / 2) kload((k2 + 1) & 1, k2 + 1);
-      __builtin_amdgcn_sched_barrier(0);
+    for (int k2 = 0; k2 < KK / KB; ++k2) {
+      if (k2 + 1 < KK / KB) kload((k2 + 1) & 1, k2 + 1);
+      if constexpr (!FUSED) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < KB; ++i)
 #pragma unroll
         for (int ps = 0; ps < 2; ++ps) {
-          const int kk = 2 * k2 + i;
+          const int kk = KB * k2 + i;
           S[ps] = mfma_h(kf[k2 & 1][i][ps][0], Q[0][kk], S[ps]);
           if constexpr (PL == 2) {
             S[ps] = mfma_h(kf[k2 & 1][i][ps][0], Q[PL - 1][kk], S[ps]);
             S[ps] = mfma_h(kf[k2 & 1][i][ps][PL - 1], Q[0][kk], S[ps]);
           }
         }
+      if constexpr (!FUSED) __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (FUSED) {
+      fill(v + 1, buf_of(v + 1));  // (past the last step what it writes is not read)
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+      for (int k2 = 0; k2 < KK; ++k2) {
+        if (k2 + 1 < KK) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x002, kFillOps, 0);
+          if (i & 1) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
+        }
+      }
       __builtin_amdgcn_sched_barrier(0);
+      turn();
     }
     // hidden positions: after the lane's token, or before its window and no sink
-    const bool whole = t0 + kStep - 1 <= wlo && (a.window == 0 || t0 > whi - a.window || t0 + kStep <= a.sinks);
+    const bool whole = !blank && t0 + kStep - 1 <= wlo && (a.window == 0 || t0 > whi - a.window || t0 + kStep <= a.sinks);
     if (!whole) {
+      const int last = blank ? -1 : pq;
 #pragma unroll
       for (int ps = 0; ps < 2; ++ps)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int t = t0 + 32 * ps + 8 * (e >> 2) + 4 * hc + (e & 3);
-          const bool seen = t <= pq && (t > plow || t < a.sinks);
+          const bool seen = t <= last && (t > plow || t < a.sinks);
           S[ps][e] = seen ? S[ps][e] : -INFINITY;
         }
     }
@@ -706,71 +826,48 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
       __builtin_amdgcn_sched_barrier(0);
     }
     lsum += ls[0] + ls[1];
+    if constexpr (FUSED) __syncthreads();
   }
   if (!odd) break;
   {
-      const int t0 = step_pos(v);
-      const bool hidden = idle || t0 > whi || (a.window > 0 && t0 + kStep - 1 <= wlo - a.window && t0 >= a.sinks);
-      uint8_t* buf = sm + (SH::buffers == 2 ? (v & 1) * SH::plane * PL : 0);
-      // the step position by position in binary32, 16 positions of K and V at a time through its buffer (in
-      // the lanes' order: the values of (kk, hc) at 16 kk + 8 hc, for V of (ct, i, hc) at 32 ct + 8 i + 4 hc)
-      constexpr int SUB = 16;
-      static_assert(2 * SUB * D * 4 <= SH::plane * PL, "space of the rows");
-      float* rows32 = reinterpret_cast<float*>(buf);
-      const int live = min(kStep, held - t0);
+    const int t0 = step_pos(v);
+    odd_rows([&](int s0, int count, const float* krows, const float* vrows) {
 #pragma unroll 1
-      for (int s0 = 0; s0 < live; s0 += SUB) {
-        __syncthreads();
-#pragma unroll 1
-        for (int x = tid; x < 2 * SUB * (D / 4); x += NT) {
-          const bool val = x >= SUB * (D / 4);
-          const int y = val ? x - SUB * (D / 4) : x, pos = y / (D / 4), ch = 4 * (y - pos * (D / 4));
-          float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-          if (s0 + pos < live && ch < d) load4(val ? a.vc : a.kc, c, crow + s0 + pos, d, ch, z);
-          float* dst = rows32 + (val ? SUB * D : 0) + pos * D + (ch & ~15);
-          const int half = (ch >> 3) & 1, h4 = (ch >> 2) & 1;  // channels 16 kk + 8 half + 4 h4 ..
+      for (int u = 0; u < count; ++u) {
+        const float* kr = krows + u * D;
+        const float* vr = vrows + u * D;
+        const int t = t0 + s0 + u;
+        const bool seen = t <= pq && (t > plow || t < a.sinks);
+        float s = 0.0f;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) dst[8 * h4 + 2 * j + half] = z[j];
-        }
-        __syncthreads();
-        if (hidden) continue;
-#pragma unroll 1
-        for (int u = 0; u < min(SUB, live - s0); ++u) {
-          const int t = t0 + s0 + u;
-          const bool seen = t <= pq && (t > plow || t < a.sinks);
-          const float* kr = rows32 + u * D + 8 * hc;
-          const float* vr = rows32 + SUB * D + u * D + 4 * hc;
-          float s = 0.0f;
+        for (int kk = 0; kk < KK; ++kk) {
+          // (opaque: the queries in binary32 would otherwise be kept for this rare path, in registers
+          // that the others need)
+          u32x4_t qa = __builtin_bit_cast(u32x4_t, Q[0][kk]), qb = __builtin_bit_cast(u32x4_t, Q[PL - 1][kk]);
+          asm volatile("" : "+v"(qa), "+v"(qb));
 #pragma unroll
-          for (int kk = 0; kk < KK; ++kk) {
-            // (opaque: the queries in binary32 would otherwise be kept for this rare path, in registers
-            // that the others need)
-            u32x4_t qa = __builtin_bit_cast(u32x4_t, Q[0][kk]), qb = __builtin_bit_cast(u32x4_t, Q[PL - 1][kk]);
-            asm volatile("" : "+v"(qa), "+v"(qb));
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              float q = (e & 1) ? h_hi(qa[e >> 1]) : h_lo(qa[e >> 1]);
-              if constexpr (PL == 2) q += (e & 1) ? h_hi(qb[e >> 1]) : h_lo(qb[e >> 1]);
-              s = fmaf(q, kr[16 * kk + e], s);
-            }
+          for (int e = 0; e < 8; ++e) {
+            float q = (e & 1) ? h_hi(qa[e >> 1]) : h_lo(qa[e >> 1]);
+            if constexpr (PL == 2) q += (e & 1) ? h_hi(qb[e >> 1]) : h_lo(qb[e >> 1]);
+            s = fmaf(q, kr[16 * kk + e], s);
           }
-          s = halves_sum(s);
-          const float mn = seen ? fmaxf(m, s) : m;
-          const float al = m == mn ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * cs);
-          const float p = seen ? __builtin_amdgcn_exp2f(fmaf(s, cs, kPBias - (mn == -INFINITY ? 0.0f : mn * cs))) : 0.0f;
-          m = mn;
-          lsum = fmaf(lsum, al, hc ? 0.0f : p);
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const float o = O[ct][e] * al;
-              O[ct][e] = seen ? fmaf(p, vr[32 * ct + 8 * (e >> 2) + (e & 3)], o) : o;
-            }
         }
+        s = halves_sum(s);
+        const float mn = seen ? fmaxf(m, s) : m;
+        const float al = m == mn ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * cs);
+        const float p = seen ? __builtin_amdgcn_exp2f(fmaf(s, cs, kPBias - (mn == -INFINITY ? 0.0f : mn * cs))) : 0.0f;
+        m = mn;
+        lsum = fmaf(lsum, al, hc ? 0.0f : p);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float o = O[ct][e] * al;
+            O[ct][e] = seen ? fmaf(p, vr[32 * ct + 8 * (e >> 2) + (e & 3)], o) : o;
+          }
       }
+    });
   }
-  ++v;
   }
   // ---- o = G_V^T (sums / normaliser): the sums are the B operand as they lie
   const float lall = halves_sum(lsum), inv = lall == 0.0f ? 0.0f : 1.0f / lall;  // nothing visible: zeros
@@ -791,14 +888,10 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
     u32x4_t t[OP];
 #pragma unroll
     for (int e2 = 0; e2 < 4; ++e2) {
-      float x0 = O[kk >> 1][8 * (kk & 1) + 2 * e2] * inv, x1 = O[kk >> 1][8 * (kk & 1) + 2 * e2 + 1] * inv;
+      uint32_t o[OP];
+      split_b<OP>(O[kk >> 1][8 * (kk & 1) + 2 * e2] * inv, O[kk >> 1][8 * (kk & 1) + 2 * e2 + 1] * inv, o);
 #pragma unroll
-      for (int p = 0; p < OP; ++p) {
-        const uint32_t b0 = f32_to_bf16_rne(x0), b1 = f32_to_bf16_rne(x1);
-        t[p][e2] = b0 | (b1 << 16);
-        x0 = fabsf(x0) < INFINITY ? x0 - bf16_to_f32(b0) : 0.0f;
-        x1 = fabsf(x1) < INFINITY ? x1 - bf16_to_f32(b1) : 0.0f;
-      }
+      for (int p = 0; p < OP; ++p) t[p][e2] = o[p];
     }
 #pragma unroll
     for (int p = 0; p < OP; ++p) x[p][kk] = as_bf16x8(t[p]);
@@ -835,7 +928,7 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
         *reinterpret_cast<float4*>(a.part + phead * d + ch) = o;
       } else if (a.o.bf16) {
         *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.o.ptr) + ooff + ch) =
-            make_uint2(f32_to_bf16_rne(o.x) | (f32_to_bf16_rne(o.y) << 16), f32_to_bf16_rne(o.z) | (f32_to_bf16_rne(o.w) << 16));
+            make_uint2(pk_b(o.x, o.y), pk_b(o.z, o.w));
       } else {
         *reinterpret_cast<float4*>(static_cast<float*>(a.o.ptr) + ooff + ch) = o;
       }
