@@ -217,6 +217,7 @@ struct ChunkShape {
   static constexpr int plane = kStep * (KP + VP);
   static constexpr int buffers = PL == 1 && D <= 128 ? 2 : 1;
   static constexpr int bytes = plane * PL * buffers;
+  static constexpr int all = bytes + 64;                         // with the waves' flags
   static_assert(VP % 64 == 0 && kStep * KP % 64 == 0, "V runs on multiples of 64 bytes");
 };
 
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
   constexpr int ITEMS = 2 * kStep * RUNS, IT = (ITEMS + NT - 1) / NT;  // (position, run) of K, then of V
   static_assert(ITEMS % NT == 0, "items per thread");
   extern __shared__ __attribute__((aligned(64))) uint8_t sm[];
-  __shared__ uint32_t state[2][NW];  // per step parity and wave: what its items hold (kOver ...)
+  uint32_t(*state)[NW] = reinterpret_cast<uint32_t(*)[NW]>(sm + SH::bytes);  // per step parity and wave: what its items hold (kOver ...)
   constexpr uint32_t kOver = 1, kBigK = 2, kBigV = 4, kAnyK = 8, kAnyV = 16;
 
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, hc = lane >> 5;
@@ -289,9 +290,10 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
   const bool pass = !WIDE && c.backend == CG_BACKEND_PASSTHROUGH;
   const int words = d * bits / 32, nblk = WIDE ? d / c.n : 1;  // words and side words of a row
   auto item = [&](int i, bool& val, int& pos, int& run) {
-    const int x0 = i * NT + 64 * w;  // the same side for a whole wave
+    // the same side for a whole wave
+    const int x0 = (ITEMS / 2) % NT == 0 ? i * NT : i * NT + 64 * w;
     val = x0 >= ITEMS / 2;
-    const int y = (val ? x0 - ITEMS / 2 : x0) + lane;
+    const int y = ((ITEMS / 2) % NT == 0 ? i * NT + tid : x0 + lane) - (val ? ITEMS / 2 : 0);
     pos = y / RUNS;
     run = y % RUNS;
   };
@@ -376,7 +378,17 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
     }
   };
   // codes -> binary16 rows in LDS; positions from `held` on become zeros (their bytes may hold anything)
-  auto fill = [&](int v, uint8_t* buf) {
+  // decode() gives the granules of item i to out(i, plane, 2 kk + half, granule), store() puts one into a buffer.
+  auto store = [&](uint8_t* buf, int i, int plane, int g, const u32x4_t& o) {
+    bool val;
+    int pos, run;
+    item(i, val, pos, run);
+    // V rows that share their banks (every fourth) keep the granules of a run in another order; their runs
+    // start on multiples of 64 bytes, so granule g of one is at its first one's address ^ 16 g
+    const uint32_t dst = uint32_t(buf - sm) + 64 * run + (val ? kStep * SH::KP + pos * SH::VP + 16 * (pos & 3) : pos * SH::KP);
+    *reinterpret_cast<u32x4_t*>(sm + (val ? dst ^ (16 * g) : dst + 16 * g) + plane * SH::plane) = o;
+  };
+  auto decode = [&](int v, auto out) {
     const int t0 = step_pos(v);
     uint32_t st = 0;
     auto one = [&](int i, Raw32& rw) {
@@ -384,13 +396,7 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
       int pos, run;
       item(i, val, pos, run);
       const bool live = have && t0 + pos < held;  // (nothing of a page outside the pool)
-      // V rows that share their banks (every fourth) keep the granules of a run in another order; their runs
-      // start on multiples of 64 bytes, so granule g of one is at its first one's address ^ 16 g
-      const uint32_t dst = uint32_t(buf - sm) + 64 * run + (val ? kStep * SH::KP + pos * SH::VP + 16 * (pos & 3) : pos * SH::KP);
-      auto put = [&](int plane, int kk, int half, const u32x4_t& o) {
-        const uint32_t g = 16 * (2 * kk + half);
-        *reinterpret_cast<u32x4_t*>(sm + (val ? dst ^ g : dst + g) + plane * SH::plane) = o;
-      };
+      auto put = [&](int plane, int kk, int half, const u32x4_t& o) { out(i, plane, 2 * kk + half, o); };
       // the pair (codes p) of a granule with its two blocks' side words
       auto pair = [&](uint32_t p, f16x2_t sc, f16x2_t mn, uint32_t& hi, uint32_t& lo) {
         const f16x2_t q = int_pair(p);
@@ -410,7 +416,7 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
         const f16x2_t mn = {m1, m1}, sc = {s1, s1};
         auto all = [&](auto width) {
           uint32_t one = 0x64006400u, m = ((1u << decltype(width)::value) - 1u) * 0x00010001u;
-          asm volatile("" : "+v"(one), "+v"(m));
+          asm("" : "+v"(one), "+v"(m));
 #pragma unroll
           for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
@@ -479,7 +485,10 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
 #pragma unroll
     for (int k = 0; k < (WIDE ? 1 : 5); ++k)
       if (__builtin_amdgcn_ballot_w64((st >> k) & 1u)) all |= 1u << k;
-    state[v & 1][w] = all;
+    return all;
+  };
+  auto fill = [&](int v, uint8_t* buf) {
+    state[v & 1][w] = decode(v, [&](int i, int plane, int g, const u32x4_t& o) { store(buf, i, plane, g, o); });
   };
 
   if (v0 < v1) fetch();
@@ -708,7 +717,10 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
       if constexpr (!FUSED) __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (FUSED) {
-      fill(v + 1, buf_of(v + 1));  // (past the last step what it writes is not read)
+      // the next step's codes, between the products; past all of this one's reads they go to the other buffer
+      // (past the last step what is written there is not read)
+      u32x4_t dec[IT][4];
+      const uint32_t flags = decode(v + 1, [&](int i, int, int g, const u32x4_t& o) { dec[i][g] = o; });
       __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
 #pragma unroll
       for (int k2 = 0; k2 < KK; ++k2) {
@@ -717,10 +729,14 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
         for (int i = 0; i < 2; ++i) {
           __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
           __builtin_amdgcn_sched_group_barrier(0x002, kFillOps, 0);
-          if (i & 1) __builtin_amdgcn_sched_group_barrier(0x200, 1, 0);
         }
       }
       __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < IT; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) store(buf_of(v + 1), i, 0, g, dec[i][g]);
+      state[(v + 1) & 1][w] = flags;
       turn();
     }
     // hidden positions: after the lane's token, or before its window and no sink
@@ -939,7 +955,7 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
 template <int D, int PL, int NW, int BITS>
 hipError_t run_chunk(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st) {
   const void* fn = reinterpret_cast<const void*>(chunk_attend<D, PL, NW, BITS>);
-  const int smem = ChunkShape<D, PL>::bytes;
+  const int smem = ChunkShape<D, PL>::all;
   if (smem > 65536) {
     const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
     if (e != hipSuccess) return e;
