@@ -17,7 +17,7 @@ struct ChunkDev {
   float scale;
   int window, sinks;
   int cap;               // positions a row can hold
-  int waves, tq, heads, nqc, ntile, nsplit;  // the plan
+  int tq, heads, nqc, ntile, nsplit;  // the plan
   float *part, *ml;      // splits: [nl][nsplit][N][Hq][d], [nl][nsplit][N][Hq][2] (maximum, sum)
   int* err;
 };
@@ -27,15 +27,17 @@ inline bool chunk_wide(const CodecDev& c, int d) {
   return c.backend == CG_BACKEND_BLOCK_UNIFORM && c.n % 32 == 0 && d % 32 == 0;
 }
 
+constexpr int kChunkWaves = 4;  // waves of 32 query rows per workgroup
+
 struct ChunkPlan {
-  int waves = 1;         // waves of 32 query rows per workgroup
   int tq = 1, heads = 1; // tokens and query heads of a tile
   int nqc = 1;           // chunks of a KV head's query heads
   int ntile = 0;         // tiles at most
   int nsplit = 1;        // parts of a tile's positions
   size_t ws_bytes = 0;
 };
-ChunkPlan chunk_plan(int nl, int N, int B, int max_q, int H, int Hq, int d, int cap, int window, int sinks);
+// singles: rows of one token have another kernel
+ChunkPlan chunk_plan(int nl, int N, int B, int max_q, int H, int Hq, int d, int cap, int window, int sinks, bool singles);
 // The kernels by rounded row width and result type
 hipError_t run_chunk_64(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st);
 hipError_t run_chunk_128(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st);

@@ -4,7 +4,7 @@
 namespace cg {
 
 hipError_t run_chunk_256(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st) {
-  return by_waves<256, 1, false>(a, G, c, blocks, st);
+  return by_layout<256, 1, false>(a, G, c, blocks, st);
 }
 
 }  // namespace cg

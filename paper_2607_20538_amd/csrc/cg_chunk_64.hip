@@ -4,7 +4,7 @@
 namespace cg {
 
 hipError_t run_chunk_64(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st) {
-  return by_waves<64, 1, true>(a, G, c, blocks, st);
+  return by_layout<64, 1, true>(a, G, c, blocks, st);
 }
 
 }  // namespace cg

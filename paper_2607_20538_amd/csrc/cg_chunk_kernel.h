@@ -7,7 +7,7 @@
 // G_K^T zhat^K the scores are q' . zhat^K_t, and o = G_V^T sum_t p_t zhat^V_t, so it is applied once to the
 // queries of a tile and once to their sums, on the bf16 matrix cores (split planes of G).
 //
-// A workgroup takes 32 NW query rows (tokens x query heads of one KV head) of one batch row and walks their
+// A workgroup takes 128 query rows (tokens x query heads of one KV head) of one batch row and walks their
 // visible positions 64 at a time.  The codes of a step become binary16 zhat = fma(q, sc, mn) in LDS once per
 // workgroup; both products run on v_mfma_f32_32x32x16_f16 with the queries as columns:
 //   S^T = K Q'^T   (lane: one query, half of the 64 positions)  -> softmax without crossing lanes but for one
@@ -202,7 +202,10 @@ __device__ __forceinline__ void load4(const CacheDev& k, const CodecDev& c, size
 // ------------------------------------------------------------------------------------------
 // the kernel
 // ------------------------------------------------------------------------------------------
-// D: channels of a row rounded up (zeros past d); PL: binary16 planes of an operand; NW: waves.
+// D: channels of a row rounded up (zeros past d); PL: binary16 planes of an operand.
+// Always four waves, also where the queries fill one: the others decode its codes.  32 rows of one token, 8 KV heads
+// x 4, d = 128, n = 32, up to 8000 positions: 463 us with one wave, 297 with two, 146 with four.
+constexpr int NW = kChunkWaves;
 // BITS: the code width of rows that decode in whole runs (chunk_wide; 0: any width, read at run time), or
 // kAnyLayout: any block and row width and the error-free backend, four channels at a time.  A width known to the
 // compiler took 2088 -> 1850 us (4096 tokens at 20000 positions, 4 bits): the branches over widths, twice a step, and
@@ -221,7 +224,7 @@ struct ChunkShape {
   static_assert(VP % 64 == 0 && kStep * KP % 64 == 0, "V runs on multiples of 64 bytes");
 };
 
-template <int D, int PL, int NW, int BITS>
+template <int D, int PL, int BITS>
 __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_attend(ChunkDev a, GaugeDev G, CodecDev c) {
   using SH = ChunkShape<D, PL>;
   constexpr bool WIDE = BITS != kAnyLayout;
@@ -952,9 +955,9 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
   }
 }
 
-template <int D, int PL, int NW, int BITS>
+template <int D, int PL, int BITS>
 hipError_t run_chunk(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st) {
-  const void* fn = reinterpret_cast<const void*>(chunk_attend<D, PL, NW, BITS>);
+  const void* fn = reinterpret_cast<const void*>(chunk_attend<D, PL, BITS>);
   const int smem = ChunkShape<D, PL>::all;
   if (smem > 65536) {
     const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -968,28 +971,19 @@ hipError_t run_chunk(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, in
 }
 
 // EACH: a kernel for each code width (else one that reads it at run time)
-template <int D, int PL, int NW, bool EACH>
+template <int D, int PL, bool EACH>
 hipError_t by_layout(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st) {
-  if (!chunk_wide(c, a.q.d)) return run_chunk<D, PL, NW, kAnyLayout>(a, G, c, blocks, st);
+  if (!chunk_wide(c, a.q.d)) return run_chunk<D, PL, kAnyLayout>(a, G, c, blocks, st);
   if constexpr (EACH) {
     switch (c.bits) {
-      case 2: return run_chunk<D, PL, NW, 2>(a, G, c, blocks, st);
-      case 3: return run_chunk<D, PL, NW, 3>(a, G, c, blocks, st);
-      case 4: return run_chunk<D, PL, NW, 4>(a, G, c, blocks, st);
-      case 6: return run_chunk<D, PL, NW, 6>(a, G, c, blocks, st);
-      default: return run_chunk<D, PL, NW, 8>(a, G, c, blocks, st);
+      case 2: return run_chunk<D, PL, 2>(a, G, c, blocks, st);
+      case 3: return run_chunk<D, PL, 3>(a, G, c, blocks, st);
+      case 4: return run_chunk<D, PL, 4>(a, G, c, blocks, st);
+      case 6: return run_chunk<D, PL, 6>(a, G, c, blocks, st);
+      default: return run_chunk<D, PL, 8>(a, G, c, blocks, st);
     }
   } else {
-    return run_chunk<D, PL, NW, 0>(a, G, c, blocks, st);
-  }
-}
-
-template <int D, int PL, bool EACH>
-hipError_t by_waves(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st) {
-  switch (a.waves) {
-    case 1: return by_layout<D, PL, 1, EACH>(a, G, c, blocks, st);
-    case 2: return by_layout<D, PL, 2, EACH>(a, G, c, blocks, st);
-    default: return by_layout<D, PL, 4, EACH>(a, G, c, blocks, st);
+    return run_chunk<D, PL, 0>(a, G, c, blocks, st);
   }
 }
 

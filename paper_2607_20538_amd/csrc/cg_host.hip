@@ -1069,9 +1069,12 @@ size_t attend_chunk_workspace_bytes(cg_gauge_shape shp, int32_t nl, int32_t N, i
   if (check_shape(shp) != CG_OK || check_chunk(nl, N, B, max_q, Hq, max_pages, page_size, window, sinks, shp) != CG_OK || N == 0)
     return 0;
   const int cap = max_pages * page_size;
-  // the two launches follow one another and share it
-  return std::max(chunk_plan(nl, N, B, max_q, shp.H, Hq, shp.d, cap, window, sinks).ws_bytes,
-                  max_q == 1 || B > 1 ? singles_plan(nl, B, shp.H, Hq, shp.d, cap, window, sinks).ws_bytes : 0);
+  // whatever the codec; the two launches follow one another and share it
+  size_t ws = 0;
+  for (int singles = 0; singles < 2; ++singles)
+    ws = std::max(ws, chunk_plan(nl, N, B, max_q, shp.H, Hq, shp.d, cap, window, sinks, singles != 0).ws_bytes);
+  if (max_q == 1 || B > 1) ws = std::max(ws, singles_plan(nl, B, shp.H, Hq, shp.d, cap, window, sinks).ws_bytes);
+  return ws;
 }
 
 int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const int32_t* cu, int32_t B, int32_t max_q,
@@ -1095,9 +1098,11 @@ int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const
   if ((rc = check_chunk(nl, q->T, B, max_q, q->H, pages->max_pages, pages->page_size, window, sinks, shp)) != CG_OK) return rc;
   if (q->T == 0) return CG_OK;
   const int cap = pages->max_pages * pages->page_size;
-  const ChunkPlan p = chunk_plan(nl, q->T, B, max_q, shp.H, q->H, shp.d, cap, window, sinks);
+  const CodecDev c = codec_dev(codec);
+  const bool singles = (max_q == 1 || B > 1) && (attend_mfma_supported(shp.d, true, c) || !chunk_wide(c, shp.d));
+  const ChunkPlan p = chunk_plan(nl, q->T, B, max_q, shp.H, q->H, shp.d, cap, window, sinks, singles);
   const AttendPlan one = singles_plan(nl, B, shp.H, q->H, shp.d, cap, window, sinks);
-  const size_t ws = std::max(p.ws_bytes, max_q == 1 || B > 1 ? one.ws_bytes : 0);
+  const bool ws = (p.ws_bytes && (max_q > 1 || !singles)) || (one.ws_bytes && singles);
   if (ws && (!workspace || !aligned16(workspace))) return workspace ? CG_ERR_ALIGN : CG_ERR_ARG;
   if (int64_t(nl) * shp.H * p.nqc * p.ntile * p.nsplit > INT32_MAX) return CG_ERR_CAPACITY;
   ChunkDev a;
@@ -1120,7 +1125,6 @@ int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const
   a.window = window;
   a.sinks = sinks;
   a.cap = cap;
-  a.waves = p.waves;
   a.tq = p.tq;
   a.heads = p.heads;
   a.nqc = p.nqc;
@@ -1129,10 +1133,8 @@ int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const
   a.part = static_cast<float*>(workspace);
   a.ml = a.part ? a.part + size_t(nl) * p.nsplit * q->T * q->H * shp.d : nullptr;
   a.err = err_flag;
-  const CodecDev c = codec_dev(codec);
   const GaugeDev G = gauge_dev(G_dev, shp);
   hipStream_t st = static_cast<hipStream_t>(stream);
-  const bool singles = (max_q == 1 || B > 1) && (attend_mfma_supported(shp.d, true, c) || !chunk_wide(c, shp.d));
   a.min_q = singles ? 2 : 1;
   hipError_t e = hipSuccess;
   if (!singles || max_q > 1) e = launch_chunk(a, G, c, st);
