@@ -977,8 +977,8 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
   const uint32_t voff = uint32_t(8 * gq) * RB + (vcb & ~3u);           // its first dword, token 8 gq
   const uint32_t vsh = (vcb & 3u) * 8;                                 // chunk bit offset in that dword
 
-  // One 32-position step; FULL: all 32 positions lie before t_end (no clamping)
-  auto step = [&](int t0, auto fullc) {
+  // One 32-position step; FULL: all 32 positions lie before t_end (no clamping); packed rows come with its page
+  auto step = [&](int t0, auto fullc, int page = 0) {
     constexpr bool FULL = decltype(fullc)::value;
     const int lim = (PACK ? held : t_endq) - 1 - t0;  // last valid position offset in the step
     // packed rows: positions between the sinks and the window are hidden
@@ -987,7 +987,14 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
     // cache row of position t0 (a step never crosses a page)
     size_t sslc;
     int poff;
-    if (!step_slice(a, l, b, h, t0, sslc, poff)) return;  // uniform over the wave
+    if constexpr (PACK) {
+      poff = t0 / a.pt.page_size * a.pt.page_size;
+      if (page < 0 || page >= a.kc.B) {
+        if (a.err) atomicOr(a.err, CG_FLAG_POS_RANGE);
+        return;
+      }
+      sslc = (size_t(l) * a.kc.B + page) * a.kc.H + h;
+    } else if (!step_slice(a, l, b, h, t0, sslc, poff)) return;  // uniform over the wave
     const size_t srow = sslc * size_t(a.kc.T_cap) + (t0 - poff);
     const uint8_t* kb = a.kc.codes + srow * RB;
     const uint8_t* vb = a.vc.codes + srow * RB;
@@ -1220,10 +1227,23 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
     __builtin_amdgcn_wave_barrier();
   };
   if constexpr (PACK) {
-    for (int v = t_begin + 32 * w; v < t_end; v += 128) {
+    // the page of a step is looked up two steps before, so that its codes are not a second latency behind it
+    const int wv = __builtin_amdgcn_readfirstlane(w);
+    auto page_at = [&](int v) {
+      return v < t_end ? a.pt.pages[size_t(b) * a.pt.max_pages + pr.at(v) / a.pt.page_size] : -1;
+    };
+    auto full = [&](int t0) { return t0 + 32 <= held && (t0 >= pr.lo || t0 + 32 <= pr.sinks); };
+    int p0 = page_at(t_begin + 32 * wv), p1 = page_at(t_begin + 32 * wv + 128);
+    for (int v = t_begin + 32 * wv; v < t_end; v += 128) {
+      const int t0 = pr.at(v), page = p0;
+      p0 = p1;
+      p1 = page_at(v + 256);
+      if (full(t0)) step(t0, std::true_type{}, page);
+    }
+    // the steps seen in part, in a loop of their own (with both kinds in one: 162 registers and three waves per SIMD)
+    for (int v = t_begin + 32 * wv; v < t_end; v += 128) {
       const int t0 = pr.at(v);
-      if (t0 + 32 <= held && (t0 >= pr.lo || t0 + 32 <= pr.sinks)) step(t0, std::true_type{});
-      else if (t0 + 32 > pr.lo || t0 < pr.sinks) step(t0, std::false_type{});  // (else nothing of it is seen)
+      if (!full(t0) && (t0 + 32 > pr.lo || t0 < pr.sinks)) step(t0, std::false_type{}, page_at(v));
     }
   } else {
     int t0 = t_begin + 32 * w;

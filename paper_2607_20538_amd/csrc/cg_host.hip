@@ -1061,7 +1061,14 @@ static int32_t check_chunk(int32_t nl, int32_t N, int32_t B, int32_t max_q, int3
 // as many positions as they see:
 static AttendPlan singles_plan(int nl, int B, int H, int Hq, int d, int cap, int window, int sinks) {
   const int64_t seen = window > 0 ? int64_t(window) + sinks + 128 : cap;
-  return attend_plan(nl, B, H, Hq, d, int(std::min<int64_t>(cap, seen)));
+  const int span = int(std::min<int64_t>(cap, seen));
+  AttendPlan p = attend_plan(nl, B, H, Hq, d, span);
+  const int64_t rows = int64_t(nl) * B * H * p.nqc;
+  // three workgroups per CU, what the kernel's registers let run at once: 32 rows behind 4096 positions 56 us, 77 with
+  // the eight per CU of contiguous rows (every split reads the head's gauge)
+  p.nsplit = int(std::max<int64_t>(1, std::min<int64_t>((3 * cu_count() + rows - 1) / rows, (int64_t(span) + 255) / 256)));
+  p.ws_bytes = p.nsplit > 1 ? size_t(nl) * B * Hq * p.nsplit * (2 + 2 * size_t(d)) * sizeof(float) : 0;
+  return p;
 }
 
 size_t attend_chunk_workspace_bytes(cg_gauge_shape shp, int32_t nl, int32_t N, int32_t B, int32_t max_q, int32_t Hq,
