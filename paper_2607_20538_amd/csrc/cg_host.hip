@@ -409,10 +409,17 @@ hipError_t launch_decode(int s, const CacheDev& k, int l0, const GaugeDev& G, co
   return launch_decode_generic(s, k, l0, G, c, t0, len, pos, pos_add, Y, err, st);
 }
 
-// Packed tokens through their slots: the tokens take the place of the batch rows of a rolling append.
+// Packed tokens through their slots.  Many tokens of the shapes that the bf16 matrix-core encoder takes go through it;
+// otherwise they take the place of the batch rows of a rolling append.  Encoder against append, d = g = 128, 4 bits, us:
+// one layer of 8 heads 8 : 9 at 512 tokens, 22 : 61 at 6000; 8 layers of 8 heads 8 : 7 at 16, 8 : 9 at 64, 18 : 44 at
+// 512.  Below, they are even: both are the launch and one chain of loads.
 static hipError_t launch_append_slots(const ViewDev& Kn, const ViewDev& Vn, int l0, const int* slots, const GaugeDev& G,
                                       const CodecDev& c, const CacheDev& kc, const CacheDev& vc, int* err,
                                       hipStream_t st) {
+  constexpr int64_t kEncodeRows = 4096;  // token rows, all layers and heads
+  if (!force_generic() && int64_t(Kn.T) * Kn.L * Kn.H >= kEncodeRows && mfma_encode_supported(Kn, G, c, true) &&
+      mfma_encode_supported(Vn, G, c, true))
+    return launch_encode_slots(Kn, Vn, l0, slots, G, c, kc, vc, err, st);
   constexpr int kMost = 1 << 19;  // tokens of a launch (its grid holds 2^16 groups of 16)
   for (int i0 = 0; i0 < Kn.T; i0 += kMost) {
     ViewDev x[2] = {Kn, Vn};

@@ -117,6 +117,10 @@ bool mfma_decode_supported(int s, const ViewDev& Y, const GaugeDev& G, const Cod
 hipError_t launch_encode_mfma(int s, const ViewDev& X, int l0, const GaugeDev& G, const CodecDev& c,
                               const CacheDev& k, int t0, int tq, int* err, hipStream_t st,
                               const PageDev& pt = PageDev());
+// Packed tokens ([L][1][H][N][d], keys and values in one launch) to their slots, where
+// mfma_encode_supported(.., paged) takes both views
+hipError_t launch_encode_slots(const ViewDev& Kn, const ViewDev& Vn, int l0, const int* slots, const GaugeDev& G,
+                               const CodecDev& c, const CacheDev& kc, const CacheDev& vc, int* err, hipStream_t st);
 hipError_t launch_decode_mfma(int s, const CacheDev& k, int l0, const GaugeDev& G, const CodecDev& c, int t0,
                               int len, const int* pos, int pos_add, const ViewDev& Y, int* err, hipStream_t st);
 

@@ -39,9 +39,15 @@ struct MfmaArgs {
   uint16_t* ring;
   int kivi, win, kg, len;
   // paged encode: the page of batch row b's positions [i P, (i + 1) P) is pages[b max_pages + i], and
-  // T_cap = P = page_size, cB = pages of the pool
+  // T_cap = P = page_size, cB = pages of the pool; slots: pages[token] is the token's slot
   const int* pages;
   int max_pages;
+  struct {  // slots: the values' tokens and cache, in the same launch as the keys'
+    char* x;
+    int64_t sl, sh, st;
+    uint8_t* codes;
+    uint32_t* side;
+  } v;
   // work split
   int nslices, chunks, tiles_per_wg;
   // decode only: batch row b holds positions [0, pos[b] + pos_add) (rolling step: pos_add = 1,

@@ -104,6 +104,10 @@ constexpr int kModePass = 1;   // error-free backend: binary32 z
 constexpr int kModeKeys = 2;   // KIVI keys: one block per channel over a 32-token group
 constexpr int kModeZfp = 3;    // zfp-style fixed-rate blocks of 4 tokens x 4 channels (BITS = rate)
 
+// where rows go: the batch row, its pages, the tokens' slots (at most kSlotTiles tiles per workgroup)
+constexpr int kDestRows = 0, kDestPages = 1, kDestSlots = 2;
+constexpr int kSlotTiles = 32;
+
 // Software pipeline over 32-token tiles, one barrier per tile.  Iteration t:
 //   1. block-range partials of tile t from its accumulator (64-channel blocks: wave-pair
 //      exchange through red[t & 1]);
@@ -115,13 +119,16 @@ constexpr int kModeZfp = 3;    // zfp-style fixed-rate blocks of 4 tokens x 4 ch
 // kStages - 1 tiles are in flight between global memory and LDS.  The codes of a tile are one
 // contiguous run of 32 RB bytes in the cache and its side words one run of 32 NBK words, so
 // the staged copy leaves with whole-line stores instead of 32 scattered row pieces.
-// PAGED: the cache is a page pool; the rows of a tile (always inside one page) go to the page its
+// kDestSlots (SLOTS): every token goes where its slot says (a.pages[token], page * T_cap + position; negative:
+// nowhere); the staged rows leave as before, each to its own place.
+// kDestPages (PAGED): the cache is a page pool; the rows of a tile (always inside one page) go to the page its
 // positions map to, looked up one tile ahead of the tile's first use.  Blocks with a non-finite value are
 // coded again after the range (recode_rows).
-template <int NP, int KS, int BITS, int NB, int MODE, int TB = 1, bool PAGED = false>
+template <int NP, int KS, int BITS, int NB, int MODE, int TB = 1, int DEST = kDestRows>
 __global__ __launch_bounds__(kThreads, NP == 2 ? 3 : 2) void enc_mfma(MfmaArgs a) {
   constexpr bool PASS = MODE == kModePass, KEYS = MODE == kModeKeys, ZFP = MODE == kModeZfp;
   constexpr bool QUANT = !PASS && !ZFP;  // block ranges, staged codes and side words
+  constexpr bool PAGED = DEST == kDestPages, SLOTS = DEST == kDestSlots;
   // token-channel tiles: one range per TB tokens x NB channels (NB spans whole waves)
   constexpr bool TILE = TB > 1;
   static_assert(!TILE || (TB == 16 && MODE == kModeBU && (NB == 64 || NB == 128)), "tile shape");
@@ -144,8 +151,17 @@ __global__ __launch_bounds__(kThreads, NP == 2 ? 3 : 2) void enc_mfma(MfmaArgs a
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int n = lane & 31, hc = lane >> 5;
   const int logical = xcd_remap(blockIdx.x, gridDim.x);
-  const int slice = logical / a.chunks, chunk = logical - slice * a.chunks;
+  int slice = logical / a.chunks;
+  const int chunk = logical - slice * a.chunks;
   if (slice >= a.nslices) return;
+  if constexpr (SLOTS) {  // keys, then values
+    if (slice >= a.L * a.H) {
+      slice -= a.L * a.H;
+      a.s = 1;
+      a.x = a.v.x; a.sl = a.v.sl; a.sh = a.v.sh; a.st = a.v.st;
+      a.codes = a.v.codes; a.side = a.v.side;
+    }
+  }
   const int h = slice % a.H, b = (slice / a.H) % a.B, lv = slice / (a.H * a.B);
   const int l = lv + a.l0;
   const int ntiles = (a.T + kTok - 1) / kTok;
@@ -175,6 +191,19 @@ __global__ __launch_bounds__(kThreads, NP == 2 ? 3 : 2) void enc_mfma(MfmaArgs a
     return;
   }
   if constexpr (ZFP) zfp_tables_init(ztab);  // read after the prologue's barrier
+  int flags = 0;
+  // the cache rows of the workgroup's tokens (-1: skipped, outside the pool, or past the view), all looked up
+  // before the first tile: in the loop a lookup's wait would also be one for the tiles in flight
+  __shared__ int64_t srow[SLOTS ? kSlotTiles * kTok : 1];
+  if constexpr (SLOTS) {
+    for (int i = int(threadIdx.x); i < (te - tb) * kTok; i += kThreads) {
+      const int tok = tb * kTok + i, slot = tok < a.T ? a.pages[tok] : -1;
+      const int pg = slot >= 0 ? slot / a.T_cap : -1;
+      if (pg >= a.cB) flags |= CG_FLAG_POS_RANGE;
+      srow[i] = pg < 0 || pg >= a.cB ? int64_t(-1)
+                                     : int64_t((size_t(l) * a.cB + pg) * a.cH + h) * a.T_cap + (slot - pg * a.T_cap);
+    }
+  }
 
   // K range of this wave's rows: the group of channels 32w.. (whole head for g = 128)
   const int kbase = a.g >= 32 ? (32 * w / a.g) * a.g : 32 * w;
@@ -244,7 +273,6 @@ __global__ __launch_bounds__(kThreads, NP == 2 ? 3 : 2) void enc_mfma(MfmaArgs a
   bfrags(tb);
   f32x16_t acc[2];
   acc[0] = mfma_chain<NP, KS, KEYS>(A, Bf);
-  int flags = 0;
   // cache row of tile t's first token: positions t0 + 32 t of the row, or of its page (-1: outside
   // the table or the pool); paged caches keep the rows of the tile being flushed and of this one
   auto page_of = [&](int tile) {
@@ -256,8 +284,8 @@ __global__ __launch_bounds__(kThreads, NP == 2 ? 3 : 2) void enc_mfma(MfmaArgs a
     return int64_t((size_t(l) * a.cB + pg) * a.cH + h) * a.T_cap + (a.t0 + tile * kTok) % a.T_cap;
   };
   int64_t prow[2] = {-1, -1};
-  __shared__ int recode;  // PAGED: the workgroup met a non-finite z
-  if constexpr (PAGED) {
+  __shared__ int recode;  // pages and slots: the workgroup met a non-finite z
+  if constexpr (PAGED || SLOTS) {
     if (threadIdx.x == 0) recode = 0;  // a barrier follows in every step
   }
   if constexpr (PAGED) prow[0] = page_row(tb, page_of(tb));
@@ -267,6 +295,14 @@ __global__ __launch_bounds__(kThreads, NP == 2 ? 3 : 2) void enc_mfma(MfmaArgs a
     constexpr int P = decltype(parity)::value;
     const int tid = int(threadIdx.x);
     const int nlive = min(a.T, a.tq) - tile * kTok;  // quantised rows of the tile
+    if constexpr (SLOTS) {
+      const int64_t* rows = srow + (tile - tb) * kTok;
+      if (tid < kTok * BITS && rows[tid / BITS] >= 0)
+        *(u32x4_t*)(a.codes + size_t(rows[tid / BITS]) * RB + 16 * (tid % BITS)) = *(const u32x4_t*)(cstage[P] + 16 * tid);
+      const int si = kThreads - 1 - tid;
+      if (si < kTok * NBK && rows[si / NBK] >= 0) a.side[size_t(rows[si / NBK]) * NBK + si % NBK] = sstage[P][si];
+      return;
+    }
     if (PAGED && prow[P] < 0) return;
     const size_t crow0 = PAGED ? size_t(prow[P]) : cslice * a.T_cap + size_t(a.t0 + tile * kTok);
     if (tid < kTok * BITS && tid / BITS < nlive)
@@ -319,6 +355,7 @@ __global__ __launch_bounds__(kThreads, NP == 2 ? 3 : 2) void enc_mfma(MfmaArgs a
     if constexpr (PAGED) {
       if (tile + 1 < te) pg_next = page_of(tile + 1);  // used once this tile is staged
     }
+    if constexpr (SLOTS) live = live && srow[(tile - tb) * kTok + n] >= 0;
     bfrags(tile + 1);
     if constexpr (QUANT) {
       if (tile > tb) flush(tile - 1, std::integral_constant<int, P ^ 1>());
@@ -496,7 +533,7 @@ __global__ __launch_bounds__(kThreads, NP == 2 ? 3 : 2) void enc_mfma(MfmaArgs a
 #pragma unroll
         for (int i = 0; i < BITS; ++i) dst[i] = words[i];
       }
-      if (live) flags |= PAGED ? (bad ? kFlagRecode : sd.flags) : (sd.flags | (bad ? CG_FLAG_NONFINITE : 0));
+      if (live) flags |= PAGED || SLOTS ? (bad ? kFlagRecode : sd.flags) : (sd.flags | (bad ? CG_FLAG_NONFINITE : 0));
       if constexpr (TILE) {
         if (hc == 0 && (n & 15) == 0 && w % (NB / 32) == 0) sstage[P][(n >> 4) * NBK + w / (NB / 32)] = sd.word;
       } else if constexpr (NB == 16) {
@@ -515,7 +552,7 @@ __global__ __launch_bounds__(kThreads, NP == 2 ? 3 : 2) void enc_mfma(MfmaArgs a
   }
   if constexpr (QUANT) {
     // the last tile's staging: every wave's LDS writes done, then the final contiguous stores
-    if (PAGED && (flags & kFlagRecode)) recode = 1;
+    if ((PAGED || SLOTS) && (flags & kFlagRecode)) recode = 1;
     __builtin_amdgcn_s_waitcnt(waitcnt_imm(63));
     __builtin_amdgcn_s_barrier();
     if ((te - tb) & 1) flush(te - 1, std::integral_constant<int, 0>());
@@ -529,6 +566,18 @@ __global__ __launch_bounds__(kThreads, NP == 2 ? 3 : 2) void enc_mfma(MfmaArgs a
         const int64_t row = page_row(tile, page_of(tile));
         if (row < 0) continue;
         flags |= recode_rows(xs + int64_t(tile) * kTok * tstride, tstride, min(kTok, a.T - tile * kTok), kD, NB, BITS,
+                             a.g32 + ((size_t(l) * 2 + a.s) * a.Hg + h) * a.R * a.g * a.g, a.g,
+                             a.codes + size_t(row) * RB, a.side + size_t(row) * NBK, (int*)xtile[0], (float*)xtile[1]);
+      }
+    }
+  } else if constexpr (SLOTS) {
+    if (recode) {
+      flags &= ~kFlagRecode;
+      __builtin_amdgcn_s_waitcnt(waitcnt_imm(0));
+      for (int i = 0; i < min(a.T - tb * kTok, (te - tb) * kTok); ++i) {
+        const int64_t row = srow[i];
+        if (row < 0) continue;
+        flags |= recode_rows(xs + int64_t(tb * kTok + i) * tstride, tstride, 1, kD, NB, BITS,
                              a.g32 + ((size_t(l) * 2 + a.s) * a.Hg + h) * a.R * a.g * a.g, a.g,
                              a.codes + size_t(row) * RB, a.side + size_t(row) * NBK, (int*)xtile[0], (float*)xtile[1]);
       }
@@ -565,15 +614,16 @@ void* enc_kernel(int mode, int bt) {
 // (relative error 1.2e-7 against 2.0e-7 at g = 128, 0.7e-7 against 1.0e-7 at g = 32).  8 layers x 4 rows x
 // 8 heads x 2000 tokens in 256-position pages, g = 128, 4 bits: 1058 us per tensor on the vector ALU, 236
 // on the binary32 matrix cores (the general kernel, which other shapes keep), 70 here.
-constexpr int kModePaged = 4;
+constexpr int kModePaged = 4, kModeSlots = 5;
 
 template <int KS, int BITS>
 void* enc_by_nb(int nb, int mode, int bt) {
-  if (mode == kModePaged) {
+  if (mode == kModePaged || mode == kModeSlots) {
+    const bool slots = mode == kModeSlots;
     switch (nb) {
-      case 16: return (void*)enc_mfma<3, KS, BITS, 16, kModeBU, 1, true>;
-      case 32: return (void*)enc_mfma<3, KS, BITS, 32, kModeBU, 1, true>;
-      case 64: return (void*)enc_mfma<3, KS, BITS, 64, kModeBU, 1, true>;
+      case 16: return slots ? (void*)enc_mfma<3, KS, BITS, 16, kModeBU, 1, kDestSlots> : (void*)enc_mfma<3, KS, BITS, 16, kModeBU, 1, kDestPages>;
+      case 32: return slots ? (void*)enc_mfma<3, KS, BITS, 32, kModeBU, 1, kDestSlots> : (void*)enc_mfma<3, KS, BITS, 32, kModeBU, 1, kDestPages>;
+      case 64: return slots ? (void*)enc_mfma<3, KS, BITS, 64, kModeBU, 1, kDestSlots> : (void*)enc_mfma<3, KS, BITS, 64, kModeBU, 1, kDestPages>;
     }
     return nullptr;
   }
@@ -594,6 +644,15 @@ void* enc_by_bits(int bits, int nb, int mode, int bt) {
     case 4: return enc_by_nb<KS, 4>(nb, mode, bt);
     case 6: return enc_by_nb<KS, 6>(nb, mode, bt);
     case 8: return enc_by_nb<KS, 8>(nb, mode, bt);
+  }
+  return nullptr;
+}
+
+const void* enc_of(int g, int bits, int nb, int mode, int bt) {
+  switch (ksteps(g)) {
+    case 2: return enc_by_bits<2>(bits, nb, mode, bt);
+    case 4: return enc_by_bits<4>(bits, nb, mode, bt);
+    case 8: return enc_by_bits<8>(bits, nb, mode, bt);
   }
   return nullptr;
 }
@@ -634,17 +693,40 @@ hipError_t launch_encode_mfma(int s, const ViewDev& X, int l0, const GaugeDev& G
   m.max_pages = pt.max_pages;
   const int mode = pt.pages ? kModePaged : pass ? kModePass : (zfp ? kModeZfp : (kivi && s == 0 ? kModeKeys : kModeBU));
   const int nb = pass || zfp ? 64 : (kivi ? c.kvc : c.n), bits = pass ? 8 : c.bits, bt = tiles ? c.bt : 1;
-  void* fn = nullptr;
-  switch (ksteps(G.g)) {
-    case 2: fn = enc_by_bits<2>(bits, nb, mode, bt); break;
-    case 4: fn = enc_by_bits<4>(bits, nb, mode, bt); break;
-    case 8: fn = enc_by_bits<8>(bits, nb, mode, bt); break;
-  }
+  const void* fn = enc_of(G.g, bits, nb, mode, bt);
   if (!fn) return hipErrorInvalidValue;
   plan(m, X.L * X.B * X.H, X.T, fn);
   const int nwg = ((m.nslices * m.chunks + 7) / 8) * 8;
   void* args[] = {&m};
   return hipLaunchKernel(fn, dim3(nwg), dim3(kThreads), args, 0, st);
+}
+
+hipError_t launch_encode_slots(const ViewDev& Kn, const ViewDev& Vn, int l0, const int* slots, const GaugeDev& G,
+                               const CodecDev& c, const CacheDev& kc, const CacheDev& vc, int* err, hipStream_t st) {
+  MfmaArgs m{};
+  m.x = (char*)Kn.ptr;
+  m.sl = Kn.sl; m.sh = Kn.sh; m.st = Kn.st;
+  m.v.x = (char*)Vn.ptr;
+  m.v.sl = Vn.sl; m.v.sh = Vn.sh; m.v.st = Vn.st;
+  m.L = Kn.L; m.B = 1; m.H = Kn.H; m.T = m.tq = Kn.T;
+  m.l0 = l0;
+  for (int p = 0; p < 3; ++p) m.gp[p] = G.hi[p];
+  m.g32 = G.f32; m.g = G.g; m.R = G.R; m.Hg = G.H;
+  m.codes = kc.codes; m.side = kc.side; m.v.codes = vc.codes; m.v.side = vc.side;
+  m.T_cap = kc.T_cap; m.cB = kc.B; m.cH = kc.H;
+  m.err = err;
+  m.pages = slots;
+  const void* fn = enc_of(G.g, c.bits, c.n, kModeSlots, 1);
+  if (!fn) return hipErrorInvalidValue;
+  plan(m, 2 * Kn.L * Kn.H, Kn.T, fn);
+  if (m.tiles_per_wg > kSlotTiles) {
+    m.tiles_per_wg = kSlotTiles;
+    m.chunks = ((Kn.T + kTok - 1) / kTok + kSlotTiles - 1) / kSlotTiles;
+  }
+  const int64_t nwg = (int64_t(m.nslices) * m.chunks + 7) / 8 * 8;
+  if (nwg > INT32_MAX) return hipErrorInvalidValue;
+  void* args[] = {&m};
+  return hipLaunchKernel(fn, dim3(uint32_t(nwg)), dim3(kThreads), args, 0, st);
 }
 
 }  // namespace cg

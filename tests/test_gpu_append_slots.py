@@ -107,11 +107,11 @@ def test_slots_match_the_oracle(oc, d, g, dtype, N, tokens_first):
         check_fused_codes(got, want, z["codes"], oc, s, d, int(live.sum()))
 
 
-@pytest.mark.parametrize("N", [20, 1200])
+@pytest.mark.parametrize("N", [20, 1200, 2100])
 def test_slots_flags_and_layers(N):
     """Layers [1, 2) alone are written; slots past the pool are flagged and skipped; a non-finite token is flagged
     and changes no other token."""
-    L, H, d, P, pages = 3, 2, 128, 64, 20
+    L, H, d, P, pages = 3, 2, 128, 64, max(20, N // 64 + 2)
     oc = O.Codec(backend=O.BLOCK_UNIFORM, bits=4, block_c=64)
     c = to_cg(oc)
     G = S.haar(L, H, d, 32, 3)
@@ -256,3 +256,30 @@ def test_a_serving_run(window, sinks):
                     A = scale * (x.abs() @ K[l, j // grp].abs().T).max().item()
                     lim = (math.expm1(4 * 2 * 2.0 ** -11 * A) + 2.0 ** -9) * V[l, j // grp].norm(dim=-1).max() + 2.0 ** -8 * o.norm(dim=-1)
                     assert ((got[l, j, a0:a1] - o).norm(dim=-1) <= lim).all()
+
+
+@pytest.mark.parametrize("bits,n", [(4, 64), (6, 16), (3, 32)])
+def test_slots_long_ranges_of_a_workgroup(monkeypatch, bits, n):
+    """The bytes do not depend on how many tiles of tokens a workgroup takes, nor on the tokens beside a skipped one."""
+    L, H, d, P, N = 1, 2, 128, 64, 2501
+    pages = N // P + 2
+    c = cg.Codec(cg.BLOCK_UNIFORM, bits, n)
+    shp, Gd = S.gauge_dev(S.haar(L, H, d, 64, 7))
+    torch.manual_seed(N + bits)
+    x = [torch.randn((L, 1, N, H, d), device="cuda").to(torch.bfloat16).transpose(2, 3) for _ in (0, 1)]
+    x[0][0, 0, 1, 2200, 5] = float("inf")
+    slots = torch.randperm(pages * P, device="cuda")[:N].to(torch.int32)
+    slots[::97] = -1
+    got = []
+    for tiles in ("1", "3", "40", ""):
+        monkeypatch.setenv("CG_TILES_PER_WG", tiles)
+        pools = _pools(c, L, pages, H, P, d)
+        err = torch.zeros(1, dtype=torch.int32, device="cuda")
+        cg.kv_append_slots(0, L, *x, slots, Gd, shp, c, *pools, err)
+        torch.cuda.synchronize()
+        # the infinite token's block ranges are infinite in binary16 too
+        assert int(err.item()) == cg.CG_FLAG_NONFINITE | cg.CG_FLAG_SIDE_OVERFLOW
+        got.append([(p.codes.clone(), p.side.clone()) for p in pools])
+    for g in got[1:]:
+        for (ca, sa), (cb, sb) in zip(got[0], g):
+            assert torch.equal(ca, cb) and torch.equal(sa, sb)
