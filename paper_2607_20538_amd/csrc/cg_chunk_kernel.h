@@ -34,7 +34,6 @@ namespace cg {
 namespace {
 
 typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
-typedef _Float16 f16x4_t __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
@@ -89,13 +88,20 @@ __device__ __forceinline__ uint32_t gauge_at(const uint16_t* blk, int g, int d, 
   if (col / g != r) return 0u;
   return blk[size_t(r) * g * g + size_t(row - r * g) * g + (col - r * g)];
 }
+// First and last channel of the groups that channels [ch, ch + n) lie in
+__device__ __forceinline__ void reached(int g, int ch, int n, int& first, int& last) {
+  const float invg = 1.0f / float(g);  // (x + 1/2) / g lies at least 1/512 from an integer
+  first = __builtin_amdgcn_readfirstlane(int((float(ch) + 0.5f) * invg)) * g;
+  last = __builtin_amdgcn_readfirstlane(int((float(ch + n - 1) + 0.5f) * invg)) * g + g - 1;
+}
 // Rows row0 .. row0 + ROWS - 1, K-steps kk0 .. kk0 + KS - 1 of NP planes to LDS: row i of plane p at
-// (p ROWS + i) (32 KS + 16), its channels in order.  All NT threads of the workgroup.  Eight reads are in flight
-// per thread: one at a time they were half of the time of a tile with a window of 1024 positions.
-template <int NP, int ROWS, int KS, int NT>
+// (p ROWS + i) (32 KS + 16), its channels in order.  All NT threads of the workgroup.  MOST reads are in flight
+// per thread: one at a time they were half of the time of a tile with a window of 1024 positions; eight instead of
+// four cost the step loop registers (4096 tokens at 20000 positions 1945 us, 1914 with four).
+template <int NP, int ROWS, int KS, int NT, int MOST = 4>
 __device__ __forceinline__ void stage_gauge(uint8_t* dst, const uint16_t* const (&planes)[3], size_t gb, int g, int d,
                                             int row0, int kk0) {
-  constexpr int PER = 2 * KS, TOTAL = NP * ROWS * PER, ITS = (TOTAL + NT - 1) / NT, UN = ITS < 8 ? ITS : 8;
+  constexpr int PER = 2 * KS, TOTAL = NP * ROWS * PER, ITS = (TOTAL + NT - 1) / NT, UN = ITS < MOST ? ITS : MOST;
   auto plane = [&](int p) { return (p == 0 ? planes[0] : (p == 1 ? planes[1] : planes[2])) + gb; };
   auto put = [&](int p, int i, int gr, const u32x4_t& o) {
     *reinterpret_cast<u32x4_t*>(dst + size_t(p * ROWS + i) * (32 * KS + 16) + 16 * gr) = o;
@@ -279,7 +285,7 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
   const int r = min(32 * w + n, rows - 1);
   const int tok = r / nh, jj = r - tok * nh;
   const int pq = pa + tok;
-  const int plow = a.window > 0 ? pq - a.window : -1;   // positions up to here are hidden unless a sink
+  const int plow = a.window > 0 ? max(pq - a.window, -1) : -1;   // positions up to here are hidden unless a sink
   // the first and last position of the wave's queries
   const int wlo = pa + min(32 * w, rows - 1) / nh, whi = pa + min(32 * w + 31, rows - 1) / nh;
   const bool idle = 32 * w >= rows;                     // a wave without queries only moves codes and gauges
@@ -504,49 +510,78 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) z[ct] = f32x16_t{};
     const size_t gb = ((size_t(l) * 2 + 0) * G.H + h) * G.R * size_t(G.g) * G.g;
-    constexpr int GP = PL == 1 ? 2 : 3, KC = D == 256 && PL == 1 ? 2 : 4, GPITCH = 32 * KC + 16;
+    // The gauge in one pass where LDS holds it, here and at the end, and the queries two K-steps ahead of their
+    // products: in passes of 64 channels (32 at the end) with every query waited for, 3 rows of 37 tokens took 34 us
+    // (29 so), 6000 tokens behind a window of 64 positions 124 (116).
+    constexpr int GP = PL == 1 ? 2 : 3, KQ = 2;
+    constexpr int KC = GP * D * (32 * KK + 16) <= SH::bytes ? KK : (D == 256 && PL == 1 ? 2 : 4), GPITCH = 32 * KC + 16;
     static_assert(GP * D * GPITCH <= SH::bytes, "space of the gauge");
+    const bool qb = a.q.bf16;
+    u32x4_t xq[KQ];  // bf16 queries of the KQ K-steps that come next
+    auto read_q = [&](int kk0) {
+#pragma unroll
+      for (int i = 0; i < KQ; ++i) {
+        const int ch = 16 * (kk0 + i) + 8 * hc;
+        xq[i] = u32x4_t{0u, 0u, 0u, 0u};
+        if (qb && ch < d) xq[i] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(a.q.ptr) + qoff + ch);
+      }
+    };
+    // one K-step: NX planes of its queries
+    auto kstep = [&](int kk, int k0, const auto& x, auto nx) {
+      constexpr int NX = decltype(nx)::value;
+      const uint8_t* src = sm + n * GPITCH + 32 * (kk - k0) + 16 * hc;
+      int c0, c1;
+      reached(G.g, 16 * kk, 16, c0, c1);
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        if (32 * ct > c1 || 32 * ct + 31 < c0) continue;  // no group of the K-step reaches this channel tile
+        bf16x8_t A[GP];
+#pragma unroll
+        for (int p = 0; p < GP; ++p) A[p] = as_bf16x8(*reinterpret_cast<const u32x4_t*>(src + (p * D + 32 * ct) * GPITCH));
+#pragma unroll
+        for (int s = 0; s < NX; ++s)
+#pragma unroll
+          for (int p = 0; p < GP; ++p)
+            if (p + s < 3) z[ct] = mfma(A[p], as_bf16x8(x[s]), z[ct]);
+      }
+    };
+    read_q(0);
     for (int k0 = 0; 16 * k0 < d; k0 += KC) {
       if (k0) __syncthreads();
       stage_gauge<GP, D, KC, NT>(sm, G.hi, gb, G.g, d, 0, k0);
       __syncthreads();
+      if (qb) {
+#pragma unroll 1
+        for (int k4 = k0; k4 < k0 + KC && 16 * k4 < d; k4 += KQ) {
+          u32x4_t xc[KQ];
+#pragma unroll
+          for (int i = 0; i < KQ; ++i) xc[i] = xq[i];
+          read_q(k4 + KQ);
+#pragma unroll
+          for (int i = 0; i < KQ; ++i) {
+            const u32x4_t one[1] = {xc[i]};
+            if (16 * (k4 + i) < d) kstep(k4 + i, k0, one, std::integral_constant<int, 1>());
+          }
+        }
+        continue;
+      }
 #pragma unroll 1
       for (int kk = k0; kk < k0 + KC && 16 * kk < d; ++kk) {
         const int ch = 16 * kk + 8 * hc;
         u32x4_t x[3];
 #pragma unroll
         for (int p = 0; p < 3; ++p) x[p] = u32x4_t{0u, 0u, 0u, 0u};
-        int np = 1;
-        if (a.q.bf16) {
-          if (ch < d) x[0] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(a.q.ptr) + qoff + ch);
-        } else {
-          np = 3;
-          if (ch < d) {
-            const float* src = static_cast<const float*>(a.q.ptr) + qoff + ch;
+        if (ch < d) {
+          const float* src = static_cast<const float*>(a.q.ptr) + qoff + ch;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              uint32_t o[3];
-              split_b<3>(src[2 * e], src[2 * e + 1], o);
+          for (int e = 0; e < 4; ++e) {
+            uint32_t o[3];
+            split_b<3>(src[2 * e], src[2 * e + 1], o);
 #pragma unroll
-              for (int p = 0; p < 3; ++p) x[p][e] = o[p];
-            }
+            for (int p = 0; p < 3; ++p) x[p][e] = o[p];
           }
         }
-        const uint8_t* src = sm + n * GPITCH + 32 * (kk - k0) + 16 * hc;
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
-          // rows of this channel tile that no group of the K-step's channels reaches add nothing
-          if (32 * ct / G.g > (16 * kk + 15) / G.g || (32 * ct + 31) / G.g < 16 * kk / G.g) continue;
-          bf16x8_t A[GP];
-#pragma unroll
-          for (int p = 0; p < GP; ++p) A[p] = as_bf16x8(*reinterpret_cast<const u32x4_t*>(src + (p * D + 32 * ct) * GPITCH));
-#pragma unroll
-          for (int s = 0; s < 3; ++s)
-            if (s < np)
-#pragma unroll
-              for (int p = 0; p < GP; ++p)
-                if (p + s < 3) z[ct] = mfma(A[p], as_bf16x8(x[s]), z[ct]);
-        }
+        kstep(kk, k0, x, std::integral_constant<int, 3>());
       }
     }
     __syncthreads();  // the gauge is read
@@ -745,14 +780,17 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
     // hidden positions: after the lane's token, or before its window and no sink
     const bool whole = !blank && t0 + kStep - 1 <= wlo && (a.window == 0 || t0 > whi - a.window || t0 + kStep <= a.sinks);
     if (!whole) {
-      const int last = blank ? -1 : pq;
+      // bit c: position t0 + 4 hc + c is seen; element (ps, e) is bit 32 ps + 8 (e / 4) + e % 4
+      const int t1 = t0 + 4 * hc;
+      auto below = [](int x) { return x <= 0 ? 0ull : (x >= 64 ? ~0ull : (1ull << x) - 1ull); };
+      const uint64_t seen = blank ? 0ull : below(pq - t1 + 1) & (~below(plow - t1 + 1) | below(a.sinks - t1));
+      const uint32_t half[2] = {uint32_t(seen), uint32_t(seen >> 32)};
 #pragma unroll
       for (int ps = 0; ps < 2; ++ps)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          const int t = t0 + 32 * ps + 8 * (e >> 2) + 4 * hc + (e & 3);
-          const bool seen = t <= last && (t > plow || t < a.sinks);
-          S[ps][e] = seen ? S[ps][e] : -INFINITY;
+          const uint32_t keep = uint32_t(__builtin_amdgcn_sbfe(int(half[ps]), 8 * (e >> 2) + (e & 3), 1));
+          S[ps][e] = __uint_as_float((__float_as_uint(S[ps][e]) & keep) | (0xff800000u & ~keep));
         }
     }
     float mx = S[0][0];
@@ -891,7 +929,8 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
   // ---- o = G_V^T (sums / normaliser): the sums are the B operand as they lie
   const float lall = halves_sum(lsum), inv = lall == 0.0f ? 0.0f : 1.0f / lall;  // nothing visible: zeros
   constexpr int OP = PL == 1 ? 2 : 3, OPITCH = 2 * D + 16;
-  static_assert(OP * 32 * OPITCH <= SH::bytes, "space of the gauge");
+  constexpr int OROWS = OP * D * OPITCH <= SH::bytes ? D : 32;  // output channels of a pass
+  static_assert(OP * OROWS * OPITCH <= SH::bytes, "space of the gauge");
   const size_t gb = ((size_t(l) * 2 + 1) * G.H + h) * G.R * size_t(G.g) * G.g;
   const bool mine = 32 * w + n < rows;
   const size_t orow = (size_t(lv) * a.nsplit + sp) * a.N + (qt.tok0 + qt.i0 + tok);
@@ -917,18 +956,22 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
   }
 #pragma unroll 1
   for (int ct = 0; 32 * ct < d; ++ct) {  // output channels 32 ct ..
-    __syncthreads();
-    stage_gauge<OP, 32, KK, NT>(sm, G.tr, gb, G.g, d, 32 * ct, 0);
-    __syncthreads();
+    if (OROWS == 32 || ct == 0) {
+      __syncthreads();
+      stage_gauge<OP, OROWS, KK, NT>(sm, G.tr, gb, G.g, d, 32 * ct, 0);
+      __syncthreads();
+    }
     if (idle) continue;
     f32x16_t y = f32x16_t{};
+    int c0, c1;
+    reached(G.g, 32 * ct, 32, c0, c1);
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
-      if (16 * kk >= d || 32 * ct / G.g > (16 * kk + 15) / G.g || (32 * ct + 31) / G.g < 16 * kk / G.g) continue;
+      if (16 * kk >= d || 16 * kk > c1 || 16 * kk + 15 < c0) continue;
 #pragma unroll
       for (int p = 0; p < OP; ++p) {
         // element e of the sums' operand is channel 16 kk + 8 (e & 1) + 4 (e >> 2) + 2 hc + ((e & 3) >> 1)
-        const uint32_t* src = reinterpret_cast<const uint32_t*>(sm + (32 * p + n) * OPITCH + 32 * kk) + hc;
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(sm + (OROWS * p + (OROWS == 32 ? 0 : 32 * ct) + n) * OPITCH + 32 * kk) + hc;
         const uint32_t c0 = src[0], c4 = src[2], c8 = src[4], c12 = src[6];
         const bf16x8_t A = as_bf16x8(u32x4_t{__builtin_amdgcn_perm(c8, c0, 0x05040100u), __builtin_amdgcn_perm(c8, c0, 0x07060302u),
                                              __builtin_amdgcn_perm(c12, c4, 0x05040100u), __builtin_amdgcn_perm(c12, c4, 0x07060302u)});
