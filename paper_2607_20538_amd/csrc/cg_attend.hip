@@ -33,8 +33,15 @@ __device__ __forceinline__ size_t gauge_block(int l, int s, int h, int r, int H,
   return ((size_t(l) * 2 + s) * H + h) * R + r;
 }
 
+// The larger of two; NANS: a NaN if one is (packed tokens: a score that is no number makes its query's result one, as
+// it does in a chunk; contiguous rows give zeros there)
+template <bool NANS>
+__device__ __forceinline__ float larger(float a, float b) {
+  return NANS ? max_nan(a, b) : fmaxf(a, b);
+}
+template <bool NANS = false>
 __device__ __forceinline__ float wave_max(float v) {
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+  for (int o = 32; o > 0; o >>= 1) v = larger<NANS>(v, __shfl_xor(v, o));
   return v;
 }
 __device__ __forceinline__ float wave_sum(float v) {
@@ -244,7 +251,7 @@ __device__ void finalize_rows(const AttendDev& a, const GaugeDev& G, const OutRo
     }
     if (accr) x += accr[jj * d + i];
     const float ls = lsum[jj];
-    const float o = ls > 0.0f ? x / ls : 0.0f;
+    const float o = ls > 0.0f || (a.cu && ls != ls) ? x / ls : 0.0f;  // (packed tokens: a NaN stays one)
     const size_t off = size_t(lv) * a.o.sl + size_t(b) * a.o.sb + size_t(hq0 + jj) * a.o.sh + i;
     if (a.o.bf16) ((uint16_t*)a.o.ptr)[off] = (uint16_t)f32_to_bf16_rne(o);
     else ((float*)a.o.ptr)[off] = o;
@@ -400,7 +407,7 @@ __global__ __launch_bounds__(kAThreads) void att_generic(AttendDev a, GaugeDev G
       for (int jj = 0; jj < nj; ++jj) {
         const float s = pw[jj * kGTile + lane];
         const float mold = st[jj];
-        const float mnew = fmaxf(mold, wave_max(s));
+        const float mnew = larger<PACK>(mold, wave_max<PACK>(s));
         const float pv = lane < nt ? __expf(s - mnew) : 0.0f;
         const float sum = wave_sum(pv);
         pw[jj * kGTile + lane] = pv;
@@ -545,8 +552,8 @@ __global__ __launch_bounds__(kAThreads) void att_combine(AttendDev a, GaugeDev G
   for (int jj = w; jj < nj; jj += kAThreads / 64) {
     const float* P = part + size_t(jj) * ns * pstride;
     float M = -INFINITY, L = 0.0f;
-    for (int sp = lane; sp < ns; sp += 64) M = fmaxf(M, P[sp * pstride]);
-    M = wave_max(M);
+    for (int sp = lane; sp < ns; sp += 64) M = larger<PACK>(M, P[sp * pstride]);
+    M = wave_max<PACK>(M);
     for (int sp = lane; sp < ns; sp += 64) {
       const float m = P[sp * pstride];
       const float e = m == -INFINITY ? 0.0f : __expf(m - M);
@@ -619,11 +626,12 @@ __device__ __forceinline__ f32x4_t mfma16(const bf16x8_t& a, const bf16x8_t& b, 
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
+template <bool NANS>
 __device__ __forceinline__ float row16_max(float v) {
-  v = fmaxf(v, dpp_mov<0xB1>(v));   // quad_perm [1,0,3,2]
-  v = fmaxf(v, dpp_mov<0x4E>(v));   // quad_perm [2,3,0,1]
-  v = fmaxf(v, dpp_mov<0x124>(v));  // row_ror:4
-  return fmaxf(v, dpp_mov<0x128>(v));  // row_ror:8
+  v = larger<NANS>(v, dpp_mov<0xB1>(v));   // quad_perm [1,0,3,2]
+  v = larger<NANS>(v, dpp_mov<0x4E>(v));   // quad_perm [2,3,0,1]
+  v = larger<NANS>(v, dpp_mov<0x124>(v));  // row_ror:4
+  return larger<NANS>(v, dpp_mov<0x128>(v));  // row_ror:8
 }
 __device__ __forceinline__ float row16_sum(float v) {
   v += dpp_mov<0xB1>(v);
@@ -1164,8 +1172,8 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
 #pragma unroll
     for (int qi = 0; qi < NQL; ++qi) {
       const int j = NBLK == 2 ? gq : 2 * gq + qi;
-      const float mx = row16_max(fmaxf(s[0][qi], s[1][qi]));
-      const float mnew = fmaxf(mrun[qi], mx);
+      const float mx = row16_max<PACK>(larger<PACK>(s[0][qi], s[1][qi]));
+      const float mnew = larger<PACK>(mrun[qi], mx);
       alpha[qi] = __expf(mrun[qi] - mnew);
       const float p0 = __expf(s[0][qi] - mnew), p1 = __expf(s[1][qi] - mnew);
       lp[qi] = fmaf(lp[qi], alpha[qi], p0 + p1);
@@ -1426,7 +1434,7 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
   for (int qi = 0; qi < NQL; ++qi) {
     const int j = NBLK == 2 ? gq : 2 * gq + qi;
     float M = RAW ? rml[0][j < RJ ? j : 0] : -INFINITY;
-    for (int v = 0; v < 4; ++v) M = fmaxf(M, ml[v][0][j]);
+    for (int v = 0; v < 4; ++v) M = larger<PACK>(M, ml[v][0][j]);
     fq[qi] = mrun[qi] == -INFINITY ? 0.0f : __expf(mrun[qi] - M);
 #pragma unroll
     for (int k = 0; k < NBLK; ++k) {
@@ -1457,7 +1465,7 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
   if (threadIdx.x < JQ) {
     const int jj = threadIdx.x;
     float M = RAW ? rml[0][jj < RJ ? jj : 0] : -INFINITY, L = 0.0f;
-    for (int v = 0; v < 4; ++v) M = fmaxf(M, ml[v][0][jj]);
+    for (int v = 0; v < 4; ++v) M = larger<PACK>(M, ml[v][0][jj]);
     for (int v = 0; v < 4; ++v) {
       const float mv = ml[v][0][jj];
       if (mv != -INFINITY) L += ml[v][1][jj] * __expf(mv - M);

@@ -112,6 +112,8 @@ class Case:
 
 RAGGED = [(0, 1), (0, 70), (130, 0), (63, 1), (64, 33), (200, 129), (1, 5)]
 
+ONES = [(700, 1), (0, 1), (64, 1), (130, 0), (63, 1), (131, 1)]
+
 CASES = {
     "b4": dict(rows=RAGGED),
     "b2": dict(rows=RAGGED, bits=2),
@@ -156,6 +158,31 @@ CASES = {
     "window_f32": dict(rows=[(0, 70), (500, 40)], window=100, sinks=70, dtype=torch.float32, H=1),
     "singles": dict(rows=[(700, 1), (0, 1), (64, 1), (63, 1), (131, 1)], grp=4),
     "singles_window": dict(rows=[(700, 1), (0, 1), (64, 1), (63, 1), (131, 1)], grp=4, window=100, sinks=5),
+    "singles_b2": dict(rows=ONES, bits=2, grp=4),
+    "singles_b3_window": dict(rows=ONES, bits=3, n=32, grp=3, window=70, sinks=66),
+    "singles_b6": dict(rows=ONES, bits=6, g=128, grp=1),
+    "singles_b8_window_1": dict(rows=ONES, bits=8, g=64, window=1, grp=9, H=1),
+    "singles_n128": dict(rows=ONES, n=128, g=128, grp=4, window=200, sinks=1),
+    "singles_n32_window": dict(rows=ONES, n=32, grp=4, window=200, sinks=1),
+    "singles_n16": dict(rows=ONES, n=16, bits=6, H=1),
+    "singles_pass": dict(rows=ONES, backend=cg.PASSTHROUGH, H=1, window=90, sinks=3),
+    "singles_f32": dict(rows=ONES, dtype=torch.float32, window=90, sinks=3, grp=4),
+    "singles_f32_n128": dict(rows=ONES, dtype=torch.float32, n=128, bits=3),
+    "singles_d64": dict(rows=ONES, d=64, g=64, n=32, window=90, sinks=3),
+    "singles_d80": dict(rows=ONES, d=80, g=80, n=80, H=1, window=90, sinks=3),
+    "singles_d256": dict(rows=ONES, d=256, g=128, n=128, bits=8, H=1),
+    "singles_grp40": dict(rows=ONES, grp=40, H=1),
+    "singles_layers_p128": dict(rows=ONES, L=2, P=128, grp=4, g=128, window=300, sinks=5),
+    "singles_long": dict(rows=[(9000, 1), (40, 1), (0, 0), (5000, 1)], grp=4, H=1),
+    "singles_long_window": dict(rows=[(9000, 1), (40, 1), (0, 0), (5000, 1)], grp=4, H=1, window=2500, sinks=300),
+    "singles_heads_first": dict(rows=ONES, tokens_first=False, grp=4),
+    "mixed_window": dict(rows=[(700, 1), (40, 90), (0, 1), (300, 33), (64, 1)], grp=4, window=100, sinks=70),
+    "mixed_window_f32": dict(rows=[(700, 1), (40, 90), (0, 1), (300, 3)], grp=2, H=1, window=100, sinks=70, dtype=torch.float32),
+    "mixed_n128": dict(rows=[(700, 1), (40, 90), (0, 1), (300, 33), (64, 1)], n=128, window=1000),
+    "window_largest": dict(rows=[(0, 70), (200, 40), (90, 1)], window=2 ** 31 - 1, sinks=0),
+    "window_and_sinks_largest": dict(rows=[(0, 70), (200, 40), (90, 1)], window=2 ** 31 - 1, sinks=2 ** 31 - 1),
+    "sinks_largest": dict(rows=[(0, 70), (200, 40), (90, 1)], window=3, sinks=2 ** 31 - 1),
+    "many_rows": dict(rows=[(7 * i % 190, 1 + (i % 5 == 0) * (i % 40)) for i in range(130)], H=1),
     "single_long_split": dict(rows=[(6000, 1)], grp=8, H=1),
     "few_long_split": dict(rows=[(5000, 3), (100, 7)], grp=4, H=1, g=128),
     "split_f32": dict(rows=[(3000, 5)], grp=2, H=1, dtype=torch.float32),
@@ -217,6 +244,93 @@ def test_non_finite_positions_reach_only_who_sees_them(what, dtype):
         else:
             err = (got[:, i] - want[0, :, i]).norm(dim=-1)
             assert (err <= bound[0, :, i] + step * want[0, :, i].norm(dim=-1)).all(), i
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(n=128), dict(d=80, g=80, n=80), dict(dtype=torch.float32)], ids=["b4", "n128", "d80", "f32"])
+@pytest.mark.parametrize("what", ["k", "v"])
+def test_non_finite_positions_of_single_tokens(what, kw):
+    """Behind the window and past the sinks a NaN range is not seen; one inside the window or at a sink is."""
+    c = Case([(200, 1), (200, 1), (200, 1)], H=1, window=30, sinks=2, **kw)
+    codes, side = c.pools[0 if what == "k" else 1]
+    good = side.copy()
+    for b, at in enumerate((120, 185, 1)):
+        side[:, c.table[b, at // 64], :, at % 64, 0, 0] = np.float16("nan")
+    c.upload()
+    c.call()
+    torch.cuda.synchronize()
+    got = c.out[0, 0].double().cpu()
+    side[...] = good
+    want, bound = c.ref()
+    step = 2.0 ** -8 if c.out.dtype == torch.bfloat16 else 2.0 ** -24
+    err = (got[:, 0] - want[0, :, 0]).norm(dim=-1)
+    assert (err <= bound[0, :, 0] + step * want[0, :, 0].norm(dim=-1)).all()
+    assert torch.isnan(got[:, 1]).any(-1).all() and torch.isnan(got[:, 2]).any(-1).all()
+
+
+@pytest.mark.parametrize("name", ["b4", "singles_window", "mixed_window", "singles_n128"])
+def test_general_kernels_agree(monkeypatch, name):
+    """With the general kernels asked for the single tokens take theirs; the bounds are the same."""
+    monkeypatch.setenv("CG_KERNELS", "generic")
+    c = Case(**CASES[name])
+    c.call()
+    c.check()
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(d=80, g=80, n=80), dict(dtype=torch.float32, n=128)], ids=["b4", "d80", "f32"])
+@pytest.mark.parametrize("long", [90, 6000])
+def test_non_finite_query_of_a_single_token(kw, long):
+    c = Case([(long, 1), (70, 1), (long, 1)], H=1, grp=2, **kw)
+    c.qd[0, 0, 1, 0, 5] = float("nan")
+    c.qd[0, 0, 0, 2, 9] = float("inf")
+    c.call()
+    torch.cuda.synchronize()
+    got = c.out[0, 0].double().cpu()
+    want, bound = c.ref()
+    step = 2.0 ** -8 if c.out.dtype == torch.bfloat16 else 2.0 ** -24
+    for j, i in ((0, 0), (0, 1), (1, 1), (1, 2)):
+        assert (got[j, i] - want[0, j, i]).norm() <= bound[0, j, i] + step * want[0, j, i].norm()
+    assert not torch.isfinite(got[1, 0]).any() and not torch.isfinite(got[0, 2]).all()
+
+
+def test_lost_pages_of_single_tokens():
+    """A page outside the pool contributes nothing; a row with no other page gives zeros."""
+    c = Case([(300, 1), (40, 1), (200, 1)], H=1)
+    c.pages[0, 1] = c.kc.B
+    c.pages[1, 0] = -5
+    c.call()
+    torch.cuda.synchronize()
+    assert int(c.err.item()) == cg.CG_FLAG_POS_RANGE
+    got = c.out[0, 0].double().cpu()
+    assert (got[:, 1] == 0).all()
+    want, bound = c.ref()
+    assert ((got[:, 2] - want[0, :, 2]).norm(dim=-1) <= bound[0, :, 2] + 2.0 ** -8 * want[0, :, 2].norm(dim=-1)).all()
+    zk, zv = (S.pool_values(c.codec, *p) for p in c.pools)
+    pg = c.table[0][:5]
+    K, V = (torch.from_numpy(z[0, pg, 0].reshape(-1, 128)[:301].copy()) for z in (zk, zv))
+    t = torch.arange(301) // 64 != 1
+    for j in range(2):
+        s = c.scale * (K[t] @ (S.full_gauge(c.G, 0, 0, 0) @ c.q[0, j, 0].double()))
+        o = S.full_gauge(c.G, 0, 1, 0).T @ (torch.softmax(s, 0) @ V[t])
+        assert (got[j, 0] - o).norm() <= 0.03 * V[t].norm(dim=1).max()
+
+
+def test_two_streams_at_once():
+    cs = [Case([(3000, 40), (900, 1)], grp=4, seed=3), Case([(1500, 1), (2000, 17)], grp=4, seed=5, window=900, sinks=4)]
+    ws = [c.workspace()[0] for c in cs]
+    for c, w in zip(cs, ws):
+        c.call(w)
+    torch.cuda.synchronize()
+    want = [c.out.clone() for c in cs]
+    streams = [torch.cuda.Stream() for _ in cs]
+    for _ in range(5):
+        for c in cs:
+            c.base.fill_(7.0)
+        torch.cuda.synchronize()
+        for c, w, st in zip(cs, ws, streams):
+            c.call(w, stream=st.cuda_stream)
+        torch.cuda.synchronize()
+        for c, x in zip(cs, want):
+            assert torch.equal(c.out, x)
 
 
 def test_non_finite_query_stays_in_its_row():
@@ -344,12 +458,13 @@ def test_same_results_twice():
     assert torch.equal(c.out, first)
 
 
-def test_positions_past_32_bits_of_bytes():
+@pytest.mark.parametrize("new", [10, 1])
+def test_positions_past_32_bits_of_bytes(new):
     """The last page of a pool larger than 2^32 bytes of codes (8 bits, 128 channels, 8 heads)."""
     P, H, pages = 256, 8, 17000
     codec = cg.Codec(cg.BLOCK_UNIFORM, 8, 64)
     assert P * H * pages * 128 > 2 ** 32
-    c = Case([(70, 10)], H=8, grp=1, bits=8, P=256, g=128)
+    c = Case([(70, new)], H=8, grp=1, bits=8, P=256, g=128)
     big = [cg.Cache(codec, s, 1, pages, H, P, 128) for s in (0, 1)]
     for s in (0, 1):
         codes, side = c.pools[s]
