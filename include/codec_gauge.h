@@ -401,8 +401,9 @@ int32_t kv_append_paged(int32_t l0, int32_t l1, const cg_kv_view* k_new, const c
  * max_pages * P positions, negative lengths, and more than N tokens set CG_FLAG_POS_RANGE; a pool that
  * runs out sets CG_FLAG_POOL_EMPTY and leaves -1 in the table.  Tokens without a page get slot -1, a negative
  * add counts as 0, a row with a negative held takes no page.  page_size a multiple of 64;
- * n_pages * page_size and max_pages * page_size below 2^31 (CG_ERR_CAPACITY).  Errors: CG_ERR_ARG,
- * CG_ERR_SHAPE, CG_ERR_ALIGN, CG_ERR_CAPACITY, CG_ERR_DEVICE. */
+ * n_pages * page_size and max_pages * page_size below 2^31 (CG_ERR_CAPACITY).  Calls on one pool follow one
+ * another (on one stream, or ordered by events).  Errors: CG_ERR_ARG, CG_ERR_SHAPE, CG_ERR_ALIGN,
+ * CG_ERR_CAPACITY, CG_ERR_DEVICE. */
 int32_t kv_page_map(const int32_t* held, const int32_t* add, int32_t B, const cg_page_pool* pool, int32_t* pages,
                     int32_t max_pages, int32_t page_size, int32_t N, int32_t* cu, int32_t* lens, int32_t* pos,
                     int32_t* slots, int32_t* err_flag, void* stream);
@@ -423,7 +424,8 @@ int32_t rope_make(const cg_rope* rope, cg_rope_plan* plan);
  * (angles exact to 2^-32 turns at any position, products and sums in binary32, one rounding).  x0, y0: views
  * [L][B][H0][T][d] of one element type; x1, y1 (both or neither): views [L][B][H1][T][d] of the same type,
  * turned by the same launch (queries and keys).  y may be x itself (same pointer and strides), else they must
- * not overlap.  pos: device int32 [B][T]; a token with a negative position is left as it was.
+ * not overlap; no two elements of a y share an address (CG_ERR_ARG).  pos: device int32 [B][T]; a token with a
+ * negative position is left as it was.
  * inverse != 0: the transposed map (turned back, the same amplitude): the gradient with respect to x of
  * a gradient given for y.  Errors: CG_ERR_ARG, CG_ERR_SHAPE, CG_ERR_ALIGN, CG_ERR_UNSUPPORTED (d no multiple
  * of 8 or above 256), CG_ERR_CAPACITY (2^31 or more tokens x channels / 2), CG_ERR_DEVICE. */
@@ -434,8 +436,9 @@ int32_t kv_rope(const cg_rope_plan* plan, const cg_kv_view* x0, const cg_kv_view
  * token i of the views k_new, v_new [l1 - l0][1][H][N][d] (view layer j is cache layer l0 + j) goes to position
  * slots[i] mod P of page slots[i] / P of the pools kc, vc (P = their T_cap; slots: device int32 [N], as
  * kv_page_map writes them).  A negative slot skips its token; a page outside the pool sets CG_FLAG_POS_RANGE and
- * skips it; of two tokens with one slot either may stay.  Block-uniform with block_t = 1, or passthrough;
- * P a multiple of 64, pages * P below 2^31.  Errors: as kv_append_paged. */
+ * skips it.  The slots of a call differ (what is left of two tokens with one slot may be a mixture of them).
+ * Block-uniform with block_t = 1, or passthrough; P a multiple of 64, pages * P below 2^31.  Few tokens are coded as
+ * kv_append_paged codes them, many as kv_encode_paged does.  Errors: as kv_append_paged, and CG_ERR_CAPACITY. */
 int32_t kv_append_slots(int32_t l0, int32_t l1, const cg_kv_view* k_new, const cg_kv_view* v_new, const int32_t* slots,
                         const void* G_dev, cg_gauge_shape shp, const cg_codec* codec, const cg_cache* kc,
                         const cg_cache* vc, int32_t* err_flag, void* stream);
@@ -453,10 +456,10 @@ size_t attend_chunk_workspace_bytes(cg_gauge_shape shp, int32_t nl, int32_t N, i
  * Khat, Vhat as kv_decode would return them in binary32.  The first `sinks` positions stay visible behind the
  * window; window = 0: causal (sinks unused).  bf16 outputs are computed from binary16 operands with
  * binary32 sums, binary32 outputs from operands of 22 bits.  Positions a token does not see do not reach its
- * output, whatever their bytes decode to.  Tokens behind the last row are left as they were.  A row whose lens is
+ * output, whatever their bytes decode to; a NaN or infinity that it does see makes it NaN.  Tokens behind the last row are left as they were.  A row whose lens is
  * below n_b or above max_pages * page_size sets CG_FLAG_POS_RANGE and gets zeros; a row whose cu runs backwards,
  * past N or over max_q sets it and is left as it was; a page outside the pool sets it and contributes nothing.
- * Caches: page pools as in kv_attend_paged.  workspace: attend_chunk_workspace_bytes bytes, 16-byte aligned;
+ * Caches: page pools as in kv_attend_paged.  No two elements of out share an address (CG_ERR_ARG).  workspace: attend_chunk_workspace_bytes bytes, 16-byte aligned;
  * calls sharing one workspace on different streams race.  Errors: as kv_attend_paged. */
 int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const int32_t* cu, int32_t B, int32_t max_q,
                               const cg_cache* kc, const cg_cache* vc, const cg_page_table* pages, const void* G_dev,

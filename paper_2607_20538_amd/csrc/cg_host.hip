@@ -2,12 +2,13 @@
 // sizing and dispatch of the encode / decode / rolling-append kernels.
 #include <math.h>
 #include <climits>
-#include <algorithm>
 #include <stdlib.h>
 #include <string.h>
 
+#include <algorithm>
 #include <atomic>
 #include <thread>
+#include <utility>
 #include <vector>
 
 #include "cg_internal.h"
@@ -362,6 +363,19 @@ int32_t check_rows(const cg_kv_view* v) {
   const int64_t unit = v->dtype == CG_DTYPE_BF16 ? 8 : 4;
   if (v->stride_l % unit || v->stride_b % unit || v->stride_h % unit || v->stride_t % unit) return CG_ERR_ALIGN;
   if (v->stride_l < 0 || v->stride_b < 0 || v->stride_h < 0 || v->stride_t < 0) return CG_ERR_ARG;
+  return CG_OK;
+}
+
+// Rows that are written: no two elements share an address
+int32_t check_apart(const cg_kv_view* v) {
+  std::pair<int64_t, int64_t> dims[4] = {{v->stride_l, v->L}, {v->stride_b, v->B}, {v->stride_h, v->H}, {v->stride_t, v->T}};
+  std::sort(dims, dims + 4);
+  int64_t extent = v->d;
+  for (const auto& [stride, n] : dims) {
+    if (n <= 1) continue;
+    if (stride < extent || stride > (INT64_MAX - extent) / n) return CG_ERR_ARG;
+    extent += stride * (n - 1);
+  }
   return CG_OK;
 }
 
@@ -1013,6 +1027,8 @@ int32_t kv_rope(const cg_rope_plan* plan, const cg_kv_view* x0, const cg_kv_view
   if (!aligned4(pos)) return CG_ERR_ALIGN;
   if (int64_t(x0->B) * x0->T > INT32_MAX / (x0->d / 2) - 256 || int64_t(x0->L) * (int64_t(x0->H) + (x1 ? x1->H : 0)) > 65535)
     return CG_ERR_CAPACITY;
+  for (int i = 1; i < (x1 ? 4 : 2); i += 2)
+    if ((rc = check_apart(vs[i])) != CG_OK) return rc;
   ViewDev none{};
   hipError_t e = launch_rope(*plan, view_dev(x0), view_dev(y0), x1 ? view_dev(x1) : none, x1 ? view_dev(y1) : none, pos,
                              inverse != 0, static_cast<hipStream_t>(stream));
@@ -1044,7 +1060,7 @@ int32_t kv_append_slots(int32_t l0, int32_t l1, const cg_kv_view* k_new, const c
   if ((rc = check_view(v_new, shp, nl)) != CG_OK) return rc;
   if (k_new->B != 1 || v_new->B != 1 || v_new->T != k_new->T) return CG_ERR_SHAPE;
   if ((rc = check_pools(kc, vc, codec, shp)) != CG_OK) return rc;
-  if (int64_t(kc->B) * kc->T_cap > INT32_MAX) return CG_ERR_CAPACITY;
+  if (int64_t(kc->B) * kc->T_cap > INT32_MAX || k_new->T > INT32_MAX - 64) return CG_ERR_CAPACITY;
   if (k_new->T == 0) return CG_OK;
   if (!slots) return CG_ERR_ARG;
   if (!aligned4(slots) || !aligned4(err_flag)) return CG_ERR_ALIGN;
@@ -1111,6 +1127,7 @@ int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const
   if ((rc = check_pages(pages, codec, kc)) != CG_OK) return rc;
   if ((rc = check_chunk(nl, q->T, B, max_q, q->H, pages->max_pages, pages->page_size, window, sinks, shp)) != CG_OK) return rc;
   if (q->T == 0) return CG_OK;
+  if ((rc = check_apart(out)) != CG_OK) return rc;
   const int cap = pages->max_pages * pages->page_size;
   const CodecDev c = codec_dev(codec);
   const bool singles = (max_q == 1 || B > 1) && (attend_mfma_supported(shp.d, true, c) || !chunk_wide(c, shp.d));
@@ -1119,6 +1136,7 @@ int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const
   const bool ws = (p.ws_bytes && (max_q > 1 || !singles)) || (one.ws_bytes && singles);
   if (ws && (!workspace || !aligned16(workspace))) return workspace ? CG_ERR_ALIGN : CG_ERR_ARG;
   if (int64_t(nl) * shp.H * p.nqc * p.ntile * p.nsplit > INT32_MAX) return CG_ERR_CAPACITY;
+  if (singles && int64_t(nl) * shp.H * one.nqc * one.nsplit > INT32_MAX / B) return CG_ERR_CAPACITY;
   ChunkDev a;
   a.q = view_dev(q);
   a.o = view_dev(out);

@@ -194,3 +194,16 @@ def test_binding_refuses_host_tensors_and_other_types():
         cg._int32("f", 4, pos=torch.zeros(5, dtype=torch.int32))
     with pytest.raises(ValueError):
         cg._int32("f", None, pages=torch.zeros((4, 4), dtype=torch.int32).t())
+
+
+@pytest.mark.parametrize("strides", [(0, 0, 0, 64), (2048, 2048, 1024, 0), (2048, 2048, 0, 64), (2048, 2048, 64, 64),
+                                     (2048, 2048, 960, 64), (2048, 2048, 32, 128)])
+def test_outputs_that_overlap_are_refused(strides):
+    assert _rope(y0=_view(strides=strides)) == cg.CG_ERR_ARG
+    assert _rope(x1=_view(), y1=_view(strides=strides)) == cg.CG_ERR_ARG
+    assert _attend(q=_view(), out=_view(strides=strides)) == cg.CG_ERR_ARG
+
+
+def test_append_slots_of_too_many_tokens():
+    v = _view(T=2 ** 31 - 32, strides=(0, 0, 0, 0))
+    assert _append(k=v, v=v) == cg.CG_ERR_CAPACITY
