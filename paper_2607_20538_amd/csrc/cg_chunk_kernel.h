@@ -709,222 +709,222 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
     }
   }
   while (v < v1) {
-  bool odd = false;
-  for (; v < v1; ++v) {
-    const int t0 = step_pos(v);
-    const uint8_t* buf = buf_of(v);
-    if constexpr (!FUSED) begin();
-    odd = odd_step();
-    if (odd) break;
-    // nothing of the step is visible to this wave's queries, or it holds nothing
-    const bool blank = !ok || skip;
-    skip = false;
-    // scores; operands KB K-steps ahead of the products
-    f32x16_t S[2];
-    S[0] = f32x16_t{};
-    S[1] = f32x16_t{};
-    constexpr int KB = FUSED ? 1 : 2;
-    const uint8_t* kb = buf + n * SH::KP + 16 * hc;
-    f16x8_t kf[2][KB][2][PL];  // buffer, K-step, positions, plane
-    auto kload = [&](int s, int k2) {
+    bool odd = false;
+    for (; v < v1; ++v) {
+      const int t0 = step_pos(v);
+      const uint8_t* buf = buf_of(v);
+      if constexpr (!FUSED) begin();
+      odd = odd_step();
+      if (odd) break;
+      // nothing of the step is visible to this wave's queries, or it holds nothing
+      const bool blank = !ok || skip;
+      skip = false;
+      // scores; operands KB K-steps ahead of the products
+      f32x16_t S[2];
+      S[0] = f32x16_t{};
+      S[1] = f32x16_t{};
+      constexpr int KB = FUSED ? 1 : 2;
+      const uint8_t* kb = buf + n * SH::KP + 16 * hc;
+      f16x8_t kf[2][KB][2][PL];  // buffer, K-step, positions, plane
+      auto kload = [&](int s, int k2) {
 #pragma unroll
-      for (int i = 0; i < KB; ++i)
+        for (int i = 0; i < KB; ++i)
+#pragma unroll
+          for (int ps = 0; ps < 2; ++ps)
+#pragma unroll
+            for (int p = 0; p < PL; ++p)
+              kf[s][i][ps][p] = as_f16x8(*reinterpret_cast<const u32x4_t*>(kb + 32 * ps * SH::KP + 32 * (KB * k2 + i) + p * SH::plane));
+      };
+      __builtin_amdgcn_sched_barrier(0);
+      kload(0, 0);
+#pragma unroll
+      for (int k2 = 0; k2 < KK / KB; ++k2) {
+        if (k2 + 1 < KK / KB) kload((k2 + 1) & 1, k2 + 1);
+        if constexpr (!FUSED) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < KB; ++i)
+#pragma unroll
+          for (int ps = 0; ps < 2; ++ps) {
+            const int kk = KB * k2 + i;
+            S[ps] = mfma_h(kf[k2 & 1][i][ps][0], Q[0][kk], S[ps]);
+            if constexpr (PL == 2) {
+              S[ps] = mfma_h(kf[k2 & 1][i][ps][0], Q[PL - 1][kk], S[ps]);
+              S[ps] = mfma_h(kf[k2 & 1][i][ps][PL - 1], Q[0][kk], S[ps]);
+            }
+          }
+        if constexpr (!FUSED) __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (FUSED) {
+        // the next step's codes, between the products; past all of this one's reads they go to the other buffer
+        // (past the last step what is written there is not read)
+        u32x4_t dec[IT][4];
+        const uint32_t flags = decode(v + 1, [&](int i, int, int g, const u32x4_t& o) { dec[i][g] = o; });
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+        for (int k2 = 0; k2 < KK; ++k2) {
+          if (k2 + 1 < KK) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, kFillOps, 0);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < IT; ++i)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) store(buf_of(v + 1), i, 0, g, dec[i][g]);
+        state[(v + 1) & 1][w] = flags;
+        turn();
+      }
+      // hidden positions: after the lane's token, or before its window and no sink
+      const bool whole = !blank && t0 + kStep - 1 <= wlo && (a.window == 0 || t0 > whi - a.window || t0 + kStep <= a.sinks);
+      if (!whole) {
+        // bit c: position t0 + 4 hc + c is seen; element (ps, e) is bit 32 ps + 8 (e / 4) + e % 4
+        const int t1 = t0 + 4 * hc;
+        auto below = [](int x) { return x <= 0 ? 0ull : (x >= 64 ? ~0ull : (1ull << x) - 1ull); };
+        const uint64_t seen = blank ? 0ull : below(pq - t1 + 1) & (~below(plow - t1 + 1) | below(a.sinks - t1));
+        const uint32_t half[2] = {uint32_t(seen), uint32_t(seen >> 32)};
 #pragma unroll
         for (int ps = 0; ps < 2; ++ps)
 #pragma unroll
-          for (int p = 0; p < PL; ++p)
-            kf[s][i][ps][p] = as_f16x8(*reinterpret_cast<const u32x4_t*>(kb + 32 * ps * SH::KP + 32 * (KB * k2 + i) + p * SH::plane));
-    };
-    __builtin_amdgcn_sched_barrier(0);
-    kload(0, 0);
-#pragma unroll
-    for (int k2 = 0; k2 < KK / KB; ++k2) {
-      if (k2 + 1 < KK / KB) kload((k2 + 1) & 1, k2 + 1);
-      if constexpr (!FUSED) __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int i = 0; i < KB; ++i)
-#pragma unroll
-        for (int ps = 0; ps < 2; ++ps) {
-          const int kk = KB * k2 + i;
-          S[ps] = mfma_h(kf[k2 & 1][i][ps][0], Q[0][kk], S[ps]);
-          if constexpr (PL == 2) {
-            S[ps] = mfma_h(kf[k2 & 1][i][ps][0], Q[PL - 1][kk], S[ps]);
-            S[ps] = mfma_h(kf[k2 & 1][i][ps][PL - 1], Q[0][kk], S[ps]);
+          for (int e = 0; e < 16; ++e) {
+            const uint32_t keep = uint32_t(__builtin_amdgcn_sbfe(int(half[ps]), 8 * (e >> 2) + (e & 3), 1));
+            S[ps][e] = __uint_as_float((__float_as_uint(S[ps][e]) & keep) | (0xff800000u & ~keep));
           }
-        }
-      if constexpr (!FUSED) __builtin_amdgcn_sched_barrier(0);
-    }
-    if constexpr (FUSED) {
-      // the next step's codes, between the products; past all of this one's reads they go to the other buffer
-      // (past the last step what is written there is not read)
-      u32x4_t dec[IT][4];
-      const uint32_t flags = decode(v + 1, [&](int i, int, int g, const u32x4_t& o) { dec[i][g] = o; });
-      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-#pragma unroll
-      for (int k2 = 0; k2 < KK; ++k2) {
-        if (k2 + 1 < KK) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x002, kFillOps, 0);
-        }
       }
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int i = 0; i < IT; ++i)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) store(buf_of(v + 1), i, 0, g, dec[i][g]);
-      state[(v + 1) & 1][w] = flags;
-      turn();
-    }
-    // hidden positions: after the lane's token, or before its window and no sink
-    const bool whole = !blank && t0 + kStep - 1 <= wlo && (a.window == 0 || t0 > whi - a.window || t0 + kStep <= a.sinks);
-    if (!whole) {
-      // bit c: position t0 + 4 hc + c is seen; element (ps, e) is bit 32 ps + 8 (e / 4) + e % 4
-      const int t1 = t0 + 4 * hc;
-      auto below = [](int x) { return x <= 0 ? 0ull : (x >= 64 ? ~0ull : (1ull << x) - 1ull); };
-      const uint64_t seen = blank ? 0ull : below(pq - t1 + 1) & (~below(plow - t1 + 1) | below(a.sinks - t1));
-      const uint32_t half[2] = {uint32_t(seen), uint32_t(seen >> 32)};
+      float mx = S[0][0];
 #pragma unroll
       for (int ps = 0; ps < 2; ++ps)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const uint32_t keep = uint32_t(__builtin_amdgcn_sbfe(int(half[ps]), 8 * (e >> 2) + (e & 3), 1));
-          S[ps][e] = __uint_as_float((__float_as_uint(S[ps][e]) & keep) | (0xff800000u & ~keep));
-        }
-    }
-    float mx = S[0][0];
-#pragma unroll
-    for (int ps = 0; ps < 2; ++ps)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, S[ps][e]);
-    mx = halves_max(mx);
-    // the maximum moves only when a score passes it by 2^kLag: the sums are seldom rescaled
-    const bool lift = mx > m && (m == -INFINITY || (mx - m) * cs > kLag);
-    if (__builtin_amdgcn_ballot_w64(lift)) {
-      const float mn = fmaxf(m, mx);
-      const float al = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * cs);
-      m = mn;
-      lsum *= al;
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) O[ct][e] *= al;
-    }
-    const float off = kPBias - (m == -INFINITY ? 0.0f : m * cs);
-    float ls[2] = {0.0f, 0.0f};
-    // values: element e of the lane's operand is position 16 kp + 8 (e / 4) + 4 hc + e % 4
-    const uint8_t* vb = buf + kStep * SH::KP + (4 * hc + ((lane >> 2) & 3)) * SH::VP +
-                        16 * ((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ ((lane >> 2) & 3)) + 8 * (lane & 1);
-    auto vfrag = [&](int plane, int ct, int kp) {
-      typedef __attribute__((address_space(3))) s16x4_t* lds4;
-      const uint8_t* src = vb + plane * SH::plane + 16 * kp * SH::VP + 64 * ct;
-      const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(src));
-      const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(src + 8 * SH::VP));
-      return __builtin_bit_cast(f16x8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-    };
-    // probabilities of K-step kp, operands in P
-    f16x8_t P[2][PL];
-    auto weights = [&](int s, int kp) {
-      u32x4_t hi, lo;
-#pragma unroll
-      for (int e2 = 0; e2 < 4; ++e2) {
-        const int e = 8 * (kp & 1) + 2 * e2;
-        const float p0 = __builtin_amdgcn_exp2f(fmaf(S[kp >> 1][e], cs, off));
-        const float p1 = __builtin_amdgcn_exp2f(fmaf(S[kp >> 1][e + 1], cs, off));
-        const uint32_t both = pk_h(p0, p1);
-        hi[e2] = both;
-        if constexpr (PL == 2) {
-          ls[0] += p0;
-          ls[1] += p1;
-          lo[e2] = pk_h(p0 - h_lo(both), p1 - h_hi(both));
-        } else {
-          // the rounded weights, as the values meet them (v_dot2_f32_f16 adds both to binary32 exactly)
-          const f16x2_t ones = {(_Float16)1.0f, (_Float16)1.0f};
-          ls[e2 & 1] = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2_t, both), ones, ls[e2 & 1], false);
-        }
-      }
-      P[s][0] = as_f16x8(hi);
-      if constexpr (PL == 2) P[s][PL - 1] = as_f16x8(lo);
-    };
-    // the products of K-step kp run while the probabilities of the next are computed
-    constexpr int CB = CT < 4 ? CT : 4;  // channel tiles whose operands are loaded together
-    f16x8_t vf[2][CB][PL];
-    auto vload = [&](int s, int x) {  // batch x: K-step x / (CT / CB), channel tiles CB (x % (CT / CB)) ..
-#pragma unroll
-      for (int i = 0; i < CB; ++i)
-#pragma unroll
-        for (int p = 0; p < PL; ++p) vf[s][i][p] = vfrag(p, CB * (x % (CT / CB)) + i, x / (CT / CB));
-    };
-    constexpr int NB = 4 * (CT / CB);
-    vload(0, 0);
-    weights(0, 0);
-#pragma unroll
-    for (int x = 0; x < NB; ++x) {
-      const int kp = x / (CT / CB), c0 = CB * (x % (CT / CB));
-      if (x + 1 < NB) vload((x + 1) & 1, x + 1);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int i = 0; i < CB; ++i) {
-        O[c0 + i] = mfma_h(vf[x & 1][i][0], P[kp & 1][0], O[c0 + i]);
-        if constexpr (PL == 2) {
-          O[c0 + i] = mfma_h(vf[x & 1][i][0], P[kp & 1][PL - 1], O[c0 + i]);
-          O[c0 + i] = mfma_h(vf[x & 1][i][PL - 1], P[kp & 1][0], O[c0 + i]);
-        }
-      }
-      if (c0 == 0 && kp + 1 < 4) weights((kp + 1) & 1, kp + 1);
-      if (x + 1 < NB) {
-#pragma unroll
-        for (int i = 0; i < CB * (PL == 2 ? 3 : 1); ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-          __builtin_amdgcn_sched_group_barrier(0x402, 9, 0);
-        }
-      }
-      __builtin_amdgcn_sched_barrier(0);
-    }
-    lsum += ls[0] + ls[1];
-    if constexpr (FUSED) __syncthreads();
-  }
-  if (!odd) break;
-  {
-    const int t0 = step_pos(v);
-    odd_rows([&](int s0, int count, const float* krows, const float* vrows) {
-#pragma unroll 1
-      for (int u = 0; u < count; ++u) {
-        const float* kr = krows + u * D;
-        const float* vr = vrows + u * D;
-        const int t = t0 + s0 + u;
-        const bool seen = t <= pq && (t > plow || t < a.sinks);
-        float s = 0.0f;
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk) {
-          // (opaque: the queries in binary32 would otherwise be kept for this rare path, in registers
-          // that the others need)
-          u32x4_t qa = __builtin_bit_cast(u32x4_t, Q[0][kk]), qb = __builtin_bit_cast(u32x4_t, Q[PL - 1][kk]);
-          asm volatile("" : "+v"(qa), "+v"(qb));
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            float q = (e & 1) ? h_hi(qa[e >> 1]) : h_lo(qa[e >> 1]);
-            if constexpr (PL == 2) q += (e & 1) ? h_hi(qb[e >> 1]) : h_lo(qb[e >> 1]);
-            s = fmaf(q, kr[16 * kk + e], s);
-          }
-        }
-        s = halves_sum(s);
-        const float mn = seen ? fmaxf(m, s) : m;
-        const float al = m == mn ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * cs);
-        const float p = seen ? __builtin_amdgcn_exp2f(fmaf(s, cs, kPBias - (mn == -INFINITY ? 0.0f : mn * cs))) : 0.0f;
+        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, S[ps][e]);
+      mx = halves_max(mx);
+      // the maximum moves only when a score passes it by 2^kLag: the sums are seldom rescaled
+      const bool lift = mx > m && (m == -INFINITY || (mx - m) * cs > kLag);
+      if (__builtin_amdgcn_ballot_w64(lift)) {
+        const float mn = fmaxf(m, mx);
+        const float al = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * cs);
         m = mn;
-        lsum = fmaf(lsum, al, hc ? 0.0f : p);
+        lsum *= al;
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float o = O[ct][e] * al;
-            O[ct][e] = seen ? fmaf(p, vr[32 * ct + 8 * (e >> 2) + (e & 3)], o) : o;
-          }
+          for (int e = 0; e < 16; ++e) O[ct][e] *= al;
       }
-    });
-  }
+      const float off = kPBias - (m == -INFINITY ? 0.0f : m * cs);
+      float ls[2] = {0.0f, 0.0f};
+      // values: element e of the lane's operand is position 16 kp + 8 (e / 4) + 4 hc + e % 4
+      const uint8_t* vb = buf + kStep * SH::KP + (4 * hc + ((lane >> 2) & 3)) * SH::VP +
+                          16 * ((2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) ^ ((lane >> 2) & 3)) + 8 * (lane & 1);
+      auto vfrag = [&](int plane, int ct, int kp) {
+        typedef __attribute__((address_space(3))) s16x4_t* lds4;
+        const uint8_t* src = vb + plane * SH::plane + 16 * kp * SH::VP + 64 * ct;
+        const s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(src));
+        const s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(src + 8 * SH::VP));
+        return __builtin_bit_cast(f16x8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+      };
+      // probabilities of K-step kp, operands in P
+      f16x8_t P[2][PL];
+      auto weights = [&](int s, int kp) {
+        u32x4_t hi, lo;
+#pragma unroll
+        for (int e2 = 0; e2 < 4; ++e2) {
+          const int e = 8 * (kp & 1) + 2 * e2;
+          const float p0 = __builtin_amdgcn_exp2f(fmaf(S[kp >> 1][e], cs, off));
+          const float p1 = __builtin_amdgcn_exp2f(fmaf(S[kp >> 1][e + 1], cs, off));
+          const uint32_t both = pk_h(p0, p1);
+          hi[e2] = both;
+          if constexpr (PL == 2) {
+            ls[0] += p0;
+            ls[1] += p1;
+            lo[e2] = pk_h(p0 - h_lo(both), p1 - h_hi(both));
+          } else {
+            // the rounded weights, as the values meet them (v_dot2_f32_f16 adds both to binary32 exactly)
+            const f16x2_t ones = {(_Float16)1.0f, (_Float16)1.0f};
+            ls[e2 & 1] = __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2_t, both), ones, ls[e2 & 1], false);
+          }
+        }
+        P[s][0] = as_f16x8(hi);
+        if constexpr (PL == 2) P[s][PL - 1] = as_f16x8(lo);
+      };
+      // the products of K-step kp run while the probabilities of the next are computed
+      constexpr int CB = CT < 4 ? CT : 4;  // channel tiles whose operands are loaded together
+      f16x8_t vf[2][CB][PL];
+      auto vload = [&](int s, int x) {  // batch x: K-step x / (CT / CB), channel tiles CB (x % (CT / CB)) ..
+#pragma unroll
+        for (int i = 0; i < CB; ++i)
+#pragma unroll
+          for (int p = 0; p < PL; ++p) vf[s][i][p] = vfrag(p, CB * (x % (CT / CB)) + i, x / (CT / CB));
+      };
+      constexpr int NB = 4 * (CT / CB);
+      vload(0, 0);
+      weights(0, 0);
+#pragma unroll
+      for (int x = 0; x < NB; ++x) {
+        const int kp = x / (CT / CB), c0 = CB * (x % (CT / CB));
+        if (x + 1 < NB) vload((x + 1) & 1, x + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < CB; ++i) {
+          O[c0 + i] = mfma_h(vf[x & 1][i][0], P[kp & 1][0], O[c0 + i]);
+          if constexpr (PL == 2) {
+            O[c0 + i] = mfma_h(vf[x & 1][i][0], P[kp & 1][PL - 1], O[c0 + i]);
+            O[c0 + i] = mfma_h(vf[x & 1][i][PL - 1], P[kp & 1][0], O[c0 + i]);
+          }
+        }
+        if (c0 == 0 && kp + 1 < 4) weights((kp + 1) & 1, kp + 1);
+        if (x + 1 < NB) {
+#pragma unroll
+          for (int i = 0; i < CB * (PL == 2 ? 3 : 1); ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x402, 9, 0);
+          }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      lsum += ls[0] + ls[1];
+      if constexpr (FUSED) __syncthreads();
+    }
+    if (!odd) break;
+    {
+      const int t0 = step_pos(v);
+      odd_rows([&](int s0, int count, const float* krows, const float* vrows) {
+#pragma unroll 1
+        for (int u = 0; u < count; ++u) {
+          const float* kr = krows + u * D;
+          const float* vr = vrows + u * D;
+          const int t = t0 + s0 + u;
+          const bool seen = t <= pq && (t > plow || t < a.sinks);
+          float s = 0.0f;
+#pragma unroll
+          for (int kk = 0; kk < KK; ++kk) {
+            // (opaque: the queries in binary32 would otherwise be kept for this rare path, in registers
+            // that the others need)
+            u32x4_t qa = __builtin_bit_cast(u32x4_t, Q[0][kk]), qb = __builtin_bit_cast(u32x4_t, Q[PL - 1][kk]);
+            asm volatile("" : "+v"(qa), "+v"(qb));
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              float q = (e & 1) ? h_hi(qa[e >> 1]) : h_lo(qa[e >> 1]);
+              if constexpr (PL == 2) q += (e & 1) ? h_hi(qb[e >> 1]) : h_lo(qb[e >> 1]);
+              s = fmaf(q, kr[16 * kk + e], s);
+            }
+          }
+          s = halves_sum(s);
+          const float mn = seen ? fmaxf(m, s) : m;
+          const float al = m == mn ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * cs);
+          const float p = seen ? __builtin_amdgcn_exp2f(fmaf(s, cs, kPBias - (mn == -INFINITY ? 0.0f : mn * cs))) : 0.0f;
+          m = mn;
+          lsum = fmaf(lsum, al, hc ? 0.0f : p);
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const float o = O[ct][e] * al;
+              O[ct][e] = seen ? fmaf(p, vr[32 * ct + 8 * (e >> 2) + (e & 3)], o) : o;
+            }
+        }
+      });
+    }
   }
   // ---- o = G_V^T (sums / normaliser): the sums are the B operand as they lie
   const float lall = halves_sum(lsum), inv = lall == 0.0f ? 0.0f : 1.0f / lall;  // nothing visible: zeros
