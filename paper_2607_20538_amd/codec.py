@@ -420,29 +420,39 @@ def kv_append_paged(l0: int, l1: int, k_new, v_new, pos, pt: PageTable, G_dev, s
 # a serving step over paged caches: tables and slots, rotary positions, packed tokens
 # ------------------------------------------------------------------------------------------
 
-def _on_device(fn: str, **tensors):
-    """The named tensors lie on the device that is current (the library launches there); int32 ones are
-    contiguous.  None is left out."""
-    import torch
+_int32_type = _current = None
 
-    dev = None
+
+def _on_device(fn: str, **tensors):
+    """The named tensors lie on the device that is current (the library launches there).  None is left out.
+    (Five tensors took 1.0 of a call's 10 us with torch's own question for the device and an import in here.)"""
+    global _current
+    if _current is None:
+        import torch
+
+        _current = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    dev = -1
     for name, t in tensors.items():
         if t is None:
             continue
-        if not t.is_cuda:
+        at = t.get_device()
+        if at < 0:
             raise ValueError(f"{fn}: {name} is not a GPU tensor")
-        if dev is None:
-            dev = torch.cuda.current_device()
-        if t.get_device() != dev:
-            raise ValueError(f"{fn}: {name} is on cuda:{t.get_device()}, the current device is cuda:{dev}")
+        if dev < 0:
+            dev = _current()
+        if at != dev:
+            raise ValueError(f"{fn}: {name} is on cuda:{at}, the current device is cuda:{dev}")
 
 
 def _int32(fn: str, count: int | None = None, **tensors):
     """The named tensors are contiguous int32 tensors of `count` elements (any number: None)."""
-    import torch
+    global _int32_type
+    if _int32_type is None:
+        import torch
 
+        _int32_type = torch.int32
     for name, t in tensors.items():
-        if t.dtype != torch.int32 or not t.is_contiguous():
+        if t.dtype != _int32_type or not t.is_contiguous():
             raise ValueError(f"{fn}: {name} must be a contiguous int32 tensor")
         if count is not None and t.numel() != count:
             raise ValueError(f"{fn}: {name} needs {count} elements, not {t.numel()}")
