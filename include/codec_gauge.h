@@ -459,7 +459,7 @@ size_t attend_chunk_workspace_bytes(cg_gauge_shape shp, int32_t nl, int32_t N, i
  * output, whatever their bytes decode to; a NaN or infinity that it does see makes it NaN.  Tokens behind the last row are left as they were.  A row whose lens is
  * below n_b or above max_pages * page_size sets CG_FLAG_POS_RANGE and gets zeros; a row whose cu runs backwards,
  * past N or over max_q sets it and is left as it was; a page outside the pool sets it and contributes nothing.
- * Caches: page pools as in kv_attend_paged.  No two elements of out share an address (CG_ERR_ARG).  workspace: attend_chunk_workspace_bytes bytes, 16-byte aligned;
+ * Caches: page pools as in kv_attend_paged; max_pages * page_size at most 2^31 - 2^16.  No two elements of out share an address (CG_ERR_ARG).  workspace: attend_chunk_workspace_bytes bytes, 16-byte aligned;
  * calls sharing one workspace on different streams race.  Errors: as kv_attend_paged. */
 int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const int32_t* cu, int32_t B, int32_t max_q,
                               const cg_cache* kc, const cg_cache* vc, const cg_page_table* pages, const void* G_dev,

@@ -109,7 +109,7 @@ __device__ __forceinline__ PackRow pack_row(const AttendDev& a, int b, int sp, b
     r.s64 = min((r.sinks + 63) & ~63, r.lo64);
     r.nv = r.s64 + r.held - r.lo64;
     const int chunk = ((r.nv + a.nsplit - 1) / a.nsplit + 127) & ~127;
-    r.begin = min(r.nv, sp * chunk);
+    r.begin = int(min(int64_t(r.nv), int64_t(sp) * chunk));
     r.end = min(r.nv, r.begin + chunk);
   }
   if (report && flags && a.err) atomicOr(a.err, flags);
@@ -293,8 +293,9 @@ __global__ __launch_bounds__(kAThreads) void att_generic(AttendDev a, GaugeDev G
   float* st = pw + kJQ * kGTile;        // [3][kJQ] running max, normaliser, step factor
 
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  const int sp = blockIdx.x;
-  int sv = blockIdx.y;
+  // (packed rows: one grid dimension, the others end at 65535)
+  const int sp = PACK ? blockIdx.x % a.nsplit : blockIdx.x;
+  int sv = PACK ? blockIdx.x / a.nsplit : blockIdx.y;
   const int qc = sv % a.nqc;
   sv /= a.nqc;
   const int h = sv % H, b = (sv / H) % B, lv = sv / (H * B);
@@ -853,8 +854,9 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int n = lane & 15, gq = lane >> 4;
   const int H = a.kc.H, B = PACK ? a.rows : a.q.B;
-  const int sp = blockIdx.x;
-  int sv = blockIdx.y;
+  // (packed rows: one grid dimension, the others end at 65535)
+  const int sp = PACK ? blockIdx.x % a.nsplit : blockIdx.x;
+  int sv = PACK ? blockIdx.x / a.nsplit : blockIdx.y;
   const int qc = sv % a.nqc;
   sv /= a.nqc;
   const int h = sv % H, b = (sv / H) % B, lv = sv / (H * B);
@@ -1582,8 +1584,8 @@ hipError_t launch_attend(const AttendDev& args_in, const GaugeDev& G, const Code
     const int nrow_f = a.q.L * B * a.kc.H * af.nqc;
     GaugeDev g2 = G;
     void* args[] = {&af, &g2};
-    e = hipLaunchKernel(att_mfma_kernel(c.bits, nblk, c.bt, kivi, pack), dim3(a.nsplit, nrow_f), dim3(kAThreads), args, 0,
-                        st);
+    e = hipLaunchKernel(att_mfma_kernel(c.bits, nblk, c.bt, kivi, pack), pack ? dim3(unsigned(nrow_f) * a.nsplit) : dim3(a.nsplit, nrow_f),
+                        dim3(kAThreads), args, 0, st);
     if (e != hipSuccess) return e;
   } else {
     const size_t smem = (size_t(2) * kJQ * d + generic_tile_floats(d) + kJQ * kGTile + 3 * kJQ) * sizeof(float);
@@ -1593,7 +1595,7 @@ hipError_t launch_attend(const AttendDev& args_in, const GaugeDev& G, const Code
     GaugeDev g2 = G;
     CodecDev c2 = c;
     void* args[] = {&a, &g2, &c2};
-    e = hipLaunchKernel(fn, dim3(a.nsplit, nrow), dim3(kAThreads), args, smem, st);
+    e = hipLaunchKernel(fn, pack ? dim3(unsigned(nrow) * a.nsplit) : dim3(a.nsplit, nrow), dim3(kAThreads), args, smem, st);
     if (e != hipSuccess) return e;
   }
   e = hipGetLastError();

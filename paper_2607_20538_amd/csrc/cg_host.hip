@@ -1073,7 +1073,8 @@ static int32_t check_chunk(int32_t nl, int32_t N, int32_t B, int32_t max_q, int3
                            int32_t window, int32_t sinks, const cg_gauge_shape& shp) {
   if (nl <= 0 || N < 0 || B <= 0 || max_q <= 0 || window < 0 || sinks < 0 || max_pages <= 0) return CG_ERR_ARG;
   if (Hq < shp.H || Hq % shp.H || page_size <= 0 || page_size % 64) return CG_ERR_SHAPE;
-  if (int64_t(max_pages) * page_size > INT32_MAX) return CG_ERR_CAPACITY;
+  // (positions are stepped past in int32, by less than 2^16)
+  if (int64_t(max_pages) * page_size > INT32_MAX - 65535) return CG_ERR_CAPACITY;
   return CG_OK;
 }
 
@@ -1136,7 +1137,8 @@ int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const
   const bool ws = (p.ws_bytes && (max_q > 1 || !singles)) || (one.ws_bytes && singles);
   if (ws && (!workspace || !aligned16(workspace))) return workspace ? CG_ERR_ALIGN : CG_ERR_ARG;
   if (int64_t(nl) * shp.H * p.nqc * p.ntile * p.nsplit > INT32_MAX) return CG_ERR_CAPACITY;
-  if (singles && int64_t(nl) * shp.H * one.nqc * one.nsplit > INT32_MAX / B) return CG_ERR_CAPACITY;
+  // (the matrix-core kernel may halve its query chunks)
+  if (singles && 2 * int64_t(nl) * shp.H * one.nqc * one.nsplit > INT32_MAX / B) return CG_ERR_CAPACITY;
   ChunkDev a;
   a.q = view_dev(q);
   a.o = view_dev(out);

@@ -314,6 +314,54 @@ def test_lost_pages_of_single_tokens():
         assert (got[j, 0] - o).norm() <= 0.03 * V[t].norm(dim=1).max()
 
 
+@pytest.mark.parametrize("kw", [dict(), dict(d=80, g=80, n=80)], ids=["b4", "d80"])
+def test_many_single_rows(kw):
+    """72000 (row, head) pairs, more than a grid's second dimension holds: rows that share pages, lengths and queries."""
+    reps = 3000
+    c = Case([(70, 1), (5, 1), (130, 1)], H=8, grp=1, pad=0, **kw)
+    c.call()
+    c.check()
+    one = c.out.clone()
+    c.pages = c.pages.repeat(reps, 1)
+    c.table = np.tile(c.table, (reps, 1))
+    c.lens = c.lens.repeat(reps)
+    c.N = 3 * reps
+    c.rows = c.rows * reps
+    c.cu = torch.arange(c.N + 1, dtype=torch.int32, device="cuda")
+    c.qd = c.qd.repeat(1, 1, 1, reps, 1)
+    c.out = torch.full((1, 1, 8, c.N, c.d), 7.0, dtype=torch.bfloat16, device="cuda")
+    c.call()
+    torch.cuda.synchronize()
+    assert int(c.err.item()) == 0
+    got = c.out.view(1, 1, 8, reps, 3, c.d)
+    assert (got == got[:, :, :, :1]).all()
+    # the splits may differ: both are within the bound of the same values
+    _, bound = Case([(70, 1), (5, 1), (130, 1)], H=8, grp=1, pad=0, **kw).ref()
+    err = (got[0, 0, :, 0].double() - one[0, 0].double()).cpu().norm(dim=-1)
+    assert (err <= 2 * (bound[0] + 2.0 ** -8 * one[0, 0].double().cpu().norm(dim=-1))).all()
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(d=80, g=80, n=80), dict(dtype=torch.float32)], ids=["b4", "d80", "f32"])
+@pytest.mark.parametrize("new", [40, 1])
+def test_window_at_the_end_of_the_longest_table(kw, new):
+    """The row's last pages moved to the end of a table of 2^31 - 2^16 positions, its first one (the sinks) left in
+    place, nothing between: the same results."""
+    c = Case([(600, new)], H=1, P=256, window=100, sinks=4, spare_pages=0, **kw)
+    want, bound = c.ref()
+    M = (2 ** 31 - 2 ** 16) // 256
+    far = torch.full((1, M), -1, dtype=torch.int32, device="cuda")
+    far[0, 0] = c.pages[0, 0]
+    far[0, M - 2:] = c.pages[0, 1:]
+    c.pages, c.table = far, np.zeros((1, M), np.int8)
+    c.lens += 256 * (M - 3)
+    c.call()
+    torch.cuda.synchronize()
+    assert int(c.err.item()) == 0
+    got = c.out[:, 0].double().cpu()[:, :, :new]
+    step = 2.0 ** -8 if c.out.dtype == torch.bfloat16 else 2.0 ** -24
+    assert ((got - want[:, :, :new]).norm(dim=-1) <= bound[:, :, :new] + step * want[:, :, :new].norm(dim=-1)).all()
+
+
 def test_two_streams_at_once():
     cs = [Case([(3000, 40), (900, 1)], grp=4, seed=3), Case([(1500, 1), (2000, 17)], grp=4, seed=5, window=900, sinks=4)]
     ws = [c.workspace()[0] for c in cs]

@@ -207,3 +207,12 @@ def test_outputs_that_overlap_are_refused(strides):
 def test_append_slots_of_too_many_tokens():
     v = _view(T=2 ** 31 - 32, strides=(0, 0, 0, 0))
     assert _append(k=v, v=v) == cg.CG_ERR_CAPACITY
+
+
+def test_attend_chunk_of_the_longest_tables():
+    top = (2 ** 31 - 2 ** 16) // 64
+    assert _attend(max_pages=top + 1) == cg.CG_ERR_CAPACITY
+    assert _attend(max_pages=top, max_q=1, ws=None) == cg.CG_ERR_ARG
+    shp = cg.shape(1, 2, 64, 16)
+    assert cg.attend_chunk_workspace_bytes(shp, 1, 4, 1, 4, 4, top, 64) > 0
+    assert cg.attend_chunk_workspace_bytes(shp, 1, 4, 1, 4, 4, top + 1, 64) == 0
