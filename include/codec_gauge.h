@@ -456,10 +456,12 @@ size_t attend_chunk_workspace_bytes(cg_gauge_shape shp, int32_t nl, int32_t N, i
  * Khat, Vhat as kv_decode would return them in binary32.  The first `sinks` positions stay visible behind the
  * window; window = 0: causal (sinks unused).  bf16 outputs are computed from binary16 operands with
  * binary32 sums, binary32 outputs from operands of 22 bits.  Positions a token does not see do not reach its
- * output, whatever their bytes decode to; a NaN or infinity that it does see makes it NaN.  Tokens behind the last row are left as they were.  A row whose lens is
- * below n_b or above max_pages * page_size sets CG_FLAG_POS_RANGE and gets zeros; a row whose cu runs backwards,
- * past N or over max_q sets it and is left as it was; a page outside the pool sets it and contributes nothing.
- * Caches: page pools as in kv_attend_paged; max_pages * page_size at most 2^31 - 2^16.  No two elements of out share an address (CG_ERR_ARG).  workspace: attend_chunk_workspace_bytes bytes, 16-byte aligned;
+ * output, whatever their bytes decode to; a NaN or infinity that it does see makes it NaN.  Tokens behind the
+ * last row are left as they were.  A row whose lens is below n_b or above max_pages * page_size sets
+ * CG_FLAG_POS_RANGE and gets zeros; a row whose cu runs backwards, past N or over max_q sets it and is left as it
+ * was; a page outside the pool sets it and contributes nothing.
+ * Caches: page pools as in kv_attend_paged; max_pages * page_size at most 2^31 - 2^16.  No two elements of out
+ * share an address (CG_ERR_ARG).  workspace: attend_chunk_workspace_bytes bytes, 16-byte aligned;
  * calls sharing one workspace on different streams race.  Errors: as kv_attend_paged. */
 int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const int32_t* cu, int32_t B, int32_t max_q,
                               const cg_cache* kc, const cg_cache* vc, const cg_page_table* pages, const void* G_dev,

@@ -283,3 +283,72 @@ def test_slots_long_ranges_of_a_workgroup(monkeypatch, bits, n):
     for g in got[1:]:
         for (ca, sa), (cb, sb) in zip(got[0], g):
             assert torch.equal(ca, cb) and torch.equal(sa, sb)
+
+
+def test_captured_steps_follow_the_lengths():
+    """A step of single tokens captured once (tables, rotary positions, append, attention) and replayed six times, the
+    lengths moving on the device, eager work between the replays: the same bytes and outputs as eager steps."""
+    L, H, grp, d, P, maxp, B = 2, 2, 4, 128, 64, 8, 3
+    c = cg.Codec(cg.BLOCK_UNIFORM, 4, 64)
+    shp, Gd = S.gauge_dev(S.haar(L, H, d, 128, 8))
+    plan = cg.rope_make(d)
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    torch.manual_seed(3)
+    x = [torch.randn((6, L, B, h, d), device="cuda").to(torch.bfloat16) for h in (H * grp, H, H)]
+
+    class Server:
+        def __init__(self):
+            self.pool = cg.PagePool(20)
+            self.pools = [cg.Cache(c, s, L, 20, H, P, d) for s in (0, 1)]
+            self.lens, self.add = i32([0, 62, 300]), i32([1, 1, 1])
+            self.pages = torch.full((B, maxp), -1, dtype=torch.int32, device="cuda")
+            self.cu, self.pos, self.slots, self.err = i32([0] * (B + 1)), i32([0] * B), i32([0] * B), i32([0])
+            # the pages of what the rows hold already: all zeros
+            cu, pos, slots = i32([0] * (B + 1)), i32([0] * 400), i32([0] * 400)
+            cg.kv_page_map(i32([0, 0, 0]), self.lens.clone(), self.pool, self.pages, P, cu, self.lens, pos, slots, self.err)
+            self.q, self.k, self.v = (torch.zeros((L, B, h, d), dtype=torch.bfloat16, device="cuda").transpose(1, 2).unsqueeze(1)
+                                      for h in (H * grp, H, H))
+            self.out = torch.zeros_like(self.q)
+            n = cg.attend_chunk_workspace_bytes(shp, L, B, B, 1, H * grp, maxp, P)
+            self.ws = torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")
+
+        def load(self, i):
+            for t, src in zip((self.q, self.k, self.v), x):
+                t.copy_(src[i].transpose(1, 2).unsqueeze(1))
+
+        def step(self):
+            cg.kv_page_map(self.lens, self.add, self.pool, self.pages, P, self.cu, self.lens, self.pos, self.slots, self.err)
+            cg.kv_rope(plan, self.q, self.q, self.pos.view(1, -1), self.k, self.k)
+            cg.kv_append_slots(0, L, self.k, self.v, self.slots, Gd, shp, c, *self.pools, self.err)
+            cg.kv_attend_chunk_paged(0, L, self.q, self.cu, 1, *self.pools, cg.page_table(self.pages, P), Gd, shp, c, self.lens,
+                                     1 / math.sqrt(d), self.out, workspace=self.ws, err_flag=self.err)
+
+        def state(self):
+            return [t.clone() for t in (self.out, self.lens, self.pages, self.pool.count, self.pos, self.slots, self.err,
+                                        *(b for p in self.pools for b in (p.codes, p.side)))]
+
+    eager, want = Server(), []
+    for i in range(6):
+        eager.load(i)
+        eager.step()
+        torch.cuda.synchronize()
+        want.append(eager.state())
+    assert int(eager.err.item()) == 0 and eager.lens.tolist() == [6, 68, 306]
+    s = Server()
+    first = [t.clone() for t in (s.lens, s.pages, s.pool.count)]
+    s.load(0)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        s.step()
+    torch.cuda.current_stream().wait_stream(side)
+    with torch.cuda.graph(graph):
+        s.step()
+    for t, v in zip((s.lens, s.pages, s.pool.count), first):
+        t.copy_(v)
+    for i in range(6):
+        s.load(i)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(s.state(), want[i]):
+            assert torch.equal(a, b), i
