@@ -87,6 +87,8 @@ __device__ __forceinline__ bool step_slice(const AttendDev& a, int l, int b, int
 
 // A packed row's query and what it sees: positions [0, s64) and [lo64, held) in whole steps of 64, of which those
 // in [sinks, lo) are hidden.  The row's `nv` positions in that order are dealt to the splits in multiples of 128.
+// Bound by the code stream and the vector work of turning codes into operands: 32 rows behind a window of 4096
+// positions, 8 KV heads x 4, d = 128, 4 bits: 43 us = 3.5 TB/s, and 8.6 for joining the splits.
 struct PackRow {
   int tok = -1, held = 0, lo = 0, lo64 = 0, s64 = 0, sinks = 0, nv = 0, begin = 0, end = 0;
   __device__ __forceinline__ int at(int v) const { return v < s64 ? v : v - s64 + lo64; }

@@ -9,7 +9,8 @@
 //
 // A token's angles serve all heads and layers, so a thread keeps the sines and cosines of V pairs of one token
 // and walks `per` (layer, head) rows, 16-byte loads where the widths allow.  Bound by memory: every element is
-// read and written once.
+// read and written once.  8192 tokens x 40 heads of 128 channels, bf16: 30.0 us = 5.6 TB/s (an addition in place over
+// 1 GiB reaches 6.0).
 #include <algorithm>
 
 #include "cg_internal.h"
@@ -190,7 +191,8 @@ hipError_t launch_rope(const cg_rope_plan& plan, const ViewDev& x0, const ViewDe
   if (tokens == 0 || a.skip == 0) return hipSuccess;
   const int64_t blocks = (tokens * a.units + 255) / 256;
   if (tokens * a.units > 0x7fffff00) return hipErrorInvalidValue;
-  // rows per thread: as many as leave about four workgroups per CU, at most 8 (the sines are about 3 rows' work)
+  // rows per thread: as many as leave about four workgroups per CU, at most 8 (8192 tokens x 40 heads: one 41 us, up to
+  // four 31.6, eight 30.0, sixteen 30.1; eight workgroups per CU 31.1)
   a.per = int(std::max<int64_t>(1, std::min<int64_t>(8, blocks * rows / (4 * cu_count()))));
   const int gy = (rows + a.per - 1) / a.per;
   if (gy > 65535) return hipErrorInvalidValue;
