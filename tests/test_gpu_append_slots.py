@@ -352,3 +352,48 @@ def test_captured_steps_follow_the_lengths():
         torch.cuda.synchronize()
         for a, b in zip(s.state(), want[i]):
             assert torch.equal(a, b), i
+
+
+@pytest.mark.parametrize("d,g,N", [(128, 128, 70), (128, 32, 2200), (64, 64, 70)])
+def test_slices_of_a_fused_projection(d, g, N):
+    """Queries, keys and values as slices of one [N][(Hq + 2 H) d] tensor, rows 16 channels apart, turned in place:
+    the same bytes and outputs as from tensors of their own, and nothing else of the projection changes."""
+    H, Hq, P = 2, 6, 64
+    pages = -(-N // P) + 1
+    c = cg.Codec(cg.BLOCK_UNIFORM, 4, 32)
+    shp, Gd = S.gauge_dev(S.haar(1, H, d, g, 5))
+    plan = cg.rope_make(d, cg.ROPE_PAIRS)
+    torch.manual_seed(N + d)
+    wide = (Hq + 2 * H) * d + 16
+    fused = torch.randn((N, wide), device="cuda").to(torch.bfloat16)
+    before = fused.clone()
+
+    def cut(t):
+        h = t[:, : (Hq + 2 * H) * d].view(N, Hq + 2 * H, d).transpose(0, 1)[None, None]
+        return h[:, :, :Hq], h[:, :, Hq: Hq + H], h[:, :, Hq + H:]
+
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    pos = torch.arange(N, dtype=torch.int32, device="cuda")
+    table = torch.randperm(pages, device="cuda").to(torch.int32)[None]
+    slots = (table[0, (pos // P).long()] * P + pos % P).to(torch.int32)
+    res = []
+    for own in (False, True):
+        q, k, v = (t.contiguous() if own else t for t in cut(before.clone() if own else fused))
+        cg.kv_rope(plan, q, q, pos.view(1, -1), k, k)
+        pools = _pools(c, 1, pages, H, P, d)
+        err = torch.zeros(1, dtype=torch.int32, device="cuda")
+        cg.kv_append_slots(0, 1, k, v, slots, Gd, shp, c, *pools, err)
+        out = torch.zeros((N, wide), dtype=torch.bfloat16, device="cuda")
+        o = torch.zeros_like(q) if own else cut(out)[0]
+        n = cg.attend_chunk_workspace_bytes(shp, 1, N, 1, N, Hq, pages, P, 500, 4)
+        ws = torch.empty(max(n, 16), dtype=torch.uint8, device="cuda")
+        cg.kv_attend_chunk_paged(0, 1, q, i32([0, N]), N, *pools, cg.page_table(table, P), Gd, shp, c, i32([N]), d ** -0.5, o, 500,
+                                 4, ws, err)
+        torch.cuda.synchronize()
+        assert int(err.item()) == 0
+        if not own:
+            assert (out[:, Hq * d:] == 0).all()
+            assert torch.equal(fused[:, (Hq + H) * d:], before[:, (Hq + H) * d:])
+        res.append([q.clone(), k.clone(), o.clone(), *(b.clone() for p in pools for b in (p.codes, p.side))])
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
