@@ -443,9 +443,17 @@ int32_t kv_append_slots(int32_t l0, int32_t l1, const cg_kv_view* k_new, const c
                         const void* G_dev, cg_gauge_shape shp, const cg_codec* codec, const cg_cache* kc,
                         const cg_cache* vc, int32_t* err_flag, void* stream);
 
-/* Workspace bytes of kv_attend_chunk_paged (0: none needed, or invalid arguments). */
+/* Workspace bytes of the kv_attend_chunk_paged call with exactly these arguments (0: none needed, or invalid
+ * arguments).  Fewer tokens or rows may need more, since they are split into more parts: a workspace that serves
+ * several calls has attend_chunk_workspace_limit bytes. */
 size_t attend_chunk_workspace_bytes(cg_gauge_shape shp, int32_t nl, int32_t N, int32_t B, int32_t max_q, int32_t Hq,
                                     int32_t max_pages, int32_t page_size, int32_t window, int32_t sinks);
+
+/* Workspace bytes that every kv_attend_chunk_paged call of this gauge shape, Hq and page_size stays within while it has
+ * at most nl layers, N packed tokens, B rows and max_pages pages a row, whatever its max_q, window and sinks
+ * (0: none of them needs any, or invalid arguments). */
+size_t attend_chunk_workspace_limit(cg_gauge_shape shp, int32_t nl, int32_t N, int32_t B, int32_t Hq, int32_t max_pages,
+                                    int32_t page_size);
 
 /* Attention of new tokens over paged caches that hold them already: chunks of prompts, single tokens, or both in
  * one batch.  q, out: views [l1 - l0][1][Hq][N][d] (bf16 or binary32) of N packed tokens; row b's are
@@ -462,8 +470,9 @@ size_t attend_chunk_workspace_bytes(cg_gauge_shape shp, int32_t nl, int32_t N, i
  * CG_FLAG_POS_RANGE and gets zeros; a row whose cu runs backwards, past N or over max_q sets it and is left as it
  * was; a page outside the pool sets it and contributes nothing.
  * Caches: page pools as in kv_attend_paged; max_pages * page_size at most 2^31 - 2^16.  No two elements of out
- * share an address (CG_ERR_ARG).  workspace: attend_chunk_workspace_bytes bytes, 16-byte aligned;
- * calls sharing one workspace on different streams race.  Errors: as kv_attend_paged. */
+ * share an address (CG_ERR_ARG).  workspace: attend_chunk_workspace_bytes of these
+ * arguments, 16-byte aligned; its size is the caller's to get right (the call cannot see it).  Calls sharing one
+ * workspace on different streams race.  Errors: as kv_attend_paged. */
 int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const int32_t* cu, int32_t B, int32_t max_q,
                               const cg_cache* kc, const cg_cache* vc, const cg_page_table* pages, const void* G_dev,
                               cg_gauge_shape shp, const cg_codec* codec, const int32_t* lens, float scale,

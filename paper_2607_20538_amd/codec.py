@@ -31,7 +31,7 @@ EXPORTS = ["cg_status_str", "gauge_device_bytes", "gauge_make", "cache_bytes", "
            "kv_attend_noalloc",
            "attend_paged_workspace_bytes", "kv_attend_paged", "kv_encode_paged", "kv_append_paged",
            "kv_page_map", "kv_page_release", "rope_make", "kv_rope", "kv_append_slots",
-           "attend_chunk_workspace_bytes", "kv_attend_chunk_paged", "cg_selftest",
+           "attend_chunk_workspace_bytes", "attend_chunk_workspace_limit", "kv_attend_chunk_paged", "cg_selftest",
            "cg_stream_probe"]
 
 
@@ -152,6 +152,8 @@ def lib() -> C.CDLL:
         L.kv_append_slots.restype = i32
         L.attend_chunk_workspace_bytes.argtypes = [GaugeShape] + [i32] * 9
         L.attend_chunk_workspace_bytes.restype = C.c_size_t
+        L.attend_chunk_workspace_limit.argtypes = [GaugeShape] + [i32] * 6
+        L.attend_chunk_workspace_limit.restype = C.c_size_t
         L.kv_attend_chunk_paged.argtypes = [i32, i32, C.POINTER(KvView), p, i32, i32, C.POINTER(CacheStruct),
                                             C.POINTER(CacheStruct), C.POINTER(PageTable), p, GaugeShape,
                                             C.POINTER(CodecStruct), p, C.c_float, i32, i32, C.POINTER(KvView), p, p, p]
@@ -545,7 +547,13 @@ def kv_append_slots(l0: int, l1: int, k_new, v_new, slots, G_dev, shp: GaugeShap
 
 def attend_chunk_workspace_bytes(shp: GaugeShape, nl: int, N: int, B: int, max_q: int, Hq: int, max_pages: int,
                                  page_size: int, window: int = 0, sinks: int = 0) -> int:
+    """Bytes of the kv_attend_chunk_paged call with exactly these arguments; fewer tokens or rows may need more."""
     return int(lib().attend_chunk_workspace_bytes(shp, nl, N, B, max_q, Hq, max_pages, page_size, window, sinks))
+
+
+def attend_chunk_workspace_limit(shp: GaugeShape, nl: int, N: int, B: int, Hq: int, max_pages: int, page_size: int) -> int:
+    """Bytes that every kv_attend_chunk_paged call of at most these sizes stays within: for a workspace kept across calls."""
+    return int(lib().attend_chunk_workspace_limit(shp, nl, N, B, Hq, max_pages, page_size))
 
 
 def kv_attend_chunk_paged(l0: int, l1: int, q, cu, max_q: int, kc: Cache, vc: Cache, pt: PageTable, G_dev,

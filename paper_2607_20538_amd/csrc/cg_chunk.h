@@ -36,6 +36,10 @@ struct ChunkPlan {
   int nsplit = 1;        // parts of a tile's positions
   size_t ws_bytes = 0;
 };
+// Rows of partial sums that the splits of a plan have at most (layers x splits x tokens x query heads): eight workgroups
+// of 128 for every CU.  Splits past that take less than 3% off the last round, at any length of the rows.
+inline int64_t chunk_part_rows() { return int64_t(8) * 32 * kChunkWaves * cu_count(); }
+constexpr int kChunkSplits = 64;  // parts at most, each of eight steps at least
 // singles: rows of one token have another kernel
 ChunkPlan chunk_plan(int nl, int N, int B, int max_q, int H, int Hq, int d, int cap, int window, int sinks, bool singles);
 // The kernels by rounded row width and result type

@@ -86,7 +86,7 @@ ChunkPlan chunk_plan(int nl, int N, int B, int max_q, int H, int Hq, int d, int 
                                                                                       : 0.5 * rows + 0.5));
   const double wgs = tiles * nl * H * p.nqc;
   double best = 0;
-  for (int ns = 1; ns <= 64 && (ns == 1 || ns * 8 <= steps); ++ns) {
+  for (int ns = 1; ns <= kChunkSplits && (ns == 1 || (ns * 8 <= steps && int64_t(nl) * N * Hq * ns <= chunk_part_rows())); ++ns) {
     const double w = wgs * ns / cu_count(), k = w <= 3 ? std::ceil(w) : w + 0.2;
     const double t = (k <= 1 ? 1.7 : 1.33 * k) * (double(steps) / ns + 6) + (ns > 1 ? 5 + double(nl) * N * Hq * d * 8 * ns / 4e6 : 0);
     if (ns == 1 || t < best) {

@@ -1108,6 +1108,19 @@ size_t attend_chunk_workspace_bytes(cg_gauge_shape shp, int32_t nl, int32_t N, i
   return ws;
 }
 
+// Every plan of at most these sizes: chunk_plan's splits end at chunk_part_rows and at eight steps each; singles_plan
+// splits while there are fewer than three workgroups per CU, so into less than six per CU, of at most eight heads.
+size_t attend_chunk_workspace_limit(cg_gauge_shape shp, int32_t nl, int32_t N, int32_t B, int32_t Hq, int32_t max_pages,
+                                    int32_t page_size) {
+  if (check_shape(shp) != CG_OK || check_chunk(nl, N, B, 1, Hq, max_pages, page_size, 0, 0, shp) != CG_OK || N == 0) return 0;
+  const int64_t cap = int64_t(max_pages) * page_size, steps = (cap + 63) / 64;
+  const int64_t parts = std::min<int64_t>(kChunkSplits, steps / 8), parts1 = std::min<int64_t>(3 * cu_count(), (cap + 255) / 256);
+  // (in binary64: products of sizes that no call could have do not overflow)
+  const double rows = parts > 1 ? std::min(double(nl) * N * Hq * parts, double(chunk_part_rows())) : 0.0;
+  const double rows1 = parts1 > 1 ? std::min(double(nl) * B * Hq * parts1, 6.0 * 8 * cu_count()) : 0.0;
+  return sizeof(float) * size_t(std::max(rows * (shp.d + 2), rows1 * (2 + 2 * shp.d)));
+}
+
 int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const int32_t* cu, int32_t B, int32_t max_q,
                               const cg_cache* kc, const cg_cache* vc, const cg_page_table* pages, const void* G_dev,
                               cg_gauge_shape shp, const cg_codec* codec, const int32_t* lens, float scale,

@@ -1,0 +1,45 @@
+"""A serving step's operators where calls follow one another: shared workspaces, pages that run out, precision of
+single tokens, long rows whose results do not average away."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_20538_amd import codec as cg
+
+import _serving as S
+from test_gpu_chunk import Case
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    cg.lib()
+
+
+def test_one_workspace_for_calls_of_any_size():
+    """A workspace of attend_chunk_workspace_limit bytes for the largest batch serves smaller ones, which split into
+    more parts: the results are those of workspaces of their own, and nothing behind it is written."""
+    cases = [Case(rows, H=8, grp=4, P=256, seed=k, spare_pages=40 - max(-(-(h + t) // 256) for h, t in rows))
+             for k, rows in enumerate(([(8000, 2000), (40, 1)], [(9000, 700)], [(9000, 40), (8000, 1)], [(9500, 1)], [(100, 1), (3, 70)]))]
+    N = max(c.N for c in cases)
+    limit = cg.attend_chunk_workspace_limit(cases[0].shp, 1, N, 2, 32, 40, 256)
+    buf = torch.full((limit + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+    sizes = []
+    for c in cases:
+        need = c.workspace()[1]
+        assert need <= limit
+        sizes.append(need)
+        c.call()
+        torch.cuda.synchronize()
+        want = c.out.clone()
+        c.base.fill_(7.0)
+        c.call(buf[:limit])
+        torch.cuda.synchronize()
+        assert torch.equal(c.out, want) and int(c.err.item()) == 0
+        assert (buf[limit:] == 0x5A).all()
+    assert max(sizes) > 0 and sizes[0] < max(sizes)

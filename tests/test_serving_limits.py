@@ -1,0 +1,43 @@
+"""Sizes of a serving step's workspaces, on the host."""
+import math
+import random
+
+import pytest
+
+from paper_2607_20538_amd import codec as cg
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+@pytest.mark.parametrize("H,grp,d,nl,N,B,maxp,P", [
+    (8, 4, 128, 1, 4096, 1, 400, 64), (8, 4, 128, 1, 4096, 64, 400, 64), (2, 2, 64, 4, 300, 7, 60, 64),
+    (16, 1, 256, 32, 20000, 300, 500, 256), (32, 40, 64, 8, 338, 26, 3696, 256), (1, 130, 128, 1, 5000, 600, 4000, 256),
+    (1, 3, 80, 2, 1, 1, 9, 192), (4, 9, 128, 1, 900, 900, 16, 64)])
+def test_workspace_limit_covers_every_smaller_call(H, grp, d, nl, N, B, maxp, P):
+    """The size of one call does not grow with its tokens (fewer are split into more parts), the limit covers them all."""
+    shp, rng = cg.shape(max(nl, 1), H, d, d), random.Random(N + d)
+    limit = cg.attend_chunk_workspace_limit(shp, nl, N, B, H * grp, maxp, P)
+    for k in range(3000):
+        n, b = (N if k % 3 == 0 else _log_int(rng, 1, N)), (B if k % 5 == 0 else _log_int(rng, 1, B))
+        mq = rng.choice([1, n, _log_int(rng, 1, n)])
+        window, sinks = rng.choice([(0, 0), (_log_int(rng, 1, 9000), rng.choice([0, 4, 3000]))])
+        need = cg.attend_chunk_workspace_bytes(shp, _log_int(rng, 1, nl), n, b, mq, H * grp, _log_int(rng, 1, maxp), P, window, sinks)
+        assert need <= limit, (n, b, mq, window, sinks)
+
+
+def test_workspace_of_one_call_is_not_a_limit():
+    shp = cg.shape(1, 8, 128, 128)
+    need = lambda n: cg.attend_chunk_workspace_bytes(shp, 1, n, 1, n, 32, 400, 64)  # noqa: E731
+    assert need(4096) == 0 < need(1024) < need(700)
+    limit = cg.attend_chunk_workspace_limit(shp, 1, 4096, 1, 32, 400, 64)
+    assert max(need(n) for n in range(1, 4097)) <= limit <= 2 ** 28
+
+
+def test_workspace_limit_of_nothing_and_of_bad_sizes():
+    shp = cg.shape(1, 8, 128, 128)
+    lim = lambda *a: cg.attend_chunk_workspace_limit(shp, *a)  # noqa: E731
+    assert lim(1, 4096, 1, 32, 4, 64) == 0                         # rows too short to split
+    assert lim(0, 1, 1, 32, 400, 64) == lim(1, 1, 1, 31, 400, 64) == lim(1, 1, 1, 32, 400, 63) == lim(1, 0, 1, 32, 400, 64) == 0
+    assert lim(2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 8, 400, 64) <= 2 ** 30
