@@ -400,7 +400,7 @@ int32_t kv_append_paged(int32_t l0, int32_t l1, const cg_kv_view* k_new, const c
  * and the pool's free_count.  N: packed tokens there is room for.  Rows past the table's
  * max_pages * P positions, negative lengths, and more than N tokens set CG_FLAG_POS_RANGE; a pool that
  * runs out sets CG_FLAG_POOL_EMPTY and leaves -1 in the table.  Tokens without a page get slot -1, a negative
- * add counts as 0, a row with a negative held takes no page.  page_size a multiple of 64;
+ * add counts as 0, a row with a negative held takes no page and none of its tokens gets a slot.  page_size a multiple of 64;
  * n_pages * page_size and max_pages * page_size below 2^31 (CG_ERR_CAPACITY).  Calls on one pool follow one
  * another (on one stream, or ordered by events).  Errors: CG_ERR_ARG, CG_ERR_SHAPE, CG_ERR_ALIGN,
  * CG_ERR_CAPACITY, CG_ERR_DEVICE. */

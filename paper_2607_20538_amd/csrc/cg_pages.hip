@@ -83,8 +83,11 @@ __device__ __forceinline__ void map_token(const MapArgs& a, const int* cu, int i
       if (cu[mid] <= i) lo = mid;
       else hi = mid;
     }
-    p = a.lens[lo] - (cu[lo + 1] - cu[lo]) + (i - cu[lo]);
-    const int lp = p >= 0 ? p / a.P : -1;
+    const int len = a.lens[lo], held = len - (cu[lo + 1] - cu[lo]);
+    p = held + (i - cu[lo]);
+    // (a row with a negative held has no page of its own, and a length that stuck at the largest does not say where the row's
+    // tokens go: whatever the table holds belongs to others)
+    const int lp = held >= 0 && len < 0x7fffffff ? p / a.P : -1;
     const int pg = lp >= 0 && lp < a.max_pages ? a.pages[size_t(lo) * a.max_pages + lp] : -1;
     if (pg >= 0 && pg < a.n_pages) slot = pg * a.P + (p - lp * a.P);
     else if (a.err) atomicOr(a.err, CG_FLAG_POS_RANGE);

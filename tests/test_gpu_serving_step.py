@@ -43,3 +43,18 @@ def test_one_workspace_for_calls_of_any_size():
         assert torch.equal(c.out, want) and int(c.err.item()) == 0
         assert (buf[limit:] == 0x5A).all()
     assert max(sizes) > 0 and sizes[0] < max(sizes)
+
+
+def test_tokens_of_a_row_with_a_negative_length_get_no_slot():
+    """Not even those whose position is not negative: what the row's table holds may be another row's page."""
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    for N in (12, 3000):                               # in the rows' launch, and in one of its own
+        pool = cg.PagePool(8)
+        pages = torch.tensor([[3, 4], [5, -1], [6, 7]], dtype=torch.int32, device="cuda")
+        cu, lens, pos, slots, err = i32([9] * 4), i32([9] * 3), i32([9] * N), i32([9] * N), i32([0])
+        cg.kv_page_map(i32([-3, 2, 2 ** 31 - 3]), i32([6, 2, 4]), pool, pages, 64, cu, lens, pos, slots, err)
+        torch.cuda.synchronize()
+        assert int(err.item()) & cg.CG_FLAG_POS_RANGE and cu.tolist() == [0, 6, 8, 12]
+        assert lens.tolist() == [3, 4, 2 ** 31 - 1] and pages.tolist() == [[3, 4], [5, -1], [6, 7]]
+        assert slots.tolist() == [-1] * 6 + [5 * 64 + 2, 5 * 64 + 3] + [-1] * (N - 8)
+        assert int(pool.count.item()) == 8
