@@ -219,7 +219,7 @@ hipError_t launch_page_map(const int* held, const int* add, int B, const cg_page
   hipLaunchKernelGGL(map_rows, dim3(1), dim3(kMapThreads), 0, st, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || N <= kOneLaunch) return e;
-  hipLaunchKernelGGL(map_tokens, dim3((N + 255) / 256), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(map_tokens, dim3(unsigned((int64_t(N) + 255) / 256)), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

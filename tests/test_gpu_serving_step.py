@@ -58,3 +58,16 @@ def test_tokens_of_a_row_with_a_negative_length_get_no_slot():
         assert lens.tolist() == [3, 4, 2 ** 31 - 1] and pages.tolist() == [[3, 4], [5, -1], [6, 7]]
         assert slots.tolist() == [-1] * 6 + [5 * 64 + 2, 5 * 64 + 3] + [-1] * (N - 8)
         assert int(pool.count.item()) == 8
+
+
+def test_page_map_with_room_for_the_most_tokens():
+    """N = 2^31 - 1: every entry of pos and slots is written, those behind the tokens as -1."""
+    N, i32 = 2 ** 31 - 1, lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    pool, pages = cg.PagePool(4), torch.full((2, 2), -1, dtype=torch.int32, device="cuda")
+    pos, slots = (torch.full((N,), 9, dtype=torch.int32, device="cuda") for _ in (0, 1))
+    cu, lens, err = i32([9] * 3), i32([9] * 2), i32([0])
+    cg.kv_page_map(i32([0, 0]), i32([2, 1]), pool, pages, 64, cu, lens, pos, slots, err)
+    torch.cuda.synchronize()
+    assert int(err.item()) == 0 and pages.tolist() == [[0, -1], [1, -1]] and int(pool.count.item()) == 2
+    assert pos[:3].tolist() == [0, 1, 0] and slots[:3].tolist() == [0, 1, 64]
+    assert all(bool((t[3:] == -1).all()) for t in (pos, slots))
