@@ -738,10 +738,18 @@ __device__ __forceinline__ bf16x8_t vfrag(const uint32_t (&lo)[8], const uint32_
 
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
 
 // bf16 pair (RN(a), RN(b)), a in the low half (the hardware conversion, round to nearest even)
 __device__ __forceinline__ uint32_t pk_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t{a, b}), bf16x2_t));
+}
+
+// what two bf16 planes of a pair leave, as a third
+__device__ __forceinline__ uint32_t third(float a, float b, uint32_t hi, uint32_t lo) {
+  return pk_bf16((a - __uint_as_float(hi << 16)) - __uint_as_float(lo << 16),
+                 (b - __uint_as_float(hi & 0xffff0000u)) - __uint_as_float(lo & 0xffff0000u));
 }
 
 // bf16 planes of v: hi = RN(v), lo = RN(v - hi)
@@ -813,11 +821,19 @@ __device__ __forceinline__ void gauge_query(const QueryRows& q, const GaugeDev& 
   }
 }
 
-template <int BITS, int NBLK, int TB, bool KIVI = false, bool PACK = false>
+// PL = 3: packed tokens with binary32 results.  Weights enter as three bf16 planes (24 bits), queries as two binary16 planes
+// (22 bits, scaled by a power of two; 8-bit codes: three bf16 ones), and the codes' middle C stays out of the sums:
+//   zhat = (mn + 2^(b-1) sc) + sc k (B - C),
+// B - C one packed subtraction for keys, for values a product with -C beside the one with B.  The sums stay near their
+// result then, while those of B grow with every channel and position.  24 rows of 30000 positions, 8 KV heads x 4, 4 bits:
+// error against binary64 9.2e-6 of the norm with two planes of both, 8.2e-6 with three, 1.1e-6 so (a plain binary32
+// evaluation: 1.8e-6); 181, 195 and 210 us.
+template <int BITS, int NBLK, int TB, bool KIVI = false, bool PACK = false, int PL = 2>
 __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a, GaugeDev G) {
   static_assert(TB == 1 || TB == 16, "token tiles of 16");
   static_assert(!KIVI || (TB == 1 && NBLK == 2), "KIVI: 32-position key groups, 64-channel value blocks");
   static_assert(!PACK || (TB == 1 && !KIVI), "packed tokens: per-token blocks");
+  static_assert(PL == 2 || (PL == 3 && PACK), "planes");
   constexpr bool RAW = TB > 1 || KIVI;         // raw bf16 positions after the quantised ones
   constexpr int JQ = 8 / NBLK;                 // query heads per workgroup (16 A rows)
   constexpr int NQL = 2 / NBLK;                // queries per D lane
@@ -826,6 +842,21 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
   constexpr float kSK = BITS == 8 ? 1.0f : (BITS == 6 ? 128.0f : float(1 << BITS));  // code_frag scale
   constexpr float kSV = BITS == 8 ? 1.0f : float(1 << BITS);                           // vfrag scale
   constexpr float kSK2 = BITS == 8 ? 1.0f : float(1 << BITS);                          // KIVI key scale
+  // PL = 3.  H16: code_frag's patterns read as binary16 are 1.875 + q kUnit, which one packed subtraction turns into
+  // (q - 2^(BITS - 1)) kUnit; the queries are then two binary16 planes (22 bits), scaled by a power of two per block.
+  constexpr bool H16 = PL == 3 && BITS != 8;
+  constexpr float kUnit = BITS == 6 ? 1.0f / 1024 : 1.0f / (8 << BITS), kHalf = float(1 << (BITS - 1));
+  auto centred = [](bf16x8_t x) {
+    u32x4_t v = __builtin_bit_cast(u32x4_t, x);
+    constexpr _Float16 c = (_Float16)(1.875f + kHalf * kUnit);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2_t, uint32_t(v[i])) - f16x2_t{c, c});
+    return __builtin_bit_cast(f16x8_t, v);
+  };
+  // -C as an operand: C = the middle of B (8 bits: of the codes themselves)
+  const uint32_t mid = BITS == 8 ? 0xC300C300u : 0xBFC0BFC0u;
+  const bf16x8_t MID = as_bf16x8(u32x4_t{mid, mid, mid, mid});
+  __shared__ int qexp[H16 ? JQ : 1][NBLK];  // exponent of a block's largest |qt|
   __shared__ __attribute__((aligned(16))) float qt[JQ][kD];
   __shared__ __attribute__((aligned(16))) float macc[JQ][kD];
   __shared__ float qsum[JQ][NBLK];
@@ -887,7 +918,7 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
   const int tq = KIVI ? (held < a.win ? 0 : (held - a.win) / 32 * 32) : (TB > 1 ? held / TB * TB : held);
   const int t_endq = min(t_end, tq);
 
-  // 1. queries: macc <- q, qt <- scale G_K q, qsum <- the per-block sums of its two planes
+  // 1. queries: macc <- q, qt <- scale G_K q, qsum <- the per-block sums of its planes
   QueryRows qrows;
   load_query_rows(qrows, G, l, h);
   for (int idx = threadIdx.x; idx < JQ * kD; idx += kAThreads) {
@@ -907,23 +938,34 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
     constexpr int GL = kAThreads / (JQ * NBLK), CPL = NB / GL;
     static_assert((GL == 32 || GL == 16) && CPL % 2 == 0, "lanes per (query, block)");
     const int pr = threadIdx.x / GL, jj = pr / NBLK, k = pr % NBLK, c0 = k * NB + (threadIdx.x % GL) * CPL;
-    float acc = 0.0f;
+    float acc = 0.0f, most = 0.0f;
 #pragma unroll
     for (int c = 0; c < CPL; c += 2) {
       const float x0 = qt[jj][c0 + c], x1 = qt[jj][c0 + c + 1];
+      if constexpr (PL == 3) {
+        acc += x0 + x1;
+        most = fmaxf(most, fmaxf(fabsf(x0), fabsf(x1)));
+        continue;
+      }
       const uint32_t hi = pk_bf16(x0, x1);
       const float h0 = __uint_as_float(hi << 16), h1 = __uint_as_float(hi & 0xffff0000u);
       const uint32_t lo = pk_bf16(x0 - h0, x1 - h1);
       acc += (h0 + __uint_as_float(lo << 16)) + (h1 + __uint_as_float(lo & 0xffff0000u));
     }
 #pragma unroll
-    for (int o = 1; o < GL; o <<= 1) acc += __shfl_xor(acc, o);
-    if (threadIdx.x % GL == 0) qsum[jj][k] = acc;
+    for (int o = 1; o < GL; o <<= 1) {
+      acc += __shfl_xor(acc, o);
+      if constexpr (H16) most = fmaxf(most, __shfl_xor(most, o));
+    }
+    if (threadIdx.x % GL == 0) {
+      qsum[jj][k] = acc;
+      if constexpr (H16) qexp[jj][k] = most > 0.0f && most < INFINITY ? __builtin_amdgcn_frexp_expf(most) : 0;
+    }
   }
   __syncthreads();
 
   // 2. score A fragments: row m = n -> (query, block, plane), region 32 gq
-  bf16x8_t AK[4];
+  bf16x8_t AK[4], AK3[PL == 3 && !H16 ? 4 : 1];  // (the third plane: in the rows of the first, the others zero)
   if constexpr (!KIVI) {
     const int j = n / (2 * NBLK), blk = (n / 2) % NBLK, plane = n & 1;
     const bool own = 32 * gq / NB == blk;  // the region lies in one block
@@ -934,17 +976,40 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
       constexpr int RUN = BITS == 2 || BITS == 3 ? 8 : 4;  // distance of the runs
       const float4 r0 = *reinterpret_cast<const float4*>(src), r1 = *reinterpret_cast<const float4*>(src + RUN);
       const float x0[4] = {r0.x, r0.y, r0.z, r0.w}, x1[4] = {r1.x, r1.y, r1.z, r1.w};
-      u32x4_t f;
+      u32x4_t f, f3;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float c0 = BITS == 8 ? (i < 2 ? x0[2 * i] : x1[2 * i - 4]) : x0[i];
         const float c1 = BITS == 8 ? (i < 2 ? x0[2 * i + 1] : x1[2 * i - 3]) : x1[i];
+        if constexpr (H16) {
+          const int up = 15 - qexp[j][blk];  // the largest to [2^14, 2^15)
+          const f32x2_t x = {__builtin_amdgcn_ldexpf(c0, up), __builtin_amdgcn_ldexpf(c1, up)};
+          const f16x2_t hi = __builtin_convertvector(x, f16x2_t);
+          const f16x2_t lo = __builtin_convertvector((f32x2_t{x[0] - (float)hi[0], x[1] - (float)hi[1]}), f16x2_t);
+          f[i] = own ? __builtin_bit_cast(uint32_t, plane ? lo : hi) : 0u;
+          continue;
+        }
         const uint32_t hi = pk_bf16(c0, c1);
         const uint32_t lo = pk_bf16(c0 - __uint_as_float(hi << 16), c1 - __uint_as_float(hi & 0xffff0000u));
         f[i] = own ? (plane ? lo : hi) : 0u;
+        if constexpr (PL == 3) f3[i] = own && !plane ? third(c0, c1, hi, lo) : 0u;
       }
       AK[u] = as_bf16x8(f);
+      if constexpr (PL == 3 && !H16) AK3[u] = as_bf16x8(f3);
     }
+  }
+  f32x4_t dmid = {0.0f, 0.0f, 0.0f, 0.0f};  // PL = 3, 8 bits: what the scores' sums start from
+  if constexpr (PL == 3 && !H16) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      dmid = mfma16(AK[u], MID, dmid);
+      dmid = mfma16(AK3[u], MID, dmid);
+    }
+  }
+  float gfac[2];  // H16: what takes the rows' scale back, by block, or (NBLK = 1) by query
+  if constexpr (H16) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) gfac[k] = __builtin_amdgcn_ldexpf(1.0f / kUnit, (NBLK == 2 ? qexp[gq][k] : qexp[2 * gq + k][0]) - 15);
   }
   // the D rows of this lane: 4 gq + i -> query jr[i], block br[i], plane i & 1
   float qrow[4];
@@ -1151,15 +1216,27 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
     } else {
 #pragma unroll
     for (int sb = 0; sb < 2; ++sb) {
-      f32x4_t d = {0.0f, 0.0f, 0.0f, 0.0f};
+      f32x4_t d = dmid;
 #pragma unroll
-      for (int u = 0; u < 4; ++u) d = mfma16(AK[u], code_frag<BITS, BITS>(rk[sb], u, one, fmask), d);
+      for (int u = 0; u < 4; ++u) {
+        const bf16x8_t x = code_frag<BITS, BITS>(rk[sb], u, one, fmask);
+        if constexpr (H16) {
+          d = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8_t, AK[u]), centred(x), d, 0, 0, 0);
+          continue;
+        }
+        d = mfma16(AK[u], x, d);
+        if constexpr (PL == 3) d = mfma16(AK3[u], x, d);
+      }
       float gam[NBLK], bet[NBLK];
 #pragma unroll
       for (int k = 0; k < NBLK; ++k) {
         const float mn = f16_bits_to_f32(swk[sb][k] & 0xffffu), sc = f16_bits_to_f32(swk[sb][k] >> 16);
-        gam[k] = kSK * sc;
-        bet[k] = BITS == 8 ? mn : mn - gam[k];
+        gam[k] = H16 ? sc : kSK * sc;
+        bet[k] = PL == 3 ? fmaf(kHalf, sc, mn) : (BITS == 8 ? mn : mn - gam[k]);
+      }
+      if constexpr (H16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] *= gfac[i >> 1];
       }
       const bool valid = shown(16 * sb + n);
       if constexpr (NBLK == 2) {
@@ -1201,7 +1278,7 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
     }
     // value A fragment: w = kSV p sc of tokens 8 gq .. 8 gq + 7 for row (jw, bw, pw), split
     // into bf16 planes by the hardware conversion (round to nearest even)
-    bf16x8_t AV;
+    bf16x8_t AV, AV3;
     {
       const float4 pa = *reinterpret_cast<const float4*>(&pbuf[w][jw][8 * gq]);
       const float4 pb = *reinterpret_cast<const float4*>(&pbuf[w][jw][8 * gq + 4]);
@@ -1210,7 +1287,7 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
       const float pe[8] = {pa.x, pa.y, pa.z, pa.w, pb.x, pb.y, pb.z, pb.w};
       const uint32_t se[8] = {sa.x, sa.y, sa.z, sa.w, sb4.x, sb4.y, sb4.z, sb4.w};
       float o = offl * abuf[w][jw];
-      u32x4_t f;
+      u32x4_t f, f3;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float x0 = kSV * f16_bits_to_f32(se[2 * i] >> 16) * pe[2 * i];
@@ -1220,6 +1297,14 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
         const uint32_t lo = pk_bf16(x0 - h0, x1 - h1);
         f[i] = pw ? lo : hi;
         const float mn0 = f16_bits_to_f32(se[2 * i] & 0xffffu), mn1 = f16_bits_to_f32(se[2 * i + 1] & 0xffffu);
+        if constexpr (PL == 3) {
+          f3[i] = pw ? 0u : third(x0, x1, hi, lo);
+          if (pw == 0) {
+            o = fmaf(pe[2 * i], fmaf(kHalf, f16_bits_to_f32(se[2 * i] >> 16), mn0), o);
+            o = fmaf(pe[2 * i + 1], fmaf(kHalf, f16_bits_to_f32(se[2 * i + 1] >> 16), mn1), o);
+          }
+          continue;
+        }
         if (pw == 0) {
           o = BITS == 8 ? fmaf(pe[2 * i], mn0, o) : fmaf(pe[2 * i], mn0, o - h0);
           o = BITS == 8 ? fmaf(pe[2 * i + 1], mn1, o) : fmaf(pe[2 * i + 1], mn1, o - h1);
@@ -1229,12 +1314,21 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
       }
       offl = o;
       AV = as_bf16x8(f);
+      if constexpr (PL == 3) AV3 = as_bf16x8(f3);
     }
     uint32_t vlo[8], vhi[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) vchunk<BITS>(vw0[e], vw1[e], vsh, vlo[e], vhi[e]);
 #pragma unroll
-    for (int nt = 0; nt < 8; ++nt) accV[nt] = mfma16(AV, vfrag<BITS>(vlo, vhi, nt, one), accV[nt]);
+    for (int nt = 0; nt < 8; ++nt) {
+      const bf16x8_t x = vfrag<BITS>(vlo, vhi, nt, one);
+      if constexpr (PL == 3) {
+        accV[nt] = mfma16(AV, MID, accV[nt]);
+        accV[nt] = mfma16(AV3, MID, accV[nt]);
+      }
+      accV[nt] = mfma16(AV, x, accV[nt]);
+      if constexpr (PL == 3) accV[nt] = mfma16(AV3, x, accV[nt]);
+    }
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
     __builtin_amdgcn_wave_barrier();
   };
@@ -1514,21 +1608,27 @@ __global__ __launch_bounds__(kAThreads, KIVI ? 3 : 2) void att_mfma(AttendDev a,
   }
 }
 
+template <int BITS, int NBLK>
+const void* att_mfma_pack_fn(bool f32) {
+  return f32 ? (const void*)att_mfma<BITS, NBLK, 1, false, true, 3> : (const void*)att_mfma<BITS, NBLK, 1, false, true>;
+}
+
 template <int BITS>
-const void* att_mfma_fn(int nblk, int bt, bool kivi, bool pack) {
-  if (pack) return nblk == 2 ? (const void*)att_mfma<BITS, 2, 1, false, true> : (const void*)att_mfma<BITS, 1, 1, false, true>;
+const void* att_mfma_fn(int nblk, int bt, bool kivi, bool pack, bool f32) {
+  if (pack) return nblk == 2 ? att_mfma_pack_fn<BITS, 2>(f32) : att_mfma_pack_fn<BITS, 1>(f32);
   if (kivi) return (const void*)att_mfma<BITS, 2, 1, true>;
   if (bt > 1) return nblk == 2 ? (const void*)att_mfma<BITS, 2, 16> : (const void*)att_mfma<BITS, 1, 16>;
   return nblk == 2 ? (const void*)att_mfma<BITS, 2, 1> : (const void*)att_mfma<BITS, 1, 1>;
 }
 
-const void* att_mfma_kernel(int bits, int nblk, int bt, bool kivi, bool pack) {
+// f32: binary32 results (of packed tokens)
+const void* att_mfma_kernel(int bits, int nblk, int bt, bool kivi, bool pack, bool f32) {
   switch (bits) {
-    case 2: return att_mfma_fn<2>(nblk, bt, kivi, pack);
-    case 3: return att_mfma_fn<3>(nblk, bt, kivi, pack);
-    case 4: return att_mfma_fn<4>(nblk, bt, kivi, pack);
-    case 6: return att_mfma_fn<6>(nblk, bt, kivi, pack);
-    default: return att_mfma_fn<8>(nblk, bt, kivi, pack);
+    case 2: return att_mfma_fn<2>(nblk, bt, kivi, pack, f32);
+    case 3: return att_mfma_fn<3>(nblk, bt, kivi, pack, f32);
+    case 4: return att_mfma_fn<4>(nblk, bt, kivi, pack, f32);
+    case 6: return att_mfma_fn<6>(nblk, bt, kivi, pack, f32);
+    default: return att_mfma_fn<8>(nblk, bt, kivi, pack, f32);
   }
 }
 
@@ -1586,7 +1686,7 @@ hipError_t launch_attend(const AttendDev& args_in, const GaugeDev& G, const Code
     const int nrow_f = a.q.L * B * a.kc.H * af.nqc;
     GaugeDev g2 = G;
     void* args[] = {&af, &g2};
-    e = hipLaunchKernel(att_mfma_kernel(c.bits, nblk, c.bt, kivi, pack), pack ? dim3(unsigned(nrow_f) * a.nsplit) : dim3(a.nsplit, nrow_f),
+    e = hipLaunchKernel(att_mfma_kernel(c.bits, nblk, c.bt, kivi, pack, !a.o.bf16), pack ? dim3(unsigned(nrow_f) * a.nsplit) : dim3(a.nsplit, nrow_f),
                         dim3(kAThreads), args, 0, st);
     if (e != hipSuccess) return e;
   } else {

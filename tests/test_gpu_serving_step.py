@@ -71,3 +71,53 @@ def test_page_map_with_room_for_the_most_tokens():
     assert int(err.item()) == 0 and pages.tolist() == [[0, -1], [1, -1]] and int(pool.count.item()) == 2
     assert pos[:3].tolist() == [0, 1, 0] and slots[:3].tolist() == [0, 1, 64]
     assert all(bool((t[3:] == -1).all()) for t in (pos, slots))
+
+
+@pytest.mark.parametrize("bits,n", [(2, 64), (3, 64), (4, 64), (6, 64), (8, 64), (3, 128), (4, 128), (8, 128), (4, 32)])
+@pytest.mark.parametrize("new", [1, 2])
+def test_binary32_results_hold_22_bits(bits, n, new):
+    """Two positions whose scores of about 60 lie within 3 of each other, one key in channel 5, the other in channel 77, and
+    opposite values: o = v tanh(D / 2), D the scores' difference.  A query's two channels are all that counts.
+
+    Bound: with A the larger score and operands of 22 bits (2^-22 of a value at most) the two products of a score are off by
+    2^-22 A together (of a code's distance from the middle, the other channel's part included), scale and
+    query by two binary32 roundings (2^-23 A), the products' sum, block offset, and their sum by four (2^-22 A): 2.5 2^-22 A
+    per score, E = 5 2^-22 A for D.  tanh(D / 2) moves by E / 2 at most; weights, their sum, the division, the values'
+    operands and sums: eight roundings of 2^-22 of |v|.  Operands of 16 bits are off by up to 2^-16 A and 2^-18 A at the
+    median, far past it in some of the 4 x 24 queries."""
+    rows = [(2 - new, new)] * 24
+    c = Case(rows, H=1, grp=4, bits=bits, n=n, g=128, dtype=torch.float32, pad=0, spare_pages=0, scale=0.25, seed=bits + n)
+    c.G = np.eye(128, dtype=np.float32).reshape(1, 1, 1, 1, 128, 128).repeat(2, axis=1)
+    c.shp, c.Gd = S.gauge_dev(c.G)
+    top, rng = 2 ** bits - 1, np.random.default_rng(7)
+    scale_h = np.float16(120.0 / top)
+    q = np.zeros((1, c.N, 4, 128), np.float32)
+    x = rng.uniform(1.9, 2.0, (c.N, 4)).astype(np.float32)
+    q[0, :, :, 5], q[0, :, :, 77] = x, x * rng.uniform(0.96, 1.04, x.shape).astype(np.float32)
+    c.q = torch.from_numpy(q).permute(c.perm)
+    c.qd = torch.from_numpy(q).cuda().permute(c.perm).unsqueeze(1)
+    codes = [np.zeros((1, c.kc.B, 1, 64, 128), np.uint8) for _ in (0, 1)]
+    codes[0][..., 0, 5] = codes[0][..., 1, 77] = top
+    codes[1][..., 0, :] = rng.integers(0, 2, 128) * top
+    codes[1][..., 1, :] = top - codes[1][..., 0, :]
+    weights = 1 << np.arange(bits)
+    for s in (0, 1):
+        b = ((codes[s][..., None] & weights) > 0).astype(np.uint8).reshape(1, c.kc.B, 1, 64, -1)
+        c.pools[s][0] = np.packbits(b, axis=-1, bitorder="little")
+        c.pools[s][1][..., 0] = 0.0 if s == 0 else np.float16(-0.5)
+        c.pools[s][1][..., 1] = scale_h if s == 0 else np.float16(1.0 / 2 ** bits)
+    c.upload()
+    c.call()
+    torch.cuda.synchronize()
+    assert int(c.err.item()) == 0
+    zk, zv = (S.pool_values(c.codec, *p)[0, 0, 0] for p in c.pools)
+    assert zk[0, 5] == zk[1, 77] == top * float(scale_h) and np.count_nonzero(zk[:2]) == 2
+    qd = torch.from_numpy(q[0]).double()[new - 1::new]                     # a row's last token sees both
+    got = c.out[0, 0].double().cpu().transpose(0, 1)[new - 1::new]
+    sc = c.scale * qd @ torch.from_numpy(zk[:2]).T
+    want = torch.softmax(sc, -1) @ torch.from_numpy(zv[:2])
+    A, v = sc.max(-1).values, float(np.abs(zv[:2]).max())
+    assert 50 < float(A.min()) and float((sc[..., 0] - sc[..., 1]).abs().max()) < 3
+    err = (got - want).abs().amax(-1)
+    lim = (2.5 * 2.0 ** -22 * A + 8 * 2.0 ** -22) * v
+    assert (err <= lim).all(), float((err / lim).max())
