@@ -14,7 +14,7 @@
 //                                                                   swap of the halves per step
 //   O^T += V^T P^T (the lane's own probabilities are its B operand: the order of the contraction is free, so
 //                   V is read in the order that S^T left the positions in, by transposing LDS reads)
-// Binary16 and not bf16: codes are exact in both, zhat, q' (scaled by a power of two to at most 1) and p then
+// Binary16 and not bf16: codes are exact in both, zhat, q' (scaled by a power of two to at most 2^15) and p then
 // carry 11 bits, four times finer than the result's own rounding.  Binary32 results take every operand in
 // two binary16 planes (22 bits, three products).  zhat beyond binary16 (the side information allows 2^24),
 // infinities and NaN make a step "odd": it is summed position by position in binary32, where a masked
@@ -598,14 +598,15 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
     mx = halves_max(mx);
     const int ex = mx > 0.0f && mx < INFINITY ? __builtin_amdgcn_frexp_expf(mx) : 0;
     const float sign = a.scale < 0.0f ? -1.0f : (a.scale > 0.0f ? 1.0f : 0.0f);
-    cs = a.scale == 0.0f ? 1.0f : fmaxf(__builtin_amdgcn_ldexpf(fabsf(a.scale) * kLog2e, ex), 1e-37f);  // (not 0: 0 times a hidden score)
+    // the largest to [2^14, 2^15), as binary16's least step would otherwise take bits from the small ones
+    cs = a.scale == 0.0f ? 1.0f : fmaxf(__builtin_amdgcn_ldexpf(fabsf(a.scale) * kLog2e, ex - 15), 1e-37f);  // (not 0: 0 times a hidden score)
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) {
       u32x4_t hi, lo;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float x0 = sign * __builtin_amdgcn_ldexpf(z[kk >> 1][8 * (kk & 1) + j], -ex);
-        const float x1 = sign * __builtin_amdgcn_ldexpf(z[kk >> 1][8 * (kk & 1) + 4 + j], -ex);
+        const float x0 = sign * __builtin_amdgcn_ldexpf(z[kk >> 1][8 * (kk & 1) + j], 15 - ex);
+        const float x1 = sign * __builtin_amdgcn_ldexpf(z[kk >> 1][8 * (kk & 1) + 4 + j], 15 - ex);
         hi[j] = pk_h(x0, x1);
         lo[j] = pk_h(x0 - h_lo(hi[j]), x1 - h_hi(hi[j]));
       }

@@ -121,3 +121,67 @@ def test_binary32_results_hold_22_bits(bits, n, new):
     err = (got - want).abs().amax(-1)
     lim = (2.5 * 2.0 ** -22 * A + 8 * 2.0 ** -22) * v
     assert (err <= lim).all(), float((err / lim).max())
+
+
+class Plain(Case):
+    """A case whose gauge is the identity, keys, values and queries set channel by channel."""
+
+    def set(self, q=None, k=None, v=None):
+        """q [N][Hq][d]; k, v [pages][64][d] of the error-free pools' (one layer and head)."""
+        d = self.d
+        self.G = np.eye(d, dtype=np.float32).reshape(1, 1, 1, 1, d, d).repeat(2, axis=1)
+        self.shp, self.Gd = S.gauge_dev(self.G)
+        if q is not None:
+            self.q = torch.from_numpy(q.astype(np.float32))[None].to(self.q.dtype).permute(self.perm)
+            self.qd = self.q.permute(self.perm).contiguous().cuda().permute(self.perm).unsqueeze(1)
+        for s, x in enumerate((k, v)):
+            if x is not None:
+                self.pools[s][0] = np.ascontiguousarray(x[None, :, None].astype(np.float32)).view(np.uint8)
+        self.upload()
+        return self
+
+    def results(self):
+        """(got, zk, zv) of the one row: outputs [Hq][new][d], positions' keys and values, in binary64."""
+        self.call()
+        torch.cuda.synchronize()
+        assert int(self.err.item()) == 0
+        n = self.held[0]
+        zk, zv = (torch.from_numpy(S.pool_values(self.codec, *p)[0, self.table[0][: -(-n // 64)], 0].reshape(-1, self.d)[:n])
+                  for p in self.pools)
+        return self.out[0, 0].double().cpu()[:, : self.rows[0][1]], zk, zv
+
+
+def _weights_bound(got, q, zk, zv, scale, unit, floor, planes, step):
+    """got [Hq][new][d] against softmax over all positions a token sees; a score is off by A (2 unit + 2^-21) plus `floor`
+    (of the queries' sum) where A = |scale| sum |q k|, a weight by a factor within exp(+-2 E) and 2 unit, weights and values by 2 unit more, sums over n positions by n 2^-24 and their planes for the gauge by
+    `planes`; all of it relative to the largest |v|."""
+    n, new = zk.shape[0], got.shape[1]
+    for j in range(got.shape[0]):
+        for i in range(new):
+            m = n - new + 1 + i
+            s = scale * zk[:m] @ q[j, i]
+            want = torch.softmax(s, 0) @ zv[:m]
+            E = abs(scale) * (float((zk[:m].abs() @ q[j, i].abs()).max()) * (2 * unit + 2.0 ** -21) + floor * float(q[j, i].abs().sum()))
+            lim = (math.expm1(2 * E) + 2 * unit + n * 2.0 ** -24 + planes) * float(zv.abs().max()) + step * want.abs()
+            assert E < 0.05 and ((got[j, i] - want).abs() <= lim).all(), (E, float(((got[j, i] - want).abs() / lim).max()))
+
+
+@pytest.mark.parametrize("bits,n,d", [(4, 32, 128), (4, 16, 128), (4, 64, 256), (8, 32, 64)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_queries_of_small_channels(bits, n, d, dtype):
+    """What tells the positions apart lies in a block of large keys, where the query is 2e-6 of its largest channel; there
+    the keys are nought.  Queries keep their bits down to 2^-29 (two planes: 2^-18, and 2^-40 beyond) of the largest."""
+    T, new, rng = 200, 3, np.random.default_rng(d + n)
+    c = Plain([(T - new, new)], H=1, grp=2, d=d, g=d, bits=bits, n=n, dtype=dtype, scale=40.0)
+    side = c.pools[0][1]
+    side[...] = 0.0
+    side[..., 1, 1] = np.float16(60000.0 / (2 ** bits - 1))
+    q = np.zeros((c.N, 2, d))
+    q[..., 0] = 1.0
+    q[..., n: 2 * n] = 2e-6 / n * rng.uniform(0.5, 1.0, q[..., n: 2 * n].shape)
+    c.set(q)
+    got, zk, zv = c.results()
+    bf = dtype == torch.bfloat16
+    floor = 0.0 if bf else 2.0 ** -40 * n * float(zk.max())       # of the largest query, 1
+    _weights_bound(got, c.q[0, :, :new].double(), zk, zv, 40.0, 2.0 ** -11 if bf else 2.0 ** -22, floor, 2.0 ** -15 if bf else 2.0 ** -22,
+                   2.0 ** -8 if bf else 2.0 ** -24)
