@@ -463,7 +463,8 @@ size_t attend_chunk_workspace_limit(cg_gauge_shape shp, int32_t nl, int32_t N, i
  *                                       window == 0 or t > p - window or t < sinks,
  * Khat, Vhat as kv_decode would return them in binary32.  The first `sinks` positions stay visible behind the
  * window; window = 0: causal (sinks unused).  bf16 outputs are computed from operands of 11 bits (binary16;
- * rows of one token: of 16 bits or more) with binary32 sums, binary32 outputs from operands of 22 bits.  out must not overlap q.  Positions a token does not see do not reach its
+ * rows of one token: of 16 bits or more) with binary32 sums, binary32 outputs from operands of 22 bits (error-free pools: below
+ * 2^-18 of a step's largest value to within 2^-40 of it).  out must not overlap q.  Positions a token does not see do not reach its
  * output, whatever their bytes decode to; a NaN or infinity that it does see makes it NaN.  Tokens behind the
  * last row are left as they were.  A row whose lens is below n_b or above max_pages * page_size sets
  * CG_FLAG_POS_RANGE and gets zeros; a row whose cu runs backwards, past N or over max_q sets it and is left as it

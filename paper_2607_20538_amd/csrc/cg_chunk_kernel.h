@@ -16,9 +16,12 @@
 //                   V is read in the order that S^T left the positions in, by transposing LDS reads)
 // Binary16 and not bf16: codes are exact in both, zhat, q' (scaled by a power of two to at most 2^15) and p then
 // carry 11 bits, four times finer than the result's own rounding.  Binary32 results take every operand in
-// two binary16 planes (22 bits, three products).  zhat beyond binary16 (the side information allows 2^24),
-// infinities and NaN make a step "odd": it is summed position by position in binary32, where a masked
-// position is left out instead of being multiplied by zero.
+// two binary16 planes (22 bits, three products).  A block's zhat are multiples of 2^-24, binary16's own least step, so
+// none is lost below its normal range; the error-free backend's are scaled by a power of two, keys by the largest of
+// their step, values by the largest so far, to at most 2^15: binary16 then holds 11 bits down to 2^-29 of it, two planes 22
+// bits down to 2^-18 and 2^-40 of it below.  zhat beyond binary16 (the side information allows 2^24), infinities, NaN, and
+// error-free values below 2^-29 of the largest make a step "odd": it is summed position by position in binary32, where a
+// masked position is left out instead of being multiplied by zero.
 //
 // Bound by the vector work of decoding and of the exponentials beside the products, which overlap in part (vector
 // units busy 50% of the time, matrix cores 34%, two waves per SIMD).  4096 tokens at the end of 20000 positions, 8 KV
@@ -194,9 +197,11 @@ __device__ __forceinline__ f16x2_t int_pair(uint32_t p) {
   return __builtin_bit_cast(f16x2_t, p) - k;
 }
 
-// Four neighbouring channels c .. c + 3 (c a multiple of 4, < d) of a cached position in binary32
+// Four neighbouring channels c .. c + 3 (c a multiple of 4, < d) of a cached position in binary32 (PASS: the error-free
+// backend)
+template <bool PASS>
 __device__ __forceinline__ void load4(const CacheDev& k, const CodecDev& c, size_t row, int d, int ch, float (&out)[4]) {
-  if (c.backend == CG_BACKEND_PASSTHROUGH) {
+  if constexpr (PASS) {
     const float4 v = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(k.codes) + row * d + ch);
     out[0] = v.x; out[1] = v.y; out[2] = v.z; out[3] = v.w;
     return;
@@ -218,10 +223,10 @@ __device__ __forceinline__ void load4(const CacheDev& k, const CodecDev& c, size
 // x 4, d = 128, n = 32, up to 8000 positions: 463 us with one wave, 297 with two, 146 with four.
 constexpr int NW = kChunkWaves;
 // BITS: the code width of rows that decode in whole runs (chunk_wide; 0: any width, read at run time), or
-// kAnyLayout: any block and row width and the error-free backend, four channels at a time.  A width known to the
+// kAnyLayout: any block and row width, or kErrorFree: the error-free backend, four channels at a time.  A width known to the
 // compiler took 2088 -> 1850 us (4096 tokens at 20000 positions, 4 bits): the branches over widths, twice a step, and
 // the registers of all of them.
-constexpr int kAnyLayout = -1;
+constexpr int kAnyLayout = -1, kErrorFree = -2;
 constexpr int kFillOps = 11;  // vector instructions of the next step's codes beside each product of the scores
 
 template <int D, int PL>
@@ -231,21 +236,21 @@ struct ChunkShape {
   static constexpr int plane = kStep * (KP + VP);
   static constexpr int buffers = PL == 1 && D <= 128 ? 2 : 1;
   static constexpr int bytes = plane * PL * buffers;
-  static constexpr int all = bytes + 64;                         // with the waves' flags
+  static constexpr int all = bytes + 128;                        // with the waves' flags and maxima
   static_assert(VP % 64 == 0 && kStep * KP % 64 == 0, "V runs on multiples of 64 bytes");
 };
 
 template <int D, int PL, int BITS>
 __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_attend(ChunkDev a, GaugeDev G, CodecDev c) {
   using SH = ChunkShape<D, PL>;
-  constexpr bool WIDE = BITS != kAnyLayout;
+  constexpr bool WIDE = BITS >= 0, PASS = BITS == kErrorFree;
   const int bits = BITS > 0 ? BITS : c.bits;
   constexpr int NT = 64 * NW, KK = D / 16, CT = D / 32, RUNS = D / 32;
   constexpr int ITEMS = 2 * kStep * RUNS, IT = (ITEMS + NT - 1) / NT;  // (position, run) of K, then of V
   static_assert(ITEMS % NT == 0, "items per thread");
   extern __shared__ __attribute__((aligned(64))) uint8_t sm[];
-  uint32_t(*state)[NW] = reinterpret_cast<uint32_t(*)[NW]>(sm + SH::bytes);  // per step parity and wave: what its items hold (kOver ...)
-  constexpr uint32_t kOver = 1, kBigK = 2, kBigV = 4, kAnyK = 8, kAnyV = 16;
+  uint32_t(*state)[NW] = reinterpret_cast<uint32_t(*)[NW]>(sm + SH::bytes);  // per step parity and wave: whether its items make the step odd
+  float(*most)[2][NW] = reinterpret_cast<float(*)[2][NW]>(sm + SH::bytes + 32);  // PASS: the largest of its keys, of its values
 
   const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, hc = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -301,7 +306,8 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
   Raw32 raw[AHEAD ? IT : 1] = {};
   size_t srow = 0;       // cache row of the step's first position
   bool have = false;     // the step's page is inside the pool
-  const bool pass = !WIDE && c.backend == CG_BACKEND_PASSTHROUGH;
+  constexpr bool KEEP = PASS && IT <= 2;
+  int up[2] = {0, 200};  // PASS: exponents that the step's keys and the values so far are scaled by (200: no values yet)
   const int words = d * bits / 32, nblk = WIDE ? d / c.n : 1;  // words and side words of a row
   auto item = [&](int i, bool& val, int& pos, int& run) {
     // the same side for a whole wave
@@ -404,7 +410,66 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
   };
   auto decode = [&](int v, auto out) {
     const int t0 = step_pos(v);
-    uint32_t st = 0;
+    bool st = false;  // zhat that binary16 does not hold
+    float zp[KEEP ? IT : 1][8][4];  // PASS: this thread's values
+    if constexpr (PASS) {
+      // the largest finite magnitudes of the step first, its values kept where registers last (32 single tokens of up
+      // to 8000 positions, 8 KV heads x 4, bf16 results: d = 128 594 us kept, 997 read twice; d = 256 3283 and 2551)
+      float mx[2] = {0.0f, 0.0f};
+      auto largest = [&](const float (&z)[8][4], bool val) {
+        float m = 0.0f;
+#pragma unroll
+        for (int g = 0; g < 8; ++g)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float x = fabsf(z[g][e]);
+            if (x < INFINITY) m = fmaxf(m, x);
+            else st = true;
+          }
+        (val ? mx[1] : mx[0]) = fmaxf(val ? mx[1] : mx[0], m);
+      };
+      auto read = [&](float (&z)[8][4], int i, bool& val) {
+        int pos, run;
+        item(i, val, pos, run);
+        const bool live = have && t0 + pos < held;
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+          const int ch = 32 * run + 4 * g;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) z[g][e] = 0.0f;
+          if (live && ch < d) load4<PASS>(val ? a.vc : a.kc, c, srow + pos, d, ch, z[g]);
+        }
+      };
+      if constexpr (KEEP) {
+        bool side[IT];
+#pragma unroll
+        for (int i = 0; i < IT; ++i) read(zp[i], i, side[i]);
+#pragma unroll
+        for (int i = 0; i < IT; ++i) largest(zp[i], side[i]);
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < IT; ++i) {
+          bool val;
+          read(zp[0], i, val);
+          largest(zp[0], val);
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) mx[s] = fmaxf(mx[s], __shfl_xor(mx[s], o));
+        if (lane == 0) most[v & 1][s][w] = mx[s];
+      }
+      __syncthreads();
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        float m = most[v & 1][s][0];
+#pragma unroll
+        for (int i = 1; i < NW; ++i) m = fmaxf(m, most[v & 1][s][i]);
+        const int e = m > 0.0f ? 15 - __builtin_amdgcn_readfirstlane(__builtin_amdgcn_frexp_expf(m)) : 200;
+        up[s] = s ? min(up[s], e) : e;
+      }
+    }
     auto one = [&](int i, Raw32& rw) {
       bool val;
       int pos, run;
@@ -425,7 +490,7 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
       if constexpr (WIDE) {
         const uint32_t s = live ? rw.side : 0u;
         const float mnf = f16_bits_to_f32(s & 0xffffu), top = fmaf(float((1 << bits) - 1), f16_bits_to_f32(s >> 16), mnf);
-        if (!(fabsf(top) <= 65504.0f && fabsf(mnf) <= 65504.0f)) st |= kOver;
+        if (!(fabsf(top) <= 65504.0f && fabsf(mnf) <= 65504.0f)) st = true;
         const _Float16 m1 = __builtin_bit_cast(_Float16, uint16_t(s)), s1 = __builtin_bit_cast(_Float16, uint16_t(s >> 16));
         const f16x2_t mn = {m1, m1}, sc = {s1, s1};
         auto all = [&](auto width) {
@@ -455,22 +520,26 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
           default: all(std::integral_constant<int, 6>()); break;
         }
       } else {
-        // any block width, row width, or the error-free backend: four channels at a time in binary32
-#pragma unroll 1
-        for (int g4 = 0; g4 < 4; ++g4) {
+        // any block width and row width, or the error-free backend: four channels at a time in binary32
+        auto granule = [&](int g4) {
           float z[2][4];
 #pragma unroll
           for (int q = 0; q < 2; ++q) {
             const int ch = 32 * run + 16 * (g4 >> 1) + 8 * q + 4 * (g4 & 1);
 #pragma unroll
             for (int e = 0; e < 4; ++e) z[q][e] = 0.0f;
-            if (live && ch < d) load4(val ? a.vc : a.kc, c, srow + pos, d, ch, z[q]);
+            if constexpr (KEEP) {
+#pragma unroll
+              for (int e = 0; e < 4; ++e) z[q][e] = zp[i][4 * (g4 >> 1) + 2 * q + (g4 & 1)][e];
+            } else {
+              if (live && ch < d) load4<PASS>(val ? a.vc : a.kc, c, srow + pos, d, ch, z[q]);
+            }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
+              const bool any = z[q][e] != 0.0f;
+              if constexpr (PASS) z[q][e] = __builtin_amdgcn_ldexpf(z[q][e], up[val]);
               const float m = fabsf(z[q][e]);
-              if (!(m <= 65504.0f)) st |= kOver;
-              if (m != 0.0f) st |= val ? kAnyV : kAnyK;
-              if (m >= 0.015625f) st |= val ? kBigV : kBigK;
+              if (!(m <= 65504.0f) || (PASS && any && m < 0x1p-14f)) st = true;
             }
           }
           u32x4_t hi, lo;
@@ -481,12 +550,19 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
           }
           put(0, g4 >> 1, g4 & 1, hi);
           if constexpr (PL == 2) put(1, g4 >> 1, g4 & 1, lo);
+        };
+        if constexpr (KEEP) {
+#pragma unroll
+          for (int g4 = 0; g4 < 4; ++g4) granule(g4);
+        } else {
+#pragma unroll 1
+          for (int g4 = 0; g4 < 4; ++g4) granule(g4);
         }
       }
     };
-    if constexpr (AHEAD) {
+    if constexpr (AHEAD || KEEP) {
 #pragma unroll
-      for (int i = 0; i < IT; ++i) one(i, raw[i]);
+      for (int i = 0; i < IT; ++i) one(i, raw[AHEAD ? i : 0]);
     } else {
 #pragma unroll 1
       for (int i = 0; i < IT; ++i) {
@@ -494,12 +570,7 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
         one(i, raw[0]);
       }
     }
-    // the wave's flags (a bit is set when any lane has it)
-    uint32_t all = 0;
-#pragma unroll
-    for (int k = 0; k < (WIDE ? 1 : 5); ++k)
-      if (__builtin_amdgcn_ballot_w64((st >> k) & 1u)) all |= 1u << k;
-    return all;
+    return __builtin_amdgcn_ballot_w64(st) ? 1u : 0u;  // (in any lane of the wave)
   };
   auto fill = [&](int v, uint8_t* buf) {
     state[v & 1][w] = decode(v, [&](int i, int plane, int g, const u32x4_t& o) { store(buf, i, plane, g, o); });
@@ -647,9 +718,7 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
     uint32_t st = 0;
 #pragma unroll
     for (int i = 0; i < NW; ++i) st |= state[v & 1][i];
-    st = __builtin_amdgcn_readfirstlane(st);
-    return ok && !skip &&
-           ((st & kOver) || (pass && (((st & kAnyK) && !(st & kBigK)) || ((st & kAnyV) && !(st & kBigV)))));
+    return ok && !skip && __builtin_amdgcn_readfirstlane(st);
   };
   // An odd step: its positions in binary32, 16 of K and V at a time through its buffer (in the lanes' order: the
   // values of (kk, hc) at 16 kk + 8 hc, for V of (ct, i, hc) at 32 ct + 8 i + 4 hc), each given to `take`
@@ -666,7 +735,13 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
         const bool val = x >= SUB * (D / 4);
         const int y = val ? x - SUB * (D / 4) : x, pos = y / (D / 4), ch = 4 * (y - pos * (D / 4));
         float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (s0 + pos < live && ch < d) load4(val ? a.vc : a.kc, c, crow + s0 + pos, d, ch, z);
+        if (s0 + pos < live && ch < d) load4<PASS>(val ? a.vc : a.kc, c, crow + s0 + pos, d, ch, z);
+        if constexpr (PASS) {
+          if (val) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[e] = __builtin_amdgcn_ldexpf(z[e], up[1]);
+          }
+        }
         float* dst = rows32 + (val ? SUB * D : 0) + pos * D + (ch & ~15);
         const int half = (ch >> 3) & 1, h4 = (ch >> 2) & 1;  // channels 16 kk + 8 half + 4 h4 ..
 #pragma unroll
@@ -719,7 +794,16 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
     for (; v < v1; ++v) {
       const int t0 = step_pos(v);
       const uint8_t* buf = buf_of(v);
+      const int was = up[1];
       if constexpr (!FUSED) begin();
+      if constexpr (PASS) {
+        if (up[1] != was) {  // (O is zero where there were no values)
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) O[ct][e] = __builtin_amdgcn_ldexpf(O[ct][e], up[1] - was);
+        }
+      }
       odd = odd_step();
       if (odd) break;
       // nothing of the step is visible to this wave's queries, or it holds nothing
@@ -782,6 +866,12 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
           for (int g = 0; g < 4; ++g) store(buf_of(v + 1), i, 0, g, dec[i][g]);
         state[(v + 1) & 1][w] = flags;
         turn();
+      }
+      if constexpr (PASS) {
+#pragma unroll
+        for (int ps = 0; ps < 2; ++ps)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) S[ps][e] = __builtin_amdgcn_ldexpf(S[ps][e], -up[0]);
       }
       // hidden positions: after the lane's token, or before its window and no sink
       const bool whole = !blank && t0 + kStep - 1 <= wlo && (a.window == 0 || t0 > whi - a.window || t0 + kStep <= a.sinks);
@@ -953,7 +1043,12 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
 #pragma unroll
     for (int e2 = 0; e2 < 4; ++e2) {
       uint32_t o[OP];
-      split_b<OP>(O[kk >> 1][8 * (kk & 1) + 2 * e2] * inv, O[kk >> 1][8 * (kk & 1) + 2 * e2 + 1] * inv, o);
+      float x0 = O[kk >> 1][8 * (kk & 1) + 2 * e2] * inv, x1 = O[kk >> 1][8 * (kk & 1) + 2 * e2 + 1] * inv;
+      if constexpr (PASS) {
+        x0 = __builtin_amdgcn_ldexpf(x0, -up[1]);
+        x1 = __builtin_amdgcn_ldexpf(x1, -up[1]);
+      }
+      split_b<OP>(x0, x1, o);
 #pragma unroll
       for (int p = 0; p < OP; ++p) t[p][e2] = o[p];
     }
@@ -1022,6 +1117,7 @@ hipError_t run_chunk(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, in
 // EACH: a kernel for each code width (else one that reads it at run time)
 template <int D, int PL, bool EACH>
 hipError_t by_layout(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st) {
+  if (c.backend == CG_BACKEND_PASSTHROUGH) return run_chunk<D, PL, kErrorFree>(a, G, c, blocks, st);
   if (!chunk_wide(c, a.q.d)) return run_chunk<D, PL, kAnyLayout>(a, G, c, blocks, st);
   if constexpr (EACH) {
     switch (c.bits) {

@@ -151,10 +151,36 @@ class Plain(Case):
         return self.out[0, 0].double().cpu()[:, : self.rows[0][1]], zk, zv
 
 
+@pytest.mark.parametrize("d", [64, 80, 128, 256])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("new", [1, 3])
+def test_error_free_values_of_small_channels(d, dtype, new):
+    """Channels from 1 down to 1e-8 beside each other, growing and falling over the positions, equal weights: every
+    channel's mean within the roundings of its own values.
+
+    Operands: u = 2^-11, or 2^-22 and 2^-40 of the largest value (two planes); the sums over T positions T 2^-24, their
+    planes for the gauge 2^-15 (2^-22), the rest 2^-22, relative to the mean of |v|; one rounding of the type."""
+    T, rng = 300, np.random.default_rng(d)
+    c = Plain([(T - new, new)], H=1, grp=2, d=d, g=d, backend=cg.PASSTHROUGH, dtype=dtype, scale=0.5)
+    pages = c.kc.B
+    v = rng.standard_normal((pages, 64, d)) * 10.0 ** -rng.uniform(0, 8, d)
+    v *= 10.0 ** np.where(np.arange(pages) % 2, 1.5, -1.5)[:, None, None]         # a step of small values after large ones
+    k = rng.standard_normal((pages, 64, d))
+    c.set(np.zeros((c.N, 2, d)), k, v)
+    got, _, zv = c.results()
+    bf = dtype == torch.bfloat16
+    for i in range(new):
+        x = zv[: T - new + 1 + i]
+        want, a = x.mean(0), x.abs().mean(0)
+        lim = a * ((2.0 ** -11 if bf else 2.0 ** -22) + T * 2.0 ** -24 + (2.0 ** -15 if bf else 2.0 ** -22) + 2.0 ** -22) \
+            + (0.0 if bf else 2.0 ** -40 * float(x.abs().max())) + (2.0 ** -8 if bf else 2.0 ** -24) * want.abs()
+        assert ((got[:, i] - want).abs() <= lim).all(), float(((got[:, i] - want).abs() / lim).max())
+
+
 def _weights_bound(got, q, zk, zv, scale, unit, floor, planes, step):
     """got [Hq][new][d] against softmax over all positions a token sees; a score is off by A (2 unit + 2^-21) plus `floor`
-    (of the queries' sum) where A = |scale| sum |q k|, a weight by a factor within exp(+-2 E) and 2 unit, weights and values by 2 unit more, sums over n positions by n 2^-24 and their planes for the gauge by
-    `planes`; all of it relative to the largest |v|."""
+    (of the queries' sum) where A = |scale| sum |q k|, a weight by a factor within exp(+-2 E) and 2 unit, the rest as
+    above; all of it relative to the largest |v|."""
     n, new = zk.shape[0], got.shape[1]
     for j in range(got.shape[0]):
         for i in range(new):
@@ -164,6 +190,25 @@ def _weights_bound(got, q, zk, zv, scale, unit, floor, planes, step):
             E = abs(scale) * (float((zk[:m].abs() @ q[j, i].abs()).max()) * (2 * unit + 2.0 ** -21) + floor * float(q[j, i].abs().sum()))
             lim = (math.expm1(2 * E) + 2 * unit + n * 2.0 ** -24 + planes) * float(zv.abs().max()) + step * want.abs()
             assert E < 0.05 and ((got[j, i] - want).abs() <= lim).all(), (E, float(((got[j, i] - want).abs() / lim).max()))
+
+
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("new", [1, 3])
+def test_error_free_keys_of_small_channels(d, dtype, new):
+    """What tells the positions apart lies in a channel of 1e-6, where the query is large, beside channels of 1 where it is
+    nought."""
+    T, rng = 200, np.random.default_rng(d + 1)
+    c = Plain([(T - new, new)], H=1, grp=2, d=d, g=d, backend=cg.PASSTHROUGH, dtype=dtype, scale=1.0)
+    k = rng.standard_normal((c.kc.B, 64, d))
+    k[..., 7] = 1e-6 * rng.standard_normal(k.shape[:2])
+    q = np.zeros((c.N, 2, d))
+    q[..., 7] = rng.uniform(1e6, 2e6, q.shape[:2])
+    c.set(q, k, rng.standard_normal((c.kc.B, 64, d)))
+    got, zk, zv = c.results()
+    bf = dtype == torch.bfloat16
+    _weights_bound(got, c.q[0, :, :new].double(), zk, zv, 1.0, 2.0 ** -11 if bf else 2.0 ** -22, 0.0 if bf else 2.0 ** -40 * float(zk.abs().max()),
+                   2.0 ** -15 if bf else 2.0 ** -22, 2.0 ** -8 if bf else 2.0 ** -24)
 
 
 @pytest.mark.parametrize("bits,n,d", [(4, 32, 128), (4, 16, 128), (4, 64, 256), (8, 32, 64)])
