@@ -1078,11 +1078,18 @@ static int32_t check_chunk(int32_t nl, int32_t N, int32_t B, int32_t max_q, int3
   return CG_OK;
 }
 
-// Single tokens go to the single-token attention (max_q = 1, or in a launch of its own beside the chunks of a
-// batch) where its matrix-core kernel takes the caches, or where the chunk kernel decodes four channels at a
-// time.  32 rows of up to 8000 positions, 8 KV heads x 4: d = 128, n = 64 675 us as chunks of one token, 86 there;
-// d = 80 1710 against 917; but d = 64 251 against 636, d = 128, n = 32 675 against 1138.  Its plan, for rows of
-// as many positions as they see:
+// Single tokens go to the single-token attention (max_q = 1, or in a launch of its own beside the chunks of a batch)
+// where its matrix-core kernel takes the caches; elsewhere they are chunks of one token, but for binary32 results over
+// error-free pools with few query heads.  32 rows of up to 8000 positions, 8 KV heads x 4, us there and as chunks: bf16
+// results d = 128, n = 64 64 : 140, n = 32 958 : 139, n = 16 964 : 440, d = 80 946 : 405, d = 64, n = 16 729 : 236, d = 256,
+// n = 64 3348 : 925; binary32 n = 64 74 : 547, n = 16 972 : 942 (one head per KV head 824 : 940, eight 1217 : 944), d = 80
+// 950 : 827, d = 64 730 : 310, d = 256, n = 16 3373 : 1960; error-free d = 128 bf16 989 : 594, binary32 989 : 1253 (one
+// head 846 : 1254, eight 1225 : 1233), d = 64 743 : 412, d = 256 3184 : 3657.
+static bool singles_apart(const CodecDev& c, int d, int grp, bool f32) {
+  return attend_mfma_supported(d, true, c) || (c.backend == CG_BACKEND_PASSTHROUGH && f32 && d > 64 && grp <= 4);
+}
+
+// Its plan, for rows of as many positions as they see:
 static AttendPlan singles_plan(int nl, int B, int H, int Hq, int d, int cap, int window, int sinks) {
   const int64_t seen = window > 0 ? int64_t(window) + sinks + 128 : cap;
   const int span = int(std::min<int64_t>(cap, seen));
@@ -1144,7 +1151,7 @@ int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const
   if ((rc = check_apart(out)) != CG_OK) return rc;
   const int cap = pages->max_pages * pages->page_size;
   const CodecDev c = codec_dev(codec);
-  const bool singles = (max_q == 1 || B > 1) && (attend_mfma_supported(shp.d, true, c) || !chunk_wide(c, shp.d));
+  const bool singles = (max_q == 1 || B > 1) && singles_apart(c, shp.d, q->H / shp.H, out->dtype == CG_DTYPE_F32);
   const ChunkPlan p = chunk_plan(nl, q->T, B, max_q, shp.H, q->H, shp.d, cap, window, sinks, singles);
   const AttendPlan one = singles_plan(nl, B, shp.H, q->H, shp.d, cap, window, sinks);
   const bool ws = (p.ws_bytes && (max_q > 1 || !singles)) || (one.ws_bytes && singles);
