@@ -421,7 +421,8 @@ int32_t rope_make(const cg_rope* rope, cg_rope_plan* plan);
 
 /* Rotary positions: y = x with channels [0, d_rot) of every token turned by its position,
  *   (x_a, x_b) -> amplitude (x_a cos - x_b sin, x_a sin + x_b cos),   angle = pos f_i
- * (angles exact to 2^-32 turns at any position, products and sums in binary32, one rounding).  x0, y0: views
+ * (angles modulo a quarter turn to 2^-31 turns at any position, p f 2^-63 more for a pair that turns by f > 1 radians per
+ * position; from there on binary32, one rounding).  x0, y0: views
  * [L][B][H0][T][d] of one element type; x1, y1 (both or neither): views [L][B][H1][T][d] of the same type,
  * turned by the same launch (queries and keys).  y may be x itself (same pointer and strides), else they must
  * not overlap; no two elements of a y share an address (CG_ERR_ARG).  pos: device int32 [B][T]; a token with a

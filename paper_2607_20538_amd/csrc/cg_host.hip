@@ -2,6 +2,8 @@
 // sizing and dispatch of the encode / decode / rolling-append kernels.
 #include <math.h>
 #include <climits>
+#include <cmath>
+#include <limits>
 #include <stdlib.h>
 #include <string.h>
 
@@ -992,17 +994,24 @@ int32_t rope_make(const cg_rope* r, cg_rope_plan* plan) {
   p.d_rot = r->d_rot;
   p.layout = r->layout;
   p.amplitude = float(r->amplitude);
+  // In 64-bit significands: a fraction off by 2^-63 turns is off by 2^-32 at position 2^31 (binary64's 2^-55: by 2^-24).
+  // Rounding the power's exponent costs f |ln f| 2^-64, at most 2^-65 where f <= 1.
+  using real = long double;
+#ifndef __HIP_DEVICE_COMPILE__
+  static_assert(std::numeric_limits<real>::digits >= 64, "turns per position as 64-bit fractions");
+#endif
+  const real pi2 = 6.283185307179586476925286766559005768394L;
   for (int i = 0; i < r->d_rot / 2; ++i) {
-    double f = pow(r->base, -2.0 * i / r->d_rot);  // radians per position
+    real f = std::pow(real(r->base), real(-2 * i) / r->d_rot);  // radians per position
     if (r->scaling == CG_ROPE_LINEAR) f /= r->factor;
     if (r->scaling == CG_ROPE_RAMP) {
-      const double w = std::min(1.0, std::max(0.0, (r->train_len * f / (2.0 * M_PI) - r->low) / (r->high - r->low)));
-      f = f * (1.0 - w) / r->factor + f * w;
+      const real w = std::min<real>(1, std::max<real>(0, (r->train_len * f / pi2 - r->low) / (real(r->high) - r->low)));
+      f = f * (1 - w) / r->factor + f * w;
     }
-    if (!isfinite(f)) return CG_ERR_ARG;
-    const double t = f / (2.0 * M_PI), frac = t - floor(t);  // whole turns per position are none
-    const double s = ldexp(frac, 64);
-    p.step[i] = s >= 18446744073709551615.0 ? 0 : uint64_t(s);
+    if (!std::isfinite(double(f))) return CG_ERR_ARG;
+    const real t = f / pi2;
+    const real s = std::rint(std::ldexp(t - std::floor(t), 64));  // whole turns per position are none
+    p.step[i] = s >= 18446744073709551616.0L ? 0 : uint64_t(s);
   }
   *plan = p;
   return CG_OK;

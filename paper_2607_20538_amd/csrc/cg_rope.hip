@@ -2,8 +2,8 @@
 // position, before the gauge sees the key.
 //
 // Pair i of a token at position p turns by p f_i radians (f_i falls geometrically with i).  In binary32 p f_i
-// is off by whole radians at far positions, so the frequency is held in turns as a 64-bit fraction F = f / 2 pi:
-// p F modulo 2^64 is the angle modulo one turn, exact up to p 2^-64, by two integer products.  The nearest
+// is off by whole radians at far positions, so the frequency is held in turns as a 64-bit fraction F = f / 2 pi (within
+// 2^-63): p F modulo 2^64 is the angle modulo one turn, to p 2^-63, by two integer products.  The nearest
 // quarter turn comes off in integers too; sine and cosine of the rest (at most pi / 4) are Taylor polynomials
 // whose first dropped terms are below 2^-28.
 //

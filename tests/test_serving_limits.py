@@ -1,6 +1,7 @@
-"""Sizes of a serving step's workspaces, on the host."""
+"""Sizes of a serving step's workspaces and plans of its rotary positions, on the host."""
 import math
 import random
+from decimal import Decimal, localcontext
 
 import pytest
 
@@ -41,3 +42,39 @@ def test_workspace_limit_of_nothing_and_of_bad_sizes():
     assert lim(1, 4096, 1, 32, 4, 64) == 0                         # rows too short to split
     assert lim(0, 1, 1, 32, 400, 64) == lim(1, 1, 1, 31, 400, 64) == lim(1, 1, 1, 32, 400, 63) == lim(1, 0, 1, 32, 400, 64) == 0
     assert lim(2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31 - 8, 400, 64) <= 2 ** 30
+
+
+# ------------------------------------------------------------------------------------------
+# turns per position
+# ------------------------------------------------------------------------------------------
+
+PI = Decimal("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899863")
+
+
+@pytest.mark.parametrize("scaling", [cg.ROPE_NONE, cg.ROPE_LINEAR, cg.ROPE_RAMP])
+@pytest.mark.parametrize("base", [10000.0, 500000.0, 1000000.5, 1.0, 1e-4])
+@pytest.mark.parametrize("d_rot", [2, 6, 20, 64, 96, 128, 256])
+def test_rope_steps_are_the_turns_to_64_bits(d_rot, base, scaling):
+    """The plan's fractions against 70-digit arithmetic, in units of 2^-64 turns.  A power and a quotient in 64-bit
+    significands: 2^-63 f for the power, f |ln f| 2^-65 for its exponent, 3 2^-64 f for two or three more operations (RAMP's
+    blend: as many again), over 2 pi, and half a unit: 1 + 2 f in all, of f radians."""
+    with localcontext() as ctx:
+        ctx.prec = 70
+        factor, low, high, train = 8.1, 1.0, 4.0, 8192
+        plan = cg.rope_make(d_rot, cg.ROPE_HALF, base=base, scaling=scaling, factor=factor, low=low, high=high, train_len=train)
+        for i in range(d_rot // 2):
+            f0 = (Decimal(base).ln() * -2 * i / d_rot).exp()
+            f = f0
+            if scaling == cg.ROPE_LINEAR:
+                f = f0 / Decimal(factor)
+            if scaling == cg.ROPE_RAMP:
+                w = min(Decimal(1), max(Decimal(0), (train * f0 / (2 * PI) - Decimal(low)) / (Decimal(high) - Decimal(low))))
+                f = f0 * (1 - w) / Decimal(factor) + f0 * w
+            want = f / (2 * PI) % 1 * 2 ** 64
+            off = abs(Decimal(plan.step[i]) - want)
+            off = min(off, 2 ** 64 - off)
+            lim = 1 + 2 * f0 * (1 + abs(f0.ln()) / 16) * (4 if scaling == cg.ROPE_RAMP else 1)
+            assert off <= lim, (i, off)
+            if base >= 1:
+                # at the last position: 2^-32 turns
+                assert off * (2 ** 31 - 1) <= 2 ** 32 * (4 if scaling == cg.ROPE_RAMP else 2)
