@@ -399,11 +399,13 @@ int32_t kv_append_paged(int32_t l0, int32_t l1, const cg_kv_view* k_new, const c
  *            kv_append_slots puts it (device int32 [N]; -1 for i >= cu[B])
  * and the pool's free_count.  N: packed tokens there is room for.  Rows past the table's
  * max_pages * P positions, negative lengths, and more than N tokens set CG_FLAG_POS_RANGE; a pool that
- * runs out sets CG_FLAG_POOL_EMPTY and leaves -1 in the table.  Tokens without a page get slot -1, a negative
- * add counts as 0, a row with a negative held takes no page and none of its tokens gets a slot.  page_size a multiple of 64;
- * n_pages * page_size and max_pages * page_size below 2^31 (CG_ERR_CAPACITY).  Calls on one pool follow one
- * another (on one stream, or ordered by events).  Errors: CG_ERR_ARG, CG_ERR_SHAPE, CG_ERR_ALIGN,
- * CG_ERR_CAPACITY, CG_ERR_DEVICE. */
+ * runs out sets CG_FLAG_POOL_EMPTY and leaves -1 in the table: no later step fills such a hole, and repeating the call
+ * would take pages anew in place of those it did get, which would be lost.  The rows with a hole are given back whole
+ * (kv_page_release skips holes) and begun again once there are pages; the others go on.  Tokens without a page
+ * get slot -1 (and set CG_FLAG_POS_RANGE), a negative add counts as 0, a row with a negative held takes no page
+ * and none of its tokens gets a slot.  page_size a multiple of 64; n_pages * page_size and
+ * max_pages * page_size below 2^31 (CG_ERR_CAPACITY).  Calls on one pool follow one another (on one stream, or
+ * ordered by events).  Errors: CG_ERR_ARG, CG_ERR_SHAPE, CG_ERR_ALIGN, CG_ERR_CAPACITY, CG_ERR_DEVICE. */
 int32_t kv_page_map(const int32_t* held, const int32_t* add, int32_t B, const cg_page_pool* pool, int32_t* pages,
                     int32_t max_pages, int32_t page_size, int32_t N, int32_t* cu, int32_t* lens, int32_t* pos,
                     int32_t* slots, int32_t* err_flag, void* stream);

@@ -478,7 +478,8 @@ class PagePool:
 def kv_page_map(held, add, pool: PagePool, pages, page_size: int, cu, lens, pos, slots, err_flag=None, stream=None):
     """Tables and slots of one step: row b holds held[b] positions and adds add[b] tokens (int32 [B]).  Takes the
     new pages off `pool` into the table `pages` [B][max_pages] and writes lens [B] (may be held), cu [B + 1], and
-    for the packed tokens pos [N] and slots [N] (-1 behind the last one)."""
+    for the packed tokens pos [N] and slots [N] (-1 behind the last one).  A step that runs out of pages
+    (CG_FLAG_POOL_EMPTY) is not repeated: the rows with a hole (-1) are released whole and begun again."""
     _on_device("kv_page_map", held=held, add=add, free=pool.free, count=pool.count, pages=pages, cu=cu, lens=lens,
                pos=pos, slots=slots, err_flag=err_flag)
     B, N = held.numel(), pos.numel()

@@ -230,3 +230,40 @@ def test_queries_of_small_channels(bits, n, d, dtype):
     floor = 0.0 if bf else 2.0 ** -40 * n * float(zk.max())       # of the largest query, 1
     _weights_bound(got, c.q[0, :, :new].double(), zk, zv, 40.0, 2.0 ** -11 if bf else 2.0 ** -22, floor, 2.0 ** -15 if bf else 2.0 ** -22,
                    2.0 ** -8 if bf else 2.0 ** -24)
+
+
+def test_a_step_that_ran_out_of_pages_is_begun_again():
+    """Rows with a hole are given back whole and begun again after another row is done: every page stands in one place
+    throughout, the rows' slots are those of their pages, and rows that had enough keep theirs."""
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    P, total, B, maxp = 64, 9, 4, 6
+    pool = cg.PagePool(total)
+    pages = torch.full((B, maxp), -1, dtype=torch.int32, device="cuda")
+    lens, cu, pos, slots, err = i32([0] * B), i32([0] * (B + 1)), i32([0] * 400), i32([0] * 400), i32([0])
+
+    def step(add):
+        err.zero_()
+        cg.kv_page_map(lens, i32(add), pool, pages, P, cu, lens, pos, slots, err)
+        torch.cuda.synchronize()
+        n = int(pool.count.item())
+        free, held = pool.free.tolist()[:n], [p for p in pages.flatten().tolist() if p >= 0]
+        assert sorted(free + held) == list(range(total))
+        table, first = pages.tolist(), cu.tolist()
+        for b in range(B):
+            for i in range(first[b], first[b + 1]):
+                t = int(lens[b]) - (first[b + 1] - i)
+                pg = table[b][t // P]
+                assert int(pos[i]) == t and int(slots[i]) == (pg * P + t % P if pg >= 0 else -1)
+        return int(err.item()), n, table
+
+    assert step([100, 60, 130, 0])[:2] == (0, 3)
+    flag, left, table = step([1, 70, 1, 200])                  # row 1 takes two pages, row 3 gets one of four
+    assert flag == cg.CG_FLAG_POOL_EMPTY | cg.CG_FLAG_POS_RANGE and left == 0 and table[3].count(-1) == maxp - 1
+    assert lens.tolist() == [101, 130, 131, 200]
+    kept = table[0], table[2]
+    cg.kv_page_release(lens, i32([0, 1, 0, 1]), pool, pages, P, err)   # row 1 is done, row 3 has holes
+    torch.cuda.synchronize()
+    assert int(pool.count.item()) == 4 and lens.tolist() == [101, 0, 131, 0]
+    flag, left, table = step([1, 0, 1, 200])
+    assert flag == 0 and left == 0 and lens.tolist() == [102, 0, 132, 200]
+    assert (table[0], table[2]) == kept and table[3][:4].count(-1) == 0
