@@ -267,3 +267,78 @@ def test_a_step_that_ran_out_of_pages_is_begun_again():
     flag, left, table = step([1, 0, 1, 200])
     assert flag == 0 and left == 0 and lens.tolist() == [102, 0, 132, 200]
     assert (table[0], table[2]) == kept and table[3][:4].count(-1) == 0
+
+
+LONG = {
+    "b2": dict(bits=2), "b3": dict(bits=3), "b4": dict(bits=4), "b6": dict(bits=6), "b8": dict(bits=8),
+    "n32": dict(n=32, bits=3), "n16": dict(n=16), "n128": dict(n=128, bits=6), "error_free": dict(backend=cg.PASSTHROUGH),
+    "d64": dict(d=64, n=32), "d64_b8": dict(d=64, n=64, bits=8), "d80": dict(d=80, n=80), "d256": dict(d=256, n=64),
+    "f32": dict(dtype=torch.float32), "f32_b8_n128": dict(dtype=torch.float32, bits=8, n=128), "f32_n16": dict(dtype=torch.float32, n=16),
+    "f32_d64": dict(dtype=torch.float32, d=64, n=32, bits=6), "f32_d256": dict(dtype=torch.float32, d=256, n=128),
+    "f32_error_free": dict(dtype=torch.float32, backend=cg.PASSTHROUGH),
+}
+
+
+@pytest.mark.parametrize("rows", [[(6000, 3)], [(5003, 70), (1, 1)], [(6001, 1)], [(4000, 1), (3000, 2), (63, 1)]], ids=lambda r: "+".join(f"{h}_{t}" for h, t in r))
+@pytest.mark.parametrize("window,sinks", [(0, 0), (2500, 300)])
+@pytest.mark.parametrize("name", list(LONG))
+def test_every_position_of_a_long_row_counts(name, window, sinks, rows):
+    """Channel c of a value is 1 at the c-th stretch of its row's positions and 0 elsewhere (identity gauge), so an output
+    channel is the weight of its stretch, about 1 / d: sums of positive terms, which do not average away.  A step
+    left out, taken twice or read from another page moves a channel by most of itself.
+
+    Bound, relative to the channel: scores of A at most are off by E = A (2 u + d 2^-24), u = 2^-11 or 2^-22 the rounding of an
+    operand; all weights by a factor within exp(+-2 E); weights and values by u each, sums over T positions by T 2^-24,
+    their planes for the gauge 2^-15 (2^-22), one rounding of the type.  Hidden stretches are nought in chunks.  Single tokens of
+    128 channels in blocks of 64 or 128 form a value from its block's offset and the code's distance from it: of each step of 32
+    positions one product's and eight offsets' additions round by 2^-24 of a partial sum, at most 2 (a range of 1, the weights'
+    sum 1): 9 n / 32 2 2^-24 whatever the channel."""
+    kw = dict(dict(d=128, n=64, bits=4, dtype=torch.bfloat16), **LONG[name])
+    d = kw["d"]
+    c = Plain(rows, H=1, grp=4, g=d, window=window, sinks=sinks, scale=0.08, seed=len(name), **kw)
+    rng = np.random.default_rng(11)
+    stretch = np.full((c.kc.B, 64), -1)
+    for b, n in enumerate(c.held):
+        for i in range(-(-n // 64)):
+            t = np.arange(64 * i, min(n, 64 * i + 64))
+            stretch[c.table[b, i], : len(t)] = t * d // n
+    one = (stretch[..., None] == np.arange(d)).astype(np.float32)                # [pages][64][d]
+    if c.codec.backend == cg.PASSTHROUGH:
+        c.set(None, rng.uniform(-1, 1, one.shape), one)
+    else:
+        top = 2 ** c.codec.bits - 1
+        bit = (top * one[..., None].astype(np.uint8) >> np.arange(c.codec.bits)) & 1
+        c.pools[1][0] = np.packbits(bit.reshape(1, c.kc.B, 1, 64, -1), axis=-1, bitorder="little")
+        for s, (mn, sc) in enumerate(((-1.0, 2.0 / top), (0.0, 1.0 / top))):
+            c.pools[s][1][..., 0], c.pools[s][1][..., 1] = np.float16(mn), np.float16(sc)
+        c.set()
+    c.call()
+    torch.cuda.synchronize()
+    assert int(c.err.item()) == 0
+    got = c.out[0, 0].double().cpu()
+    zk, zv = (S.pool_values(c.codec, *p) for p in c.pools)
+    bf = c.out.dtype == torch.bfloat16
+    u, planes, step = (2.0 ** -11, 2.0 ** -15, 2.0 ** -8) if bf else (2.0 ** -22, 2.0 ** -22, 2.0 ** -24)
+    offsets = d == 128 and c.codec.backend == cg.BLOCK_UNIFORM and c.codec.block_c >= 64
+    for b, (held, new) in enumerate(rows):
+        n = held + new
+        floor = 9 * n / 16 * 2.0 ** -24 if offsets and new == 1 else 0.0
+        K, V = (torch.from_numpy(z[0, c.table[b][: -(-n // 64)], 0].reshape(-1, d)[:n]) for z in (zk, zv))
+        for i in sorted({0, new // 2, new - 1}):
+            p = held + i
+            seen = S.visible(p, n, window, sinks)
+            q = c.q[0, :, int(c.first[b]) + i].double()
+            s = (c.scale * q @ K.T).masked_fill(~seen, -math.inf)
+            w = torch.softmax(s, -1)
+            want = w @ V
+            E = abs(c.scale) * float((q.abs() @ K[seen].abs().T).max()) * (2 * u + d * 2.0 ** -24)
+            lim = want * (math.expm1(2 * E) + 2 * u + n * 2.0 ** -24 + planes + step) + floor
+            err = (got[:, int(c.first[b]) + i] - want).abs()
+            assert (err <= lim).all(), (b, i, float((err / lim.clamp(min=1e-30)).max()))
+            if n >= 1000:
+                # without the first, a middle or the last step that is seen, the same comparison fails
+                steps = torch.unique(torch.nonzero(seen)[:, 0] // 64)
+                for gone in (steps[0], steps[len(steps) // 2], steps[-2]):
+                    x = w.masked_fill((torch.arange(n) // 64 == gone)[None], 0.0)
+                    x = x / x.sum(-1, keepdim=True)
+                    assert ((x @ V - want).abs() > 3 * lim).any(-1).all()
