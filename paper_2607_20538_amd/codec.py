@@ -384,8 +384,14 @@ def kv_attend_noalloc(l0: int, l1: int, q, kc: Cache, vc: Cache, G_dev, shp: Gau
 
 
 def page_table(pages, page_size: int) -> PageTable:
-    """cg_page_table of a device int32 tensor pages [B][max_pages]."""
-    return PageTable(_ptr(pages), int(pages.shape[1]), int(page_size))
+    """cg_page_table of a contiguous device int32 tensor pages [B][max_pages] (columns cut from a wider table are
+    not one: their rows lie further apart)."""
+    if pages.dim() != 2:
+        raise ValueError("page_table: pages must be [B][max_pages]")
+    _int32("page_table", None, pages=pages)
+    pt = PageTable(_ptr(pages), int(pages.shape[1]), int(page_size))
+    pt.tensor = pages  # lives as long as the table
+    return pt
 
 
 def attend_paged_workspace_bytes(shp: GaugeShape, nl: int, B: int, Hq: int, max_pages: int, page_size: int) -> int:
@@ -568,6 +574,11 @@ def kv_attend_chunk_paged(l0: int, l1: int, q, cu, max_q: int, kc: Cache, vc: Ca
     B = lens.numel()
     _int32("kv_attend_chunk_paged", B, lens=lens)
     _int32("kv_attend_chunk_paged", B + 1, cu=cu)
+    table = getattr(pt, "tensor", None)
+    if table is not None:
+        _on_device("kv_attend_chunk_paged", pages=table)
+        if table.shape[0] != B:
+            raise ValueError(f"kv_attend_chunk_paged: a page table of {table.shape[0]} rows, {B} lens")
     qv, ov, cs, kcs, vcs = view(q), view(out), codec.struct(), kc.struct(), vc.struct()
     if workspace is not None:
         need = attend_chunk_workspace_bytes(shp, l1 - l0, qv.T, B, max_q, qv.H, pt.max_pages, pt.page_size, window, sinks)

@@ -342,3 +342,14 @@ def test_every_position_of_a_long_row_counts(name, window, sinks, rows):
                     x = w.masked_fill((torch.arange(n) // 64 == gone)[None], 0.0)
                     x = x / x.sum(-1, keepdim=True)
                     assert ((x @ V - want).abs() > 3 * lim).any(-1).all()
+
+
+def test_attend_refuses_a_table_of_other_rows():
+    c = Case([(70, 3), (5, 1)], H=1)
+    ws = c.workspace()[0]
+    for pages in (c.pages[:1], torch.cat((c.pages, c.pages))):
+        with pytest.raises(ValueError):
+            cg.kv_attend_chunk_paged(0, 1, c.qd, c.cu, c.max_q, c.kc, c.vc, cg.page_table(pages, c.P), c.Gd, c.shp, c.codec, c.lens,
+                                     c.scale, c.out, workspace=ws)
+    torch.cuda.synchronize()
+    assert (c.out == 7).all()

@@ -1,9 +1,12 @@
-"""Sizes of a serving step's workspaces and plans of its rotary positions, on the host."""
+"""Sizes of a serving step's workspaces, plans of its rotary positions and page tables, on the host."""
+import ctypes as C
+import gc
 import math
 import random
 from decimal import Decimal, localcontext
 
 import pytest
+import torch
 
 from paper_2607_20538_amd import codec as cg
 
@@ -78,3 +81,23 @@ def test_rope_steps_are_the_turns_to_64_bits(d_rot, base, scaling):
             if base >= 1:
                 # at the last position: 2^-32 turns
                 assert off * (2 ** 31 - 1) <= 2 ** 32 * (4 if scaling == cg.ROPE_RAMP else 2)
+
+
+# ------------------------------------------------------------------------------------------
+# page tables
+# ------------------------------------------------------------------------------------------
+
+def test_page_table_refuses_what_the_kernels_would_misread():
+    wide = torch.arange(24, dtype=torch.int32).reshape(4, 6)
+    for bad in (wide[:, :3], wide[:, ::2], wide.t(), wide.long(), wide[0]):
+        with pytest.raises(ValueError):
+            cg.page_table(bad, 64)
+    for good in (wide, wide[1:], wide[:1, :3]):
+        pt = cg.page_table(good, 64)
+        assert (pt.pages, pt.max_pages, pt.page_size) == (good.data_ptr(), good.shape[1], 64)
+
+
+def test_page_table_keeps_its_tensor():
+    pt = cg.page_table(torch.arange(6, dtype=torch.int32).reshape(2, 3).clone(), 64)
+    gc.collect()
+    assert (C.c_int32 * 6).from_address(pt.pages)[:] == list(range(6))
