@@ -428,10 +428,11 @@ int32_t rope_make(const cg_rope* rope, cg_rope_plan* plan);
  * [L][B][H0][T][d] of one element type; x1, y1 (both or neither): views [L][B][H1][T][d] of the same type,
  * turned by the same launch (queries and keys).  y may be x itself (same pointer and strides), else they must
  * not overlap; no two elements of a y share an address (CG_ERR_ARG).  pos: device int32 [B][T]; a token with a
- * negative position is left as it was.
+ * negative position is skipped: its rows of y stay what they were.
  * inverse != 0: the transposed map (turned back, the same amplitude): the gradient with respect to x of
  * a gradient given for y.  Errors: CG_ERR_ARG, CG_ERR_SHAPE, CG_ERR_ALIGN, CG_ERR_UNSUPPORTED (d no multiple
- * of 8 or above 256), CG_ERR_CAPACITY (2^31 or more tokens x channels / 2), CG_ERR_DEVICE. */
+ * of 8 or above 256), CG_ERR_CAPACITY (2^31 or more tokens x channels / 2; more than 65535
+ * layers x heads of both views), CG_ERR_DEVICE. */
 int32_t kv_rope(const cg_rope_plan* plan, const cg_kv_view* x0, const cg_kv_view* y0, const cg_kv_view* x1,
                 const cg_kv_view* y1, const int32_t* pos, int32_t inverse, void* stream);
 
@@ -468,7 +469,8 @@ size_t attend_chunk_workspace_limit(cg_gauge_shape shp, int32_t nl, int32_t N, i
  * window; window = 0: causal (sinks unused).  bf16 outputs are computed from operands of 11 bits (binary16;
  * rows of one token: of 16 bits or more) with binary32 sums, binary32 outputs from operands of 22 bits (error-free pools: below
  * 2^-18 of a step's largest value to within 2^-40 of it).  out must not overlap q.  Positions a token does not see do not reach its
- * output, whatever their bytes decode to; a NaN or infinity that it does see makes it NaN.  Tokens behind the
+ * output, whatever their bytes decode to; a NaN that it does see makes it NaN, an infinity what exp and the products make
+ * of it (scores of -inf alone: zeros or NaN).  Tokens behind the
  * last row are left as they were.  A row whose lens is below n_b or above max_pages * page_size sets
  * CG_FLAG_POS_RANGE and gets zeros; a row whose cu runs backwards, past N or over max_q sets it and is left as it
  * was; a page outside the pool sets it and contributes nothing.

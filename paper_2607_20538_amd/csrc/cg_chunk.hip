@@ -80,6 +80,8 @@ ChunkPlan chunk_plan(int nl, int N, int B, int max_q, int H, int Hq, int d, int 
                                    : (int64_t(cap) + kStep - 1) / kStep;
   // Splits: the least estimated time in us, from what steps were measured to take (d = 128): 1.7 alone on a CU, 1.33
   // each beside others, queries and sums as much as 6, the sums of splits written and read at 4 TB/s and joined in 5.
+  // (bf16 results.  Against the best of 1 to 64 splits, six batches of 16 to 1500 tokens over 2000 to 20000 positions: within
+  // 9% for d = 64, 128, 256 and both result types; blocks of 16 channels and error-free pools 35% and 28% at worst.)
   // Of rows with few tokens each is a tile; where single tokens have another kernel, little is known of the others.
   const double tiles = mq == 1 ? rows
                                : std::min<double>(p.ntile, double(N) / p.tq + (singles ? 1 + std::min(rows / 2.0, N / (4.0 * p.tq))

@@ -436,7 +436,7 @@ static hipError_t launch_append_slots(const ViewDev& Kn, const ViewDev& Vn, int 
   if (!force_generic() && int64_t(Kn.T) * Kn.L * Kn.H >= kEncodeRows && mfma_encode_supported(Kn, G, c, true) &&
       mfma_encode_supported(Vn, G, c, true))
     return launch_encode_slots(Kn, Vn, l0, slots, G, c, kc, vc, err, st);
-  constexpr int kMost = 1 << 19;  // tokens of a launch (its grid holds 2^16 groups of 16)
+  constexpr int kMost = 1 << 19;  // tokens of a launch: 2^15 groups of 16, of the 65535 that its grid's second dimension holds
   for (int i0 = 0; i0 < Kn.T; i0 += kMost) {
     ViewDev x[2] = {Kn, Vn};
     for (ViewDev& v : x) {
