@@ -353,3 +353,40 @@ def test_attend_refuses_a_table_of_other_rows():
                                      c.scale, c.out, workspace=ws)
     torch.cuda.synchronize()
     assert (c.out == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("new", [1, 60])
+@pytest.mark.parametrize("what", ["k+", "k-", "v"])
+def test_infinities_act_as_in_exp_and_products(what, new, dtype):
+    """An infinite key or value at position 130 of an error-free pool, identity gauge, window of 40: a score of +inf makes
+    the result NaN, one of -inf weighs nothing, an infinite value its channel infinite or NaN; who does not see it is
+    untouched.  The bounds of the others: _weights_bound's, scores of 6 at most."""
+    c = Plain([(180 - new, new)], H=1, grp=2, d=64, g=64, backend=cg.PASSTHROUGH, dtype=dtype, scale=0.2, window=40)
+    rng = np.random.default_rng(3)
+    k, v = (rng.uniform(-1, 1, (c.kc.B, 64, 64)) for _ in (0, 1))
+    q = rng.uniform(0.2, 1.0, (c.N, 2, 64))
+    (v if what == "v" else k)[c.table[0, 2], 2, 5] = -np.inf if what == "k-" else np.inf
+    c.set(q, k, v)
+    got, zk, zv = c.results()
+    q = c.q[0, :, :new].double()
+    bf = dtype == torch.bfloat16
+    u, planes, step = (2.0 ** -11, 2.0 ** -15, 2.0 ** -8) if bf else (2.0 ** -22, 2.0 ** -22, 2.0 ** -24)
+    for i in range(new):
+        p = 180 - new + i
+        t = S.visible(p, 180, 40, 0)
+        for j in range(2):
+            if t[130] and what == "k+":
+                assert torch.isnan(got[j, i]).all()
+                continue
+            if t[130] and what == "v":
+                assert not torch.isfinite(got[j, i, 5])
+                continue
+            w = t.clone()
+            if what == "k-":
+                w[130] = False
+            K, V = zk[w], zv[w]
+            want = torch.softmax(c.scale * K @ q[j, i], 0) @ V
+            E = c.scale * float((K.abs() @ q[j, i].abs()).max()) * (2 * u + 2.0 ** -21)
+            lim = math.expm1(2 * E) + 2 * u + 40 * 2.0 ** -24 + planes + step * want.abs()
+            assert ((got[j, i] - want).abs() <= lim).all()
