@@ -25,7 +25,7 @@
 //
 // Bound by the vector work of decoding and of the exponentials beside the products, which overlap in part (vector
 // units busy 50% of the time, matrix cores 34%, two waves per SIMD).  4096 tokens at the end of 20000 positions, 8 KV
-// heads x 4, d = 128, 4 bits: 1.82 to 1.91 ms from card to card = 818 to 781 TFLOP/s (a plain
+// heads x 4, d = 128, 4 bits: 1.78 to 1.91 ms from card to card = 838 to 781 TFLOP/s (a plain
 // binary16 matrix product reaches 1169).
 #pragma once
 
