@@ -390,3 +390,32 @@ def test_infinities_act_as_in_exp_and_products(what, new, dtype):
             E = c.scale * float((K.abs() @ q[j, i].abs()).max()) * (2 * u + 2.0 ** -21)
             lim = math.expm1(2 * E) + 2 * u + 40 * 2.0 ** -24 + planes + step * want.abs()
             assert ((got[j, i] - want).abs() <= lim).all()
+
+
+@pytest.mark.parametrize("d,g,bits,n", [(64, 64, 4, 32), (128, 128, 4, 64)])
+def test_slots_of_more_tokens_than_one_launch_holds(d, g, bits, n):
+    """2^19 + 77 tokens: the same bytes as in two calls (128 channels: one launch of the matrix-core encoder, whose bytes do
+    not depend on the tokens beside)."""
+    N, P = 2 ** 19 + 77, 256
+    pages = N // P + 2
+    codec = cg.Codec(cg.BLOCK_UNIFORM, bits, n)
+    shp, Gd = S.gauge_dev(S.haar(1, 1, d, g, 2))
+    torch.manual_seed(d)
+    x = [torch.randn((1, 1, 1, N, d), device="cuda").to(torch.bfloat16) for _ in (0, 1)]
+    slots = torch.randperm(pages * P, device="cuda")[:N].to(torch.int32)
+    slots[::1001] = -1
+    one, two = ([cg.Cache(codec, s, 1, pages, 1, P, d) for s in (0, 1)] for _ in (0, 1))
+    err = torch.zeros(1, dtype=torch.int32, device="cuda")
+    cg.kv_append_slots(0, 1, *x, slots, Gd, shp, codec, *one, err)
+    for a, b in ((0, 2 ** 18), (2 ** 18, N)):
+        cg.kv_append_slots(0, 1, *(t[:, :, :, a:b] for t in x), slots[a:b], Gd, shp, codec, *two, err)
+    torch.cuda.synchronize()
+    assert int(err.item()) == 0
+    for a, b in zip(one, two):
+        assert torch.equal(a.codes, b.codes) and torch.equal(a.side, b.side)
+        dec = torch.empty((1, pages, 1, P, d), dtype=torch.float32, device="cuda")
+        cg.kv_decode(0 if a is one[0] else 1, a, Gd, shp, codec, 0, dec)
+        live = torch.nonzero(slots >= 0)[:, 0]
+        back = dec.view(-1, d)[slots[live].long()] - x[0 if a is one[0] else 1].view(-1, d)[live].float()
+        # half a step of a range of at most 12 deviations, in the 2-norm
+        assert float(back.norm(dim=-1).max()) <= 12 / (2 ** bits - 1) / 2 * math.sqrt(d)
