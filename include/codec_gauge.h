@@ -466,18 +466,18 @@ size_t attend_chunk_workspace_limit(cg_gauge_shape shp, int32_t nl, int32_t N, i
  *     o = softmax(scale q Khat^T) Vhat  over the positions t <= p with
  *                                       window == 0 or t > p - window or t < sinks,
  * Khat, Vhat as kv_decode would return them in binary32.  The first `sinks` positions stay visible behind the
- * window; window = 0: causal (sinks unused).  bf16 outputs are computed from operands of 11 bits (binary16;
- * rows of one token: of 16 bits or more) with binary32 sums, binary32 outputs from operands of 22 bits (error-free pools: below
- * 2^-18 of a step's largest value to within 2^-40 of it).  out must not overlap q.  Positions a token does not see do not reach its
- * output, whatever their bytes decode to; a NaN that it does see makes it NaN, an infinity what exp and the products make
- * of it (scores of -inf alone: zeros or NaN).  Tokens behind the
- * last row are left as they were.  A row whose lens is below n_b or above max_pages * page_size sets
- * CG_FLAG_POS_RANGE and gets zeros; a row whose cu runs backwards, past N or over max_q sets it and is left as it
- * was; a page outside the pool sets it and contributes nothing.
+ * window; window = 0: causal (sinks unused).  bf16 outputs are computed from operands of 11 bits (binary16) or
+ * more with binary32 sums, binary32 outputs from operands of 22 bits (of error-free pools: those below 2^-18 of the
+ * largest up to their step to within 2^-40 of it).  out must not overlap q.  Positions a token does
+ * not see do not reach its output, whatever their bytes decode to; a NaN that it does see makes it NaN, an infinity what
+ * exp and the products make of it (scores of -inf alone: zeros or NaN).  Tokens behind the last row are left as they
+ * were.  A row whose lens is below n_b or above max_pages * page_size sets CG_FLAG_POS_RANGE and gets zeros; a row whose
+ * cu runs backwards, past N or over max_q sets it and is left as it was; a page outside the pool sets it and
+ * contributes nothing.
  * Caches: page pools as in kv_attend_paged; max_pages * page_size at most 2^31 - 2^16.  No two elements of out
- * share an address (CG_ERR_ARG).  workspace: attend_chunk_workspace_bytes of these
- * arguments, 16-byte aligned; its size is the caller's to get right (the call cannot see it).  Calls sharing one
- * workspace on different streams race.  Errors: as kv_attend_paged. */
+ * share an address (CG_ERR_ARG).  workspace: attend_chunk_workspace_bytes of these arguments, 16-byte aligned; its size
+ * is the caller's to get right (the call cannot see it).  Calls sharing one workspace on different streams race.
+ * Errors: as kv_attend_paged. */
 int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const int32_t* cu, int32_t B, int32_t max_q,
                               const cg_cache* kc, const cg_cache* vc, const cg_page_table* pages, const void* G_dev,
                               cg_gauge_shape shp, const cg_codec* codec, const int32_t* lens, float scale,
