@@ -190,6 +190,9 @@ typedef struct cg_rope_plan {
   uint64_t step[128];
 } cg_rope_plan;
 
+/* Trees of drafted tokens: nodes of a batch row at most. */
+#define CG_TREE_MOST 1024
+
 /* Static message for a status code. */
 const char* cg_status_str(int32_t status);
 
@@ -483,6 +486,88 @@ int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const
                               cg_gauge_shape shp, const cg_codec* codec, const int32_t* lens, float scale,
                               int32_t window, int32_t sinks, const cg_kv_view* out, void* workspace,
                               int32_t* err_flag, void* stream);
+
+/* Shortens rows: row b keeps its first keep[b] positions (device int32 [B], 0 <= keep[b] <= lens[b]); the entries
+ * [ceil(keep / page_size), ceil(lens / page_size)) of its table are pushed on the pool's stack, row after row, and become
+ * -1, lens[b] becomes keep[b].  A row whose keep or lens is outside that range, or past its table, sets CG_FLAG_POS_RANGE
+ * and stays as it is.  Otherwise as kv_page_release.  Errors: as kv_page_map. */
+int32_t kv_page_trim(int32_t* lens, const int32_t* keep, int32_t B, const cg_page_pool* pool, int32_t* pages,
+                     int32_t max_pages, int32_t page_size, int32_t* err_flag, void* stream);
+
+/* A step that checks trees of drafted tokens: every row adds a tree (or several) of tokens behind the positions it
+ * holds, packed row after row as kv_page_map packs them (cu, lens and slots are its), the model runs once over all of
+ * them, and one path of each tree is kept.  parent: device int32 [N], the parent of a packed token as an index within its row's
+ * nodes (-1: a root), always an earlier node.  A row has at most CG_TREE_MOST nodes.  In order: kv_page_map, kv_tree_map,
+ * for every layer kv_append_rope and kv_attend_tree_paged, then kv_tree_accept (or a rule of the caller's), kv_tree_keep,
+ * kv_page_trim. */
+
+/* Positions and masks of trees, from their parents:
+ *   pos[i]   lens[b] - n_b + depth of the token's node (device int32 [N]; roots have depth 0)
+ *   mask[i]  bit j mod 64 of word j / 64: node j of the row is the token itself or one of its ancestors (device uint64
+ *            [N][words])
+ * with n_b = cu[b + 1] - cu[b] nodes and lens[b] positions held, the nodes among them (device int32 [B]).  Tokens behind the last row
+ * get pos -1 and mask 0.  A parent that is not an earlier node sets CG_FLAG_POS_RANGE and counts as -1; a row whose lens
+ * is below n_b sets it and gets pos -1; a row whose cu runs backwards, past N, or over min(64 words, CG_TREE_MOST) nodes
+ * sets it and is left as it was.  Errors: CG_ERR_ARG, CG_ERR_ALIGN, CG_ERR_DEVICE. */
+int32_t kv_tree_map(const int32_t* parent, const int32_t* cu, const int32_t* lens, int32_t B, int32_t N, int32_t words,
+                    int32_t* pos, uint64_t* mask, int32_t* err_flag, void* stream);
+
+/* kv_rope of keys and queries and kv_append_slots in one call: token i of k_new, v_new [l1 - l0][1][H][N][d] goes to
+ * slots[i], its key turned by pos[i] (device int32 [N]) as `plan` says, with no rounding between turn and gauge; q
+ * [l1 - l0][1][Hq][N][d] turned likewise into q_out (both or neither NULL; q_out may be q itself, else they must not
+ * overlap; one element type).  A token with a negative position is left out: nothing is appended, its row of q_out stays what it was.
+ * A negative slot leaves out the append alone.  The rotation is kv_rope's, slots, pools and codes as in
+ * kv_append_slots.  Errors: as kv_rope and kv_append_slots. */
+int32_t kv_append_rope(int32_t l0, int32_t l1, const cg_rope_plan* plan, const cg_kv_view* k_new,
+                       const cg_kv_view* v_new, const cg_kv_view* q, const cg_kv_view* q_out, const int32_t* pos,
+                       const int32_t* slots, const void* G_dev, cg_gauge_shape shp, const cg_codec* codec,
+                       const cg_cache* kc, const cg_cache* vc, int32_t* err_flag, void* stream);
+
+/* Workspace bytes that every kv_attend_tree_paged call of this gauge shape, Hq and page_size stays within while it has at
+ * most nl layers, N packed tokens, B rows and max_pages pages a row, whatever its max_q, window and sinks (0: none of
+ * them needs any, or invalid arguments). */
+size_t attend_tree_workspace_bytes(cg_gauge_shape shp, int32_t nl, int32_t N, int32_t B, int32_t Hq, int32_t max_pages,
+                                   int32_t page_size);
+
+/* kv_attend_chunk_paged for trees: which of its row's new tokens a token sees is a mask's to say.  Row b's token i, of
+ * n_b, with base = lens[b] - n_b positions held before them, sees
+ *   positions t < base    with  window == 0 or t > p - window or t < sinks,   p = max(pos[i], base),
+ *   positions base + j    with  bit j of its mask set, j < n_b (itself only if its own bit is),
+ * so a tree's masks (kv_tree_map) give every node what it would see at the end of its own path.  mask: device uint64
+ * [N][words], words >= ceil(max_q / 64), 8-byte aligned.  pos: device int32 [N] (NULL if window is 0).  The window hides no node.  A token
+ * that sees nothing gets zeros.  Everything else as kv_attend_chunk_paged; max_q at most CG_TREE_MOST.  workspace: as
+ * attend_tree_workspace_bytes says, 16-byte aligned.  Errors: as kv_attend_chunk_paged. */
+int32_t kv_attend_tree_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const int32_t* cu, int32_t B, int32_t max_q,
+                             const uint64_t* mask, int32_t words, const int32_t* pos, const cg_cache* kc,
+                             const cg_cache* vc, const cg_page_table* pages, const void* G_dev, cg_gauge_shape shp,
+                             const cg_codec* codec, const int32_t* lens, float scale, int32_t window, int32_t sinks,
+                             const cg_kv_view* out, void* workspace, int32_t* err_flag, void* stream);
+
+/* Greedy check of trees: from each row's root on, the lowest child whose draft is what the model chose after its parent.
+ * draft, target: device int32 [N], a node's own token and the model's choice after it.  head: device int32 [B], the
+ * model's choice after the positions held before (a root is kept if it drafts that), or NULL: the first root is kept.  Writes
+ *   path[cu[b] + j], j < kept[b]   the kept nodes of row b in order, -1 from there to the row's end (device int32 [N])
+ *   kept[b]                        their number (device int32 [B])
+ *   next[b]                        the model's choice after the last of them (none: head[b], or -1; device int32 [B])
+ * and path -1 behind the last row.  A parent that is not an earlier node sets CG_FLAG_POS_RANGE, its node is not kept; a row whose cu
+ * runs backwards, past N or over CG_TREE_MOST nodes sets it, gets kept 0 and next -1, and its path is left as it was.
+ * Errors: CG_ERR_ARG, CG_ERR_ALIGN, CG_ERR_DEVICE. */
+int32_t kv_tree_accept(const int32_t* parent, const int32_t* cu, const int32_t* draft, const int32_t* target,
+                       const int32_t* head, int32_t B, int32_t N, int32_t* path, int32_t* kept, int32_t* next,
+                       int32_t* err_flag, void* stream);
+
+/* Moves kept paths together: for layers [l0, l1) and every head of both pools, the entry of row b's position
+ * base + path[cu[b] + j] (base = lens[b] - n_b) goes to position base + j, j < kept[b], bit for bit; what was written behind them
+ * stays, and is no part of the row once it is trimmed.  path as kv_tree_accept writes it: ascending nodes.  held[b] (device int32 [B], not
+ * lens itself) becomes base + kept[b], what kv_page_trim takes.  lens is not modified.  A row whose kept is negative or
+ * above n_b, whose path does not ascend within the row, whose lens is below n_b or past its table, or whose cu is as in
+ * kv_tree_accept, sets CG_FLAG_POS_RANGE and moves nothing; held[b] becomes base (lens[b] where that is not known).  A
+ * page outside the pool sets it and its entries are not moved.  Caches: page pools as in kv_attend_paged, no page in two rows'
+ * tables from base on.  Errors: CG_ERR_ARG, CG_ERR_SHAPE, CG_ERR_ALIGN, CG_ERR_UNSUPPORTED, CG_ERR_CAPACITY, CG_ERR_DEVICE. */
+int32_t kv_tree_keep(int32_t l0, int32_t l1, const int32_t* path, const int32_t* kept, const int32_t* cu,
+                     const int32_t* lens, int32_t B, int32_t N, const cg_page_table* pages, cg_gauge_shape shp,
+                     const cg_codec* codec, const cg_cache* kc, const cg_cache* vc, int32_t* held, int32_t* err_flag,
+                     void* stream);
 
 /* Device self-test of the two binary32 steps of the quantiser the kernels compute without a
  * division (section 4.3 block range; the oracle divides): which = 0 compares the reciprocal

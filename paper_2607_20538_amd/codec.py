@@ -24,6 +24,7 @@ PASSTHROUGH, BLOCK_UNIFORM, KIVI, ZFP = 0, 1, 2, 3
 DTYPE_BF16, DTYPE_F32 = 0, 1
 ROPE_HALF, ROPE_PAIRS = 0, 1
 ROPE_NONE, ROPE_LINEAR, ROPE_RAMP = 0, 1, 2
+TREE_MOST = 1024  # nodes of a row's trees
 
 EXPORTS = ["cg_status_str", "gauge_device_bytes", "gauge_make", "cache_bytes", "kv_encode", "kv_decode",
            "kv_append_step", "spectral_workspace_bytes", "kv_spectral_stats", "gauge_grad_workspace_bytes",
@@ -31,8 +32,9 @@ EXPORTS = ["cg_status_str", "gauge_device_bytes", "gauge_make", "cache_bytes", "
            "kv_attend_noalloc",
            "attend_paged_workspace_bytes", "kv_attend_paged", "kv_encode_paged", "kv_append_paged",
            "kv_page_map", "kv_page_release", "rope_make", "kv_rope", "kv_append_slots",
-           "attend_chunk_workspace_bytes", "attend_chunk_workspace_limit", "kv_attend_chunk_paged", "cg_selftest",
-           "cg_stream_probe"]
+           "attend_chunk_workspace_bytes", "attend_chunk_workspace_limit", "kv_attend_chunk_paged",
+           "kv_page_trim", "kv_tree_map", "kv_append_rope", "attend_tree_workspace_bytes", "kv_attend_tree_paged",
+           "kv_tree_accept", "kv_tree_keep", "cg_selftest", "cg_stream_probe"]
 
 
 class GaugeShape(C.Structure):
@@ -158,6 +160,25 @@ def lib() -> C.CDLL:
                                             C.POINTER(CacheStruct), C.POINTER(PageTable), p, GaugeShape,
                                             C.POINTER(CodecStruct), p, C.c_float, i32, i32, C.POINTER(KvView), p, p, p]
         L.kv_attend_chunk_paged.restype = i32
+        L.kv_page_trim.argtypes = L.kv_page_release.argtypes
+        L.kv_page_trim.restype = i32
+        L.kv_tree_map.argtypes = [p, p, p, i32, i32, i32, p, p, p, p]
+        L.kv_tree_map.restype = i32
+        L.kv_append_rope.argtypes = [i32, i32, C.POINTER(RopePlan), C.POINTER(KvView), C.POINTER(KvView),
+                                     C.POINTER(KvView), C.POINTER(KvView), p, p, p, GaugeShape, C.POINTER(CodecStruct),
+                                     C.POINTER(CacheStruct), C.POINTER(CacheStruct), p, p]
+        L.kv_append_rope.restype = i32
+        L.attend_tree_workspace_bytes.argtypes = [GaugeShape] + [i32] * 6
+        L.attend_tree_workspace_bytes.restype = C.c_size_t
+        L.kv_attend_tree_paged.argtypes = [i32, i32, C.POINTER(KvView), p, i32, i32, p, i32, p, C.POINTER(CacheStruct),
+                                           C.POINTER(CacheStruct), C.POINTER(PageTable), p, GaugeShape,
+                                           C.POINTER(CodecStruct), p, C.c_float, i32, i32, C.POINTER(KvView), p, p, p]
+        L.kv_attend_tree_paged.restype = i32
+        L.kv_tree_accept.argtypes = [p, p, p, p, p, i32, i32, p, p, p, p, p]
+        L.kv_tree_accept.restype = i32
+        L.kv_tree_keep.argtypes = [i32, i32, p, p, p, p, i32, i32, C.POINTER(PageTable), GaugeShape,
+                                   C.POINTER(CodecStruct), C.POINTER(CacheStruct), C.POINTER(CacheStruct), p, p, p]
+        L.kv_tree_keep.restype = i32
         L.cg_selftest.argtypes = [i32, p, p]
         L.cg_selftest.restype = i32
         L.cg_stream_probe.argtypes = [p, C.c_int64, p, C.c_int64, p]
@@ -588,3 +609,144 @@ def kv_attend_chunk_paged(l0: int, l1: int, q, cu, max_q: int, kc: Cache, vc: Ca
                                      _ptr(G_dev), shp, C.byref(cs), _ptr(lens), float(scale), window, sinks,
                                      C.byref(ov), _ptr(workspace), _ptr(err_flag), _stream(stream))
     _check("kv_attend_chunk_paged", rc)
+
+
+# ------------------------------------------------------------------------------------------
+# a step that checks trees of drafted tokens
+# ------------------------------------------------------------------------------------------
+
+def kv_page_trim(lens, keep, pool: PagePool, pages, page_size: int, err_flag=None, stream=None):
+    """Row b keeps its first keep[b] positions (int32 [B]): the pages past them go back to `pool`, lens[b] becomes keep[b]."""
+    _on_device("kv_page_trim", lens=lens, keep=keep, free=pool.free, count=pool.count, pages=pages, err_flag=err_flag)
+    B = lens.numel()
+    if pages.dim() != 2 or pages.shape[0] != B:
+        raise ValueError("kv_page_trim: pages must be [B][max_pages]")
+    _int32("kv_page_trim", B, lens=lens, keep=keep)
+    _int32("kv_page_trim", None, pages=pages)
+    ps = pool.struct()
+    rc = lib().kv_page_trim(_ptr(lens), _ptr(keep), B, C.byref(ps), _ptr(pages), pages.shape[1], page_size, _ptr(err_flag),
+                            _stream(stream))
+    _check("kv_page_trim", rc)
+
+
+_int64_type = None
+
+
+def _mask(fn: str, mask, N: int) -> int:
+    """Words of a token's mask: a contiguous int64 tensor [N][words]."""
+    global _int64_type
+    if _int64_type is None:
+        import torch
+
+        _int64_type = torch.int64
+    if mask.dtype != _int64_type or mask.dim() != 2 or mask.shape[0] != N or not mask.is_contiguous():
+        raise ValueError(f"{fn}: mask must be a contiguous int64 tensor [{N}][words]")
+    return mask.shape[1]
+
+
+def kv_tree_map(parent, cu, lens, pos, mask, err_flag=None, stream=None):
+    """Positions pos (int32 [N]) and masks (int64 [N][words]: bit j mod 64 of word j / 64 for the node itself and its
+    ancestors) of the packed trees whose nodes' parents (int32 [N], indices within the row, -1: a root) are `parent`;
+    row b's nodes are cu[b] .. cu[b + 1], the last of its lens[b] positions."""
+    _on_device("kv_tree_map", parent=parent, cu=cu, lens=lens, pos=pos, mask=mask, err_flag=err_flag)
+    B, N = lens.numel(), parent.numel()
+    _int32("kv_tree_map", N, parent=parent, pos=pos)
+    _int32("kv_tree_map", B, lens=lens)
+    _int32("kv_tree_map", B + 1, cu=cu)
+    words = _mask("kv_tree_map", mask, N)
+    rc = lib().kv_tree_map(_ptr(parent), _ptr(cu), _ptr(lens), B, N, words, _ptr(pos), _ptr(mask), _ptr(err_flag),
+                           _stream(stream))
+    _check("kv_tree_map", rc)
+
+
+def kv_append_rope(l0: int, l1: int, plan: RopePlan, k_new, v_new, pos, slots, G_dev, shp: GaugeShape, codec: Codec,
+                   kc: Cache, vc: Cache, q=None, q_out=None, err_flag=None, stream=None):
+    """Encodes packed tokens k_new, v_new [l1-l0][1][H][N][d] into the page pools kc, vc at slots (int32 [N]; negative:
+    skipped), the keys turned by pos (int32 [N]; negative: the token is left out) before the gauge, and turns q
+    [l1-l0][1][Hq][N][d] into q_out (may be q)."""
+    _on_device("kv_append_rope", k_new=k_new, v_new=v_new, pos=pos, slots=slots, G_dev=G_dev, codes=kc.codes, v_codes=vc.codes,
+               q=q, q_out=q_out, err_flag=err_flag)
+    _int32("kv_append_rope", k_new.shape[3], pos=pos, slots=slots)
+    kn, vn, cs, kcs, vcs = view(k_new), view(v_new), codec.struct(), kc.struct(), vc.struct()
+    qv = None if q is None else C.byref(view(q))
+    qo = None if q_out is None else C.byref(view(q_out))
+    rc = lib().kv_append_rope(l0, l1, C.byref(plan), C.byref(kn), C.byref(vn), qv, qo, _ptr(pos), _ptr(slots), _ptr(G_dev),
+                              shp, C.byref(cs), C.byref(kcs), C.byref(vcs), _ptr(err_flag), _stream(stream))
+    _check("kv_append_rope", rc)
+
+
+def attend_tree_workspace_bytes(shp: GaugeShape, nl: int, N: int, B: int, Hq: int, max_pages: int, page_size: int) -> int:
+    """Bytes that every kv_attend_tree_paged call of at most these sizes stays within."""
+    return int(lib().attend_tree_workspace_bytes(shp, nl, N, B, Hq, max_pages, page_size))
+
+
+def kv_attend_tree_paged(l0: int, l1: int, q, cu, max_q: int, mask, kc: Cache, vc: Cache, pt: PageTable, G_dev,
+                         shp: GaugeShape, codec: Codec, lens, scale: float, out, pos=None, window: int = 0, sinks: int = 0,
+                         workspace=None, err_flag=None, stream=None):
+    """Attention of the packed tokens q [l1-l0][1][Hq][N][d] (row b's: cu[b] .. cu[b+1], at most max_q) over page pools that
+    hold them: all of what the row held before them (behind a window by the tokens' pos, int32 [N], the first `sinks` stay
+    visible) and of its new tokens those whose bits are set in a token's mask (int64 [N][words]); lens: int32 [B] positions
+    held with the new tokens.  Writes out (q's shape)."""
+    _on_device("kv_attend_tree_paged", q=q, cu=cu, mask=mask, pos=pos, codes=kc.codes, v_codes=vc.codes, G_dev=G_dev, lens=lens,
+               out=out, workspace=workspace, err_flag=err_flag)
+    B = lens.numel()
+    _int32("kv_attend_tree_paged", B, lens=lens)
+    _int32("kv_attend_tree_paged", B + 1, cu=cu)
+    qv, ov, cs, kcs, vcs = view(q), view(out), codec.struct(), kc.struct(), vc.struct()
+    words = _mask("kv_attend_tree_paged", mask, qv.T)
+    if pos is not None:
+        _int32("kv_attend_tree_paged", qv.T, pos=pos)
+    table = getattr(pt, "tensor", None)
+    if table is not None:
+        _on_device("kv_attend_tree_paged", pages=table)
+        if table.shape[0] != B:
+            raise ValueError(f"kv_attend_tree_paged: a page table of {table.shape[0]} rows, {B} lens")
+    if workspace is not None:
+        need = attend_tree_workspace_bytes(shp, l1 - l0, qv.T, B, qv.H, pt.max_pages, pt.page_size)
+        if workspace.nbytes < need:
+            raise ValueError(f"kv_attend_tree_paged: workspace of {workspace.nbytes} bytes, {need} needed")
+    rc = lib().kv_attend_tree_paged(l0, l1, C.byref(qv), _ptr(cu), B, max_q, _ptr(mask), words, _ptr(pos), C.byref(kcs),
+                                    C.byref(vcs), C.byref(pt), _ptr(G_dev), shp, C.byref(cs), _ptr(lens), float(scale), window,
+                                    sinks, C.byref(ov), _ptr(workspace), _ptr(err_flag), _stream(stream))
+    _check("kv_attend_tree_paged", rc)
+
+
+def kv_tree_accept(parent, cu, draft, target, path, kept, next, head=None, err_flag=None, stream=None):
+    """Greedy check of packed trees: from each row's root on the lowest child whose draft (int32 [N]) is the model's choice
+    (target, int32 [N]) after its parent; head: its choice before the roots (int32 [B]; None: the first root is kept).
+    Writes the kept nodes to path (int32 [N], -1 behind them), their number to kept and the choice after them to next (int32 [B])."""
+    _on_device("kv_tree_accept", parent=parent, cu=cu, draft=draft, target=target, path=path, kept=kept, next=next, head=head,
+               err_flag=err_flag)
+    B, N = kept.numel(), parent.numel()
+    _int32("kv_tree_accept", N, parent=parent, draft=draft, target=target, path=path)
+    _int32("kv_tree_accept", B, kept=kept, next=next)
+    _int32("kv_tree_accept", B + 1, cu=cu)
+    if head is not None:
+        _int32("kv_tree_accept", B, head=head)
+    rc = lib().kv_tree_accept(_ptr(parent), _ptr(cu), _ptr(draft), _ptr(target), _ptr(head), B, N, _ptr(path), _ptr(kept),
+                              _ptr(next), _ptr(err_flag), _stream(stream))
+    _check("kv_tree_accept", rc)
+
+
+def kv_tree_keep(l0: int, l1: int, path, kept, cu, lens, pt: PageTable, codec: Codec, kc: Cache, vc: Cache, held,
+                 err_flag=None, stream=None):
+    """Moves the entries of each row's kept nodes (path, kept: as kv_tree_accept writes them) of both pools to the first places
+    behind what the row held before its cu[b + 1] - cu[b] nodes; held (int32 [B]) becomes the positions it then holds, for
+    kv_page_trim (lens stay as they are)."""
+    _on_device("kv_tree_keep", path=path, kept=kept, cu=cu, lens=lens, held=held, codes=kc.codes, v_codes=vc.codes,
+               err_flag=err_flag)
+    B, N = lens.numel(), path.numel()
+    _int32("kv_tree_keep", N, path=path)
+    _int32("kv_tree_keep", B, kept=kept, lens=lens, held=held)
+    _int32("kv_tree_keep", B + 1, cu=cu)
+    table = getattr(pt, "tensor", None)
+    if table is not None:
+        _on_device("kv_tree_keep", pages=table)
+        if table.shape[0] != B:
+            raise ValueError(f"kv_tree_keep: a page table of {table.shape[0]} rows, {B} lens")
+    cs, kcs, vcs = codec.struct(), kc.struct(), vc.struct()
+    # (no gauge is read: any group size says the pools' shape)
+    shp = GaugeShape(kc.L, kc.H, kc.d, kc.d)
+    rc = lib().kv_tree_keep(l0, l1, _ptr(path), _ptr(kept), _ptr(cu), _ptr(lens), B, N, C.byref(pt), shp, C.byref(cs),
+                            C.byref(kcs), C.byref(vcs), _ptr(held), _ptr(err_flag), _stream(stream))
+    _check("kv_tree_keep", rc)

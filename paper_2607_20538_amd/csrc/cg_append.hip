@@ -9,9 +9,12 @@
 // its loads are in flight together.  Measured on MI355X, K and V of one layer of 8 heads, d = g = 128,
 // batch 1: 41 us in two launches (a 128-step chain of dependent 4-byte-per-lane loads and a block
 // quantised by one thread) -> 7 us in one.
+#include <type_traits>
+
 #include "cg_internal.h"
 #include "cg_device.h"
 #include "cg_general.h"
+#include "cg_rope.h"
 
 namespace cg {
 
@@ -27,6 +30,12 @@ struct AppendArgs {
   int* err;
   PageDev pt;
   bool slots;      // pos holds pool slots: page * T_cap + position, negative: no token
+};
+
+// ... and the rotation of the keys
+struct AppendRopeArgs : AppendArgs {
+  const int* turn;  // positions that the keys turn by (negative: no token)
+  cg_rope_plan plan;
 };
 
 // Cache batch row and position inside it of batch row b's new token at position p of the row; false
@@ -52,8 +61,9 @@ __device__ __forceinline__ bool token_slot(const AppendArgs& a, const CacheDev& 
 // Per-token blocks and the error-free backend: workgroup (layer and head, 16 batch rows, K or V).
 constexpr int kRows = 16;
 
-template <int KR, int NBW>
-__global__ __launch_bounds__(kThreads) void append_rows(AppendArgs a) {
+// ROPE: the keys turn by their positions before the gauge, in binary32 in the tile (no rounding between the two).
+template <int KR, int NBW, bool ROPE>
+__global__ __launch_bounds__(kThreads) void append_rows(std::conditional_t<ROPE, AppendRopeArgs, AppendArgs> a) {
   extern __shared__ float sm[];
   __shared__ int64_t rowi[kRows];  // cache token row of each batch row, or -1
   const int s = blockIdx.z;
@@ -71,6 +81,10 @@ __global__ __launch_bounds__(kThreads) void append_rows(AppendArgs a) {
   GaugeRaw<(KR > 0 ? KR : 4), NBW> raw;
   const WaveTile wt = wave_tile<NBW>(d);
   const int pv = a.pos[min(b0 + (tid & (kRows - 1)), X.B - 1)];
+  __shared__ int turns[ROPE ? kRows : 1];
+  if constexpr (ROPE) {
+    if (tid < kRows) turns[tid] = a.turn[min(b0 + tid, X.B - 1)];
+  }
   if constexpr (KR > 0) load_gauge_rows<KR, NBW>(raw, a.G, l, s, h, wt);
   // the tokens' channels, 8 per lane (at most 2 x 8: 16 rows of 256 channels); rows past the batch
   // repeat its last one and are not stored
@@ -90,6 +104,9 @@ __global__ __launch_bounds__(kThreads) void append_rows(AppendArgs a) {
   }
   if (tid < kRows) {
     int row, p = pv;
+    if constexpr (ROPE) {
+      if (turns[tid] < 0) p = -1;
+    }
     rowi[tid] = tid < nr && token_slot(a, k, b0 + tid, row, p)
                     ? int64_t((size_t(l) * k.B + row) * k.H + h) * k.T_cap + p
                     : int64_t(-1);
@@ -114,6 +131,23 @@ __global__ __launch_bounds__(kThreads) void append_rows(AppendArgs a) {
       for (int e = 0; e < 8; ++e)
         if (!isfinite(x[i][e])) flags |= CG_FLAG_NONFINITE;
     }
+  }
+  if constexpr (ROPE) {
+    if (s == 0) {
+      const int pairs = a.plan.d_rot / 2;
+      for (int idx = tid; idx < nr * pairs; idx += kThreads) {
+        const int t = idx / pairs, i = idx - t * pairs;
+        if (rowi[t] < 0) continue;
+        int c0, c1;
+        float sn, cn;
+        pair_channels(a.plan, i, c0, c1);
+        pair_turn(a.plan, i, turns[t], sn, cn);
+        const float x0 = xs[t * dp + c0], x1 = xs[t * dp + c1];
+        xs[t * dp + c0] = fmaf(x0, cn, -(x1 * sn));
+        xs[t * dp + c1] = fmaf(x0, sn, x1 * cn);
+      }
+    }
+    __syncthreads();
   }
   if constexpr (KR > 0) {
     float A[NBW][KR];
@@ -245,8 +279,8 @@ __global__ __launch_bounds__(kThreads) void append_staged(AppendArgs a) {
 
 hipError_t launch_append(const ViewDev& Kn, const ViewDev& Vn, int l0, const int* pos, const GaugeDev& G,
                          const CodecDev& c, const CacheDev& kc, const CacheDev& vc, int* err, hipStream_t st,
-                         const PageDev& pt, bool slots) {
-  AppendArgs a;
+                         const PageDev& pt, bool slots, const int* turn, const cg_rope_plan* plan) {
+  AppendRopeArgs a;
   a.slots = slots;
   a.x[0] = Kn; a.x[1] = Vn;
   a.k[0] = kc; a.k[1] = vc;
@@ -256,6 +290,8 @@ hipError_t launch_append(const ViewDev& Kn, const ViewDev& Vn, int l0, const int
   a.c = c;
   a.err = err;
   a.pt = pt;
+  a.turn = turn;
+  if (turn) a.plan = *plan;
   const int d = Kn.d, dp = d + kPad;
   const bool kivi = c.backend == CG_BACKEND_KIVI, staged = kivi || c.bt > 1;
   // codes of a staged tile: the widest row a codec can have (passthrough writes from the tile)
@@ -265,10 +301,12 @@ hipError_t launch_append(const ViewDev& Kn, const ViewDev& Vn, int l0, const int
   const dim3 grid = staged ? dim3(Kn.L * Kn.B * Kn.H, 1, 2) : dim3(Kn.L * Kn.H, (Kn.B + kRows - 1) / kRows, 2);
   return by_gauge(G.g, d, [&](auto kr, auto nbw) {
     constexpr int KR = decltype(kr)::value, NBW = decltype(nbw)::value;
-    const void* fn = staged ? (const void*)append_staged<KR, NBW> : (const void*)append_rows<KR, NBW>;
+    const void* fn = staged ? (const void*)append_staged<KR, NBW>
+                            : (turn ? (const void*)append_rows<KR, NBW, true> : (const void*)append_rows<KR, NBW, false>);
     hipError_t e = set_smem(fn, smem);
     if (e != hipSuccess) return e;
-    void* args[] = {&a};
+    AppendArgs& plain = a;
+    void* args[] = {turn ? static_cast<void*>(&a) : static_cast<void*>(&plain)};
     return hipLaunchKernel(fn, grid, dim3(kThreads), args, smem, st);
   });
 }

@@ -19,6 +19,10 @@ struct ChunkDev {
   int cap;               // positions a row can hold
   int tq, heads, nqc, ntile, nsplit;  // the plan
   float *part, *ml;      // splits: [nl][nsplit][N][Hq][d], [nl][nsplit][N][Hq][2] (maximum, sum)
+  // trees: which of its row's new tokens a token sees (device [N][words]), what its window goes by (device [N])
+  const uint64_t* mask = nullptr;
+  const int* pos = nullptr;
+  int words = 0;
   int* err;
 };
 
@@ -48,5 +52,10 @@ hipError_t run_chunk_128(const ChunkDev& a, const GaugeDev& G, const CodecDev& c
 hipError_t run_chunk_256(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st);
 hipError_t run_chunk_f32(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st);
 hipError_t launch_chunk(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, hipStream_t st);
+// ... with masks
+hipError_t run_tree_64(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st);
+hipError_t run_tree_128(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st);
+hipError_t run_tree_256(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st);
+hipError_t run_tree_f32(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st);
 
 }  // namespace cg

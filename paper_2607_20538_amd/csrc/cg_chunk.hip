@@ -107,10 +107,11 @@ hipError_t launch_chunk(const ChunkDev& a, const GaugeDev& G, const CodecDev& c,
   const int d = a.q.d;
   const bool wide = !a.o.bf16;  // binary32 results
   hipError_t e;
-  if (wide) e = run_chunk_f32(a, G, c, int(blocks), st);
-  else if (d <= 64) e = run_chunk_64(a, G, c, int(blocks), st);
-  else if (d <= 128) e = run_chunk_128(a, G, c, int(blocks), st);
-  else e = run_chunk_256(a, G, c, int(blocks), st);
+  const bool tree = a.mask != nullptr;
+  if (wide) e = (tree ? run_tree_f32 : run_chunk_f32)(a, G, c, int(blocks), st);
+  else if (d <= 64) e = (tree ? run_tree_64 : run_chunk_64)(a, G, c, int(blocks), st);
+  else if (d <= 128) e = (tree ? run_tree_128 : run_chunk_128)(a, G, c, int(blocks), st);
+  else e = (tree ? run_tree_256 : run_chunk_256)(a, G, c, int(blocks), st);
   if (e != hipSuccess || a.nsplit == 1) return e;
   const int per = std::min(65535, (a.tq * a.Hq + 3) / 4);
   hipLaunchKernelGGL(chunk_join, dim3(a.ntile * a.q.L, per), dim3(256), 0, st, a);

@@ -36,6 +36,7 @@
 #include "cg_chunk.h"
 #include "cg_chunk_rows.h"
 #include "cg_mfma_util.h"
+#include "cg_tree_mask.h"
 
 namespace cg {
 
@@ -240,7 +241,8 @@ struct ChunkShape {
   static_assert(VP % 64 == 0 && kStep * KP % 64 == 0, "V runs on multiples of 64 bytes");
 };
 
-template <int D, int PL, int BITS>
+// TREE: the row's new tokens see each other as a.mask says (cg_tree_mask.h), and all of them what the row held.
+template <int D, int PL, int BITS, bool TREE>
 __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_attend(ChunkDev a, GaugeDev G, CodecDev c) {
   using SH = ChunkShape<D, PL>;
   constexpr bool WIDE = BITS >= 0, PASS = BITS == kErrorFree;
@@ -278,7 +280,9 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
     if (tid == 0 && a.err) atomicOr(a.err, CG_FLAG_POS_RANGE);
     held = 0;
   }
-  const int pa = held - qt.n + qt.i0, pb = pa + ntok - 1;  // positions of the tile's tokens
+  const int base = held - qt.n;  // positions before the new tokens
+  // positions of the tile's tokens (TREE: what they see lies between the first's window and the row's end)
+  const int pa = TREE ? base : base + qt.i0, pb = TREE ? held - 1 : pa + ntok - 1;
   // steps: those that hold sinks before the window, then from the window's first position to the last token
   int lo_t = 0, sink_t = 0, nstep = 0;
   if (!bad_row) {
@@ -294,10 +298,17 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
   // this lane's query (columns past the tile repeat its last one and are not stored)
   const int r = min(32 * w + n, rows - 1);
   const int tok = r / nh, jj = r - tok * nh;
-  const int pq = pa + tok;
+  int pq = pa + tok;
+  const uint64_t* nodes = nullptr;  // TREE: the mask of the lane's token
+  if constexpr (TREE) {
+    const size_t at = size_t(qt.tok0) + qt.i0 + tok;
+    nodes = a.mask + at * a.words;
+    pq = a.window > 0 ? max(a.pos[at], base) : base;
+  }
   const int plow = a.window > 0 ? max(pq - a.window, -1) : -1;   // positions up to here are hidden unless a sink
   // the first and last position of the wave's queries
-  const int wlo = pa + min(32 * w, rows - 1) / nh, whi = pa + min(32 * w + 31, rows - 1) / nh;
+  const int wlo = TREE ? base - 1 : pa + min(32 * w, rows - 1) / nh;
+  const int whi = TREE ? wave_most(pq) : pa + min(32 * w + 31, rows - 1) / nh;
   const bool idle = 32 * w >= rows;                     // a wave without queries only moves codes and gauges
   const size_t qoff = size_t(lv) * a.q.sl + size_t(h * a.grp + j0 + jj) * a.q.sh + size_t(qt.tok0 + qt.i0 + tok) * a.q.st;
 
@@ -879,7 +890,12 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
         // bit c: position t0 + 4 hc + c is seen; element (ps, e) is bit 32 ps + 8 (e / 4) + e % 4
         const int t1 = t0 + 4 * hc;
         auto below = [](int x) { return x <= 0 ? 0ull : (x >= 64 ? ~0ull : (1ull << x) - 1ull); };
-        const uint64_t seen = blank ? 0ull : below(pq - t1 + 1) & (~below(plow - t1 + 1) | below(a.sinks - t1));
+        uint64_t seen = 0;
+        if constexpr (TREE) {
+          if (!blank) seen = tree_seen(nodes, a.words, base, held, plow, a.sinks, t1);
+        } else {
+          seen = blank ? 0ull : below(pq - t1 + 1) & (~below(plow - t1 + 1) | below(a.sinks - t1));
+        }
         const uint32_t half[2] = {uint32_t(seen), uint32_t(seen >> 32)};
 #pragma unroll
         for (int ps = 0; ps < 2; ++ps)
@@ -990,7 +1006,8 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
           const float* kr = krows + u * D;
           const float* vr = vrows + u * D;
           const int t = t0 + s0 + u;
-          const bool seen = t <= pq && (t > plow || t < a.sinks);
+          const bool seen = TREE ? (tree_seen(nodes, a.words, base, held, plow, a.sinks, t) & 1) != 0
+                                 : t <= pq && (t > plow || t < a.sinks);
           float s = 0.0f;
 #pragma unroll
           for (int kk = 0; kk < KK; ++kk) {
@@ -1099,9 +1116,9 @@ __global__ __launch_bounds__(64 * NW, D <= 128 && PL == 1 ? 2 : 1) void chunk_at
   }
 }
 
-template <int D, int PL, int BITS>
+template <int D, int PL, int BITS, bool TREE>
 hipError_t run_chunk(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st) {
-  const void* fn = reinterpret_cast<const void*>(chunk_attend<D, PL, BITS>);
+  const void* fn = reinterpret_cast<const void*>(chunk_attend<D, PL, BITS, TREE>);
   const int smem = ChunkShape<D, PL>::all;
   if (smem > 65536) {
     const hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, smem);
@@ -1115,20 +1132,20 @@ hipError_t run_chunk(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, in
 }
 
 // EACH: a kernel for each code width (else one that reads it at run time)
-template <int D, int PL, bool EACH>
+template <int D, int PL, bool EACH, bool TREE = false>
 hipError_t by_layout(const ChunkDev& a, const GaugeDev& G, const CodecDev& c, int blocks, hipStream_t st) {
-  if (c.backend == CG_BACKEND_PASSTHROUGH) return run_chunk<D, PL, kErrorFree>(a, G, c, blocks, st);
-  if (!chunk_wide(c, a.q.d)) return run_chunk<D, PL, kAnyLayout>(a, G, c, blocks, st);
+  if (c.backend == CG_BACKEND_PASSTHROUGH) return run_chunk<D, PL, kErrorFree, TREE>(a, G, c, blocks, st);
+  if (!chunk_wide(c, a.q.d)) return run_chunk<D, PL, kAnyLayout, TREE>(a, G, c, blocks, st);
   if constexpr (EACH) {
     switch (c.bits) {
-      case 2: return run_chunk<D, PL, 2>(a, G, c, blocks, st);
-      case 3: return run_chunk<D, PL, 3>(a, G, c, blocks, st);
-      case 4: return run_chunk<D, PL, 4>(a, G, c, blocks, st);
-      case 6: return run_chunk<D, PL, 6>(a, G, c, blocks, st);
-      default: return run_chunk<D, PL, 8>(a, G, c, blocks, st);
+      case 2: return run_chunk<D, PL, 2, TREE>(a, G, c, blocks, st);
+      case 3: return run_chunk<D, PL, 3, TREE>(a, G, c, blocks, st);
+      case 4: return run_chunk<D, PL, 4, TREE>(a, G, c, blocks, st);
+      case 6: return run_chunk<D, PL, 6, TREE>(a, G, c, blocks, st);
+      default: return run_chunk<D, PL, 8, TREE>(a, G, c, blocks, st);
     }
   } else {
-    return run_chunk<D, PL, 0>(a, G, c, blocks, st);
+    return run_chunk<D, PL, 0, TREE>(a, G, c, blocks, st);
   }
 }
 

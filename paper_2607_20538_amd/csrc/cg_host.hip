@@ -382,6 +382,7 @@ int32_t check_apart(const cg_kv_view* v) {
 }
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
 
 // A query or output view of kv_attend: [nl][B][Hq][1][d], Hq a multiple of the KV heads.
 int32_t check_qview(const cg_kv_view* v, const cg_gauge_shape& s, int L) {
@@ -431,9 +432,9 @@ hipError_t launch_decode(int s, const CacheDev& k, int l0, const GaugeDev& G, co
 // 512.  Below, they are even: both are the launch and one chain of loads.
 static hipError_t launch_append_slots(const ViewDev& Kn, const ViewDev& Vn, int l0, const int* slots, const GaugeDev& G,
                                       const CodecDev& c, const CacheDev& kc, const CacheDev& vc, int* err,
-                                      hipStream_t st) {
+                                      hipStream_t st, const int* turn = nullptr, const cg_rope_plan* plan = nullptr) {
   constexpr int64_t kEncodeRows = 4096;  // token rows, all layers and heads
-  if (!force_generic() && int64_t(Kn.T) * Kn.L * Kn.H >= kEncodeRows && mfma_encode_supported(Kn, G, c, true) &&
+  if (!turn && !force_generic() && int64_t(Kn.T) * Kn.L * Kn.H >= kEncodeRows && mfma_encode_supported(Kn, G, c, true) &&
       mfma_encode_supported(Vn, G, c, true))
     return launch_encode_slots(Kn, Vn, l0, slots, G, c, kc, vc, err, st);
   constexpr int kMost = 1 << 19;  // tokens of a launch: 2^15 groups of 16, of the 65535 that its grid's second dimension holds
@@ -445,7 +446,8 @@ static hipError_t launch_append_slots(const ViewDev& Kn, const ViewDev& Vn, int 
       v.sb = v.st;
       v.T = 1;
     }
-    const hipError_t e = launch_append(x[0], x[1], l0, slots + i0, G, c, kc, vc, err, st, PageDev(), true);
+    const hipError_t e = launch_append(x[0], x[1], l0, slots + i0, G, c, kc, vc, err, st, PageDev(), true,
+                                       turn ? turn + i0 : nullptr, plan);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -976,7 +978,18 @@ int32_t kv_page_release(int32_t* lens, const int32_t* done, int32_t B, const cg_
   if (rc != CG_OK) return rc;
   if (!lens || !done || B <= 0) return CG_ERR_ARG;
   if (!aligned4(lens) || !aligned4(done) || !aligned4(err_flag)) return CG_ERR_ALIGN;
-  hipError_t e = launch_page_release(lens, done, B, *pool, pages, max_pages, page_size, err_flag,
+  hipError_t e = launch_page_release(lens, done, B, *pool, pages, max_pages, page_size, err_flag, false,
+                                     static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
+}
+
+int32_t kv_page_trim(int32_t* lens, const int32_t* keep, int32_t B, const cg_page_pool* pool, int32_t* pages,
+                     int32_t max_pages, int32_t page_size, int32_t* err_flag, void* stream) {
+  int32_t rc = check_pool(pool, pages, max_pages, page_size);
+  if (rc != CG_OK) return rc;
+  if (!lens || !keep || B <= 0) return CG_ERR_ARG;
+  if (!aligned4(lens) || !aligned4(keep) || !aligned4(err_flag)) return CG_ERR_ALIGN;
+  hipError_t e = launch_page_release(lens, keep, B, *pool, pages, max_pages, page_size, err_flag, true,
                                      static_cast<hipStream_t>(stream));
   return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
 }
@@ -1017,9 +1030,8 @@ int32_t rope_make(const cg_rope* r, cg_rope_plan* plan) {
   return CG_OK;
 }
 
-int32_t kv_rope(const cg_rope_plan* plan, const cg_kv_view* x0, const cg_kv_view* y0, const cg_kv_view* x1,
-                const cg_kv_view* y1, const int32_t* pos, int32_t inverse, void* stream) {
-  if (!plan || !x0 || !y0 || (x1 == nullptr) != (y1 == nullptr)) return CG_ERR_ARG;
+static int32_t check_rope(const cg_rope_plan* plan, const cg_kv_view* x0, const cg_kv_view* y0, const cg_kv_view* x1,
+                          const cg_kv_view* y1) {
   if (plan->layout != CG_ROPE_HALF && plan->layout != CG_ROPE_PAIRS) return CG_ERR_ARG;
   const cg_kv_view* vs[4] = {x0, y0, x1, y1};
   int32_t rc;
@@ -1031,13 +1043,26 @@ int32_t kv_rope(const cg_rope_plan* plan, const cg_kv_view* x0, const cg_kv_view
   }
   if (x0->d % 8 || x0->d > 256) return CG_ERR_UNSUPPORTED;
   if (plan->d_rot < 2 || plan->d_rot % 2 || plan->d_rot > x0->d) return CG_ERR_SHAPE;
-  if (x0->T == 0) return CG_OK;
+  return CG_OK;
+}
+// ... and what is left of them where there are tokens
+static int32_t check_turned(const cg_kv_view* x0, const cg_kv_view* y0, const cg_kv_view* x1, const cg_kv_view* y1,
+                            const int32_t* pos) {
   if (!pos) return CG_ERR_ARG;
   if (!aligned4(pos)) return CG_ERR_ALIGN;
   if (int64_t(x0->B) * x0->T > INT32_MAX / (x0->d / 2) - 256 || int64_t(x0->L) * (int64_t(x0->H) + (x1 ? x1->H : 0)) > 65535)
     return CG_ERR_CAPACITY;
-  for (int i = 1; i < (x1 ? 4 : 2); i += 2)
-    if ((rc = check_apart(vs[i])) != CG_OK) return rc;
+  int32_t rc = check_apart(y0);
+  return rc == CG_OK && x1 ? check_apart(y1) : rc;
+}
+
+int32_t kv_rope(const cg_rope_plan* plan, const cg_kv_view* x0, const cg_kv_view* y0, const cg_kv_view* x1,
+                const cg_kv_view* y1, const int32_t* pos, int32_t inverse, void* stream) {
+  if (!plan || !x0 || !y0 || (x1 == nullptr) != (y1 == nullptr)) return CG_ERR_ARG;
+  int32_t rc = check_rope(plan, x0, y0, x1, y1);
+  if (rc != CG_OK) return rc;
+  if (x0->T == 0) return CG_OK;
+  if ((rc = check_turned(x0, y0, x1, y1, pos)) != CG_OK) return rc;
   ViewDev none{};
   hipError_t e = launch_rope(*plan, view_dev(x0), view_dev(y0), x1 ? view_dev(x1) : none, x1 ? view_dev(y1) : none, pos,
                              inverse != 0, static_cast<hipStream_t>(stream));
@@ -1056,9 +1081,8 @@ static int32_t check_pools(const cg_cache* kc, const cg_cache* vc, const cg_code
   return ok ? CG_OK : CG_ERR_UNSUPPORTED;
 }
 
-int32_t kv_append_slots(int32_t l0, int32_t l1, const cg_kv_view* k_new, const cg_kv_view* v_new, const int32_t* slots,
-                        const void* G_dev, cg_gauge_shape shp, const cg_codec* codec, const cg_cache* kc,
-                        const cg_cache* vc, int32_t* err_flag, void* stream) {
+static int32_t check_append(int32_t l0, int32_t l1, const cg_kv_view* k_new, const cg_kv_view* v_new, const void* G_dev,
+                            const cg_gauge_shape& shp, const cg_codec* codec, const cg_cache* kc, const cg_cache* vc) {
   int32_t rc = check_shape(shp);
   if (rc != CG_OK) return rc;
   if (!G_dev || l0 < 0 || l1 <= l0 || l1 > shp.L) return CG_ERR_ARG;
@@ -1069,12 +1093,89 @@ int32_t kv_append_slots(int32_t l0, int32_t l1, const cg_kv_view* k_new, const c
   if ((rc = check_view(v_new, shp, nl)) != CG_OK) return rc;
   if (k_new->B != 1 || v_new->B != 1 || v_new->T != k_new->T) return CG_ERR_SHAPE;
   if ((rc = check_pools(kc, vc, codec, shp)) != CG_OK) return rc;
-  if (int64_t(kc->B) * kc->T_cap > INT32_MAX || k_new->T > INT32_MAX - 64) return CG_ERR_CAPACITY;
+  return int64_t(kc->B) * kc->T_cap > INT32_MAX || k_new->T > INT32_MAX - 64 ? CG_ERR_CAPACITY : CG_OK;
+}
+
+int32_t kv_append_slots(int32_t l0, int32_t l1, const cg_kv_view* k_new, const cg_kv_view* v_new, const int32_t* slots,
+                        const void* G_dev, cg_gauge_shape shp, const cg_codec* codec, const cg_cache* kc,
+                        const cg_cache* vc, int32_t* err_flag, void* stream) {
+  int32_t rc = check_append(l0, l1, k_new, v_new, G_dev, shp, codec, kc, vc);
+  if (rc != CG_OK) return rc;
   if (k_new->T == 0) return CG_OK;
   if (!slots) return CG_ERR_ARG;
   if (!aligned4(slots) || !aligned4(err_flag)) return CG_ERR_ALIGN;
   hipError_t e = launch_append_slots(view_dev(k_new), view_dev(v_new), l0, slots, gauge_dev(G_dev, shp), codec_dev(codec),
                                      cache_dev(kc), cache_dev(vc), err_flag, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
+}
+
+int32_t kv_append_rope(int32_t l0, int32_t l1, const cg_rope_plan* plan, const cg_kv_view* k_new,
+                       const cg_kv_view* v_new, const cg_kv_view* q, const cg_kv_view* q_out, const int32_t* pos,
+                       const int32_t* slots, const void* G_dev, cg_gauge_shape shp, const cg_codec* codec,
+                       const cg_cache* kc, const cg_cache* vc, int32_t* err_flag, void* stream) {
+  int32_t rc = check_append(l0, l1, k_new, v_new, G_dev, shp, codec, kc, vc);
+  if (rc != CG_OK) return rc;
+  if (!plan || (q == nullptr) != (q_out == nullptr)) return CG_ERR_ARG;
+  if ((rc = check_rope(plan, q ? q : k_new, q ? q_out : k_new, nullptr, nullptr)) != CG_OK) return rc;
+  if (q && (q->L != k_new->L || q->B != 1 || q->T != k_new->T || q->d != shp.d)) return CG_ERR_SHAPE;
+  if (k_new->T == 0) return CG_OK;
+  if (!slots || !pos) return CG_ERR_ARG;
+  if (!aligned4(slots) || !aligned4(pos) || !aligned4(err_flag)) return CG_ERR_ALIGN;
+  if (q && (rc = check_turned(q, q_out, nullptr, nullptr, pos)) != CG_OK) return rc;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  hipError_t e = hipSuccess;
+  const ViewDev none{};
+  if (q) e = launch_rope(*plan, view_dev(q), view_dev(q_out), none, none, pos, false, st);
+  if (e == hipSuccess)
+    e = launch_append_slots(view_dev(k_new), view_dev(v_new), l0, slots, gauge_dev(G_dev, shp), codec_dev(codec),
+                            cache_dev(kc), cache_dev(vc), err_flag, st, pos, plan);
+  return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
+}
+
+int32_t kv_tree_map(const int32_t* parent, const int32_t* cu, const int32_t* lens, int32_t B, int32_t N, int32_t words,
+                    int32_t* pos, uint64_t* mask, int32_t* err_flag, void* stream) {
+  if (!cu || !lens || B <= 0 || B == INT32_MAX || N < 0 || words <= 0 || (N && (!parent || !pos || !mask))) return CG_ERR_ARG;
+  if (!aligned4(parent) || !aligned4(cu) || !aligned4(lens) || !aligned4(pos) || !aligned4(err_flag) || !aligned8(mask))
+    return CG_ERR_ALIGN;
+  hipError_t e = launch_tree_map(parent, cu, lens, B, N, words, pos, mask, err_flag, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
+}
+
+int32_t kv_tree_accept(const int32_t* parent, const int32_t* cu, const int32_t* draft, const int32_t* target,
+                       const int32_t* head, int32_t B, int32_t N, int32_t* path, int32_t* kept, int32_t* next,
+                       int32_t* err_flag, void* stream) {
+  if (!cu || !kept || !next || B <= 0 || B == INT32_MAX || N < 0 || (N && (!parent || !draft || !target || !path)))
+    return CG_ERR_ARG;
+  if (!aligned4(parent) || !aligned4(cu) || !aligned4(draft) || !aligned4(target) || !aligned4(head) || !aligned4(path) ||
+      !aligned4(kept) || !aligned4(next) || !aligned4(err_flag))
+    return CG_ERR_ALIGN;
+  hipError_t e = launch_tree_accept(parent, cu, draft, target, head, B, N, path, kept, next, err_flag,
+                                    static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
+}
+
+int32_t kv_tree_keep(int32_t l0, int32_t l1, const int32_t* path, const int32_t* kept, const int32_t* cu,
+                     const int32_t* lens, int32_t B, int32_t N, const cg_page_table* pages, cg_gauge_shape shp,
+                     const cg_codec* codec, const cg_cache* kc, const cg_cache* vc, int32_t* held, int32_t* err_flag,
+                     void* stream) {
+  int32_t rc = check_shape(shp);
+  if (rc != CG_OK) return rc;
+  if (!kept || !cu || !lens || !held || B <= 0 || N < 0 || (N && !path) || l0 < 0 || l1 <= l0 || l1 > shp.L) return CG_ERR_ARG;
+  if (held == lens) return CG_ERR_ARG;
+  if (!aligned4(path) || !aligned4(kept) || !aligned4(cu) || !aligned4(lens) || !aligned4(held) || !aligned4(err_flag))
+    return CG_ERR_ALIGN;
+  if ((rc = check_codec(codec, shp.d)) != CG_OK) return rc;
+  if ((rc = check_pools(kc, vc, codec, shp)) != CG_OK) return rc;
+  if ((rc = check_pages(pages, codec, kc)) != CG_OK) return rc;
+  if (int64_t(kc->B) * kc->T_cap > INT32_MAX || int64_t(pages->max_pages) * pages->page_size > INT32_MAX)
+    return CG_ERR_CAPACITY;
+  if (int64_t(2) * (l1 - l0) * shp.H > INT32_MAX / B) return CG_ERR_CAPACITY;
+  PageDev pt;
+  pt.pages = pages->pages;
+  pt.max_pages = pages->max_pages;
+  pt.page_size = pages->page_size;
+  hipError_t e = launch_tree_keep(path, kept, cu, lens, B, N, pt, codec_dev(codec), cache_dev(kc), cache_dev(vc), l0, l1 - l0,
+                                  held, err_flag, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
 }
 
@@ -1137,11 +1238,10 @@ size_t attend_chunk_workspace_limit(cg_gauge_shape shp, int32_t nl, int32_t N, i
   return sizeof(float) * size_t(std::max(rows * (shp.d + 2), rows1 * (2 + 2 * shp.d)));
 }
 
-int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const int32_t* cu, int32_t B, int32_t max_q,
-                              const cg_cache* kc, const cg_cache* vc, const cg_page_table* pages, const void* G_dev,
-                              cg_gauge_shape shp, const cg_codec* codec, const int32_t* lens, float scale,
-                              int32_t window, int32_t sinks, const cg_kv_view* out, void* workspace,
-                              int32_t* err_flag, void* stream) {
+static int32_t check_packed(int32_t l0, int32_t l1, const cg_kv_view* q, const int32_t* cu, int32_t B, int32_t max_q,
+                            const cg_cache* kc, const cg_cache* vc, const cg_page_table* pages, const void* G_dev,
+                            const cg_gauge_shape& shp, const cg_codec* codec, const int32_t* lens, float scale,
+                            int32_t window, int32_t sinks, const cg_kv_view* out, const int32_t* err_flag) {
   int32_t rc = check_shape(shp);
   if (rc != CG_OK) return rc;
   if (!G_dev || !cu || !lens || l0 < 0 || l1 <= l0 || l1 > shp.L || !isfinite(scale)) return CG_ERR_ARG;
@@ -1156,18 +1256,13 @@ int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const
   if ((rc = check_pools(kc, vc, codec, shp)) != CG_OK) return rc;
   if ((rc = check_pages(pages, codec, kc)) != CG_OK) return rc;
   if ((rc = check_chunk(nl, q->T, B, max_q, q->H, pages->max_pages, pages->page_size, window, sinks, shp)) != CG_OK) return rc;
-  if (q->T == 0) return CG_OK;
-  if ((rc = check_apart(out)) != CG_OK) return rc;
-  const int cap = pages->max_pages * pages->page_size;
-  const CodecDev c = codec_dev(codec);
-  const bool singles = (max_q == 1 || B > 1) && singles_apart(c, shp.d, q->H / shp.H, out->dtype == CG_DTYPE_F32);
-  const ChunkPlan p = chunk_plan(nl, q->T, B, max_q, shp.H, q->H, shp.d, cap, window, sinks, singles);
-  const AttendPlan one = singles_plan(nl, B, shp.H, q->H, shp.d, cap, window, sinks);
-  const bool ws = (p.ws_bytes && (max_q > 1 || !singles)) || (one.ws_bytes && singles);
-  if (ws && (!workspace || !aligned16(workspace))) return workspace ? CG_ERR_ALIGN : CG_ERR_ARG;
-  if (int64_t(nl) * shp.H * p.nqc * p.ntile * p.nsplit > INT32_MAX) return CG_ERR_CAPACITY;
-  // (the matrix-core kernel may halve its query chunks)
-  if (singles && 2 * int64_t(nl) * shp.H * one.nqc * one.nsplit > INT32_MAX / B) return CG_ERR_CAPACITY;
+  return q->T ? check_apart(out) : CG_OK;
+}
+
+// The kernel's arguments apart from its plan
+static ChunkDev chunk_dev(int32_t l0, const cg_kv_view* q, const int32_t* cu, int32_t B, int32_t max_q, const cg_cache* kc,
+                          const cg_cache* vc, const cg_page_table* pages, const cg_gauge_shape& shp, const int32_t* lens,
+                          float scale, int32_t window, int32_t sinks, const cg_kv_view* out, int32_t* err_flag) {
   ChunkDev a;
   a.q = view_dev(q);
   a.o = view_dev(out);
@@ -1187,15 +1282,42 @@ int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const
   a.scale = scale;
   a.window = window;
   a.sinks = sinks;
-  a.cap = cap;
+  a.cap = pages->max_pages * pages->page_size;
+  a.err = err_flag;
+  return a;
+}
+
+static void set_plan(ChunkDev& a, const ChunkPlan& p, void* workspace) {
   a.tq = p.tq;
   a.heads = p.heads;
   a.nqc = p.nqc;
   a.ntile = p.ntile;
   a.nsplit = p.nsplit;
   a.part = static_cast<float*>(workspace);
-  a.ml = a.part ? a.part + size_t(nl) * p.nsplit * q->T * q->H * shp.d : nullptr;
-  a.err = err_flag;
+  a.ml = a.part ? a.part + size_t(a.q.L) * p.nsplit * a.N * a.Hq * a.q.d : nullptr;
+}
+
+int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const int32_t* cu, int32_t B, int32_t max_q,
+                              const cg_cache* kc, const cg_cache* vc, const cg_page_table* pages, const void* G_dev,
+                              cg_gauge_shape shp, const cg_codec* codec, const int32_t* lens, float scale,
+                              int32_t window, int32_t sinks, const cg_kv_view* out, void* workspace,
+                              int32_t* err_flag, void* stream) {
+  const int32_t rc =
+      check_packed(l0, l1, q, cu, B, max_q, kc, vc, pages, G_dev, shp, codec, lens, scale, window, sinks, out, err_flag);
+  if (rc != CG_OK || q->T == 0) return rc;
+  const int nl = l1 - l0;
+  const int cap = pages->max_pages * pages->page_size;
+  const CodecDev c = codec_dev(codec);
+  const bool singles = (max_q == 1 || B > 1) && singles_apart(c, shp.d, q->H / shp.H, out->dtype == CG_DTYPE_F32);
+  const ChunkPlan p = chunk_plan(nl, q->T, B, max_q, shp.H, q->H, shp.d, cap, window, sinks, singles);
+  const AttendPlan one = singles_plan(nl, B, shp.H, q->H, shp.d, cap, window, sinks);
+  const bool ws = (p.ws_bytes && (max_q > 1 || !singles)) || (one.ws_bytes && singles);
+  if (ws && (!workspace || !aligned16(workspace))) return workspace ? CG_ERR_ALIGN : CG_ERR_ARG;
+  if (int64_t(nl) * shp.H * p.nqc * p.ntile * p.nsplit > INT32_MAX) return CG_ERR_CAPACITY;
+  // (the matrix-core kernel may halve its query chunks)
+  if (singles && 2 * int64_t(nl) * shp.H * one.nqc * one.nsplit > INT32_MAX / B) return CG_ERR_CAPACITY;
+  ChunkDev a = chunk_dev(l0, q, cu, B, max_q, kc, vc, pages, shp, lens, scale, window, sinks, out, err_flag);
+  set_plan(a, p, workspace);
   const GaugeDev G = gauge_dev(G_dev, shp);
   hipStream_t st = static_cast<hipStream_t>(stream);
   a.min_q = singles ? 2 : 1;
@@ -1231,6 +1353,41 @@ int32_t kv_attend_chunk_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const
     s.sinks = sinks;
     e = launch_attend(s, G, c, force_generic(), st);
   }
+  return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
+}
+
+size_t attend_tree_workspace_bytes(cg_gauge_shape shp, int32_t nl, int32_t N, int32_t B, int32_t Hq, int32_t max_pages,
+                                   int32_t page_size) {
+  if (check_shape(shp) != CG_OK || check_chunk(nl, N, B, 1, Hq, max_pages, page_size, 0, 0, shp) != CG_OK || N == 0) return 0;
+  const int64_t steps = int64_t(max_pages) * page_size / 64, parts = std::min<int64_t>(kChunkSplits, steps / 8);
+  const double rows = parts > 1 ? std::min(double(nl) * N * Hq * parts, double(chunk_part_rows())) : 0.0;
+  return sizeof(float) * size_t(rows * (shp.d + 2));
+}
+
+int32_t kv_attend_tree_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const int32_t* cu, int32_t B, int32_t max_q,
+                             const uint64_t* mask, int32_t words, const int32_t* pos, const cg_cache* kc,
+                             const cg_cache* vc, const cg_page_table* pages, const void* G_dev, cg_gauge_shape shp,
+                             const cg_codec* codec, const int32_t* lens, float scale, int32_t window, int32_t sinks,
+                             const cg_kv_view* out, void* workspace, int32_t* err_flag, void* stream) {
+  const int32_t rc =
+      check_packed(l0, l1, q, cu, B, max_q, kc, vc, pages, G_dev, shp, codec, lens, scale, window, sinks, out, err_flag);
+  if (rc != CG_OK) return rc;
+  if (max_q > CG_TREE_MOST) return CG_ERR_UNSUPPORTED;
+  if (words < (max_q + 63) / 64) return CG_ERR_SHAPE;
+  if (q->T == 0) return CG_OK;
+  if (!mask || (window > 0 && !pos)) return CG_ERR_ARG;
+  if (!aligned8(mask) || !aligned4(pos)) return CG_ERR_ALIGN;
+  const int nl = l1 - l0;
+  ChunkDev a = chunk_dev(l0, q, cu, B, max_q, kc, vc, pages, shp, lens, scale, window, sinks, out, err_flag);
+  a.mask = mask;
+  a.words = words;
+  a.pos = pos;
+  a.min_q = 1;
+  const ChunkPlan p = chunk_plan(nl, q->T, B, max_q, shp.H, q->H, shp.d, a.cap, window, sinks, false);
+  if (p.ws_bytes && (!workspace || !aligned16(workspace))) return workspace ? CG_ERR_ALIGN : CG_ERR_ARG;
+  if (int64_t(nl) * shp.H * p.nqc * p.ntile * p.nsplit > INT32_MAX) return CG_ERR_CAPACITY;
+  set_plan(a, p, workspace);
+  const hipError_t e = launch_chunk(a, gauge_dev(G_dev, shp), codec_dev(codec), static_cast<hipStream_t>(stream));
   return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
 }
 

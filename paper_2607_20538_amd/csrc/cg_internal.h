@@ -190,8 +190,17 @@ hipError_t launch_rope(const cg_rope_plan& plan, const ViewDev& x0, const ViewDe
                        const ViewDev& y1, const int* pos, bool inverse, hipStream_t st);
 hipError_t launch_page_map(const int* held, const int* add, int B, const cg_page_pool& pool, int* pages, int max_pages,
                            int P, int N, int* cu, int* lens, int* pos, int* slots, int* err, hipStream_t st);
+// trim: `done` holds the positions that the rows keep
 hipError_t launch_page_release(int* lens, const int* done, int B, const cg_page_pool& pool, int* pages, int max_pages,
-                               int P, int* err, hipStream_t st);
+                               int P, int* err, bool trim, hipStream_t st);
+// Trees of drafted tokens: positions and masks, the accepted paths, their entries moved together.
+hipError_t launch_tree_map(const int* parent, const int* cu, const int* lens, int B, int N, int words, int* pos,
+                           uint64_t* mask, int* err, hipStream_t st);
+hipError_t launch_tree_accept(const int* parent, const int* cu, const int* draft, const int* target, const int* head,
+                              int B, int N, int* path, int* kept, int* next, int* err, hipStream_t st);
+hipError_t launch_tree_keep(const int* path, const int* kept, const int* cu, const int* lens, int B, int N,
+                            const PageDev& pt, const CodecDev& c, const CacheDev& kc, const CacheDev& vc, int l0, int nl,
+                            int* held, int* err, hipStream_t st);
 
 // HBM streaming probe (read_bytes a multiple of 8 KB, write_bytes of 16 bytes).
 hipError_t launch_stream_probe(const void* src, int64_t read_bytes, void* dst, int64_t write_bytes, hipStream_t st);
@@ -213,9 +222,11 @@ hipError_t launch_decode(int s, const CacheDev& k, int l0, const GaugeDev& G, co
                          const int* pos, int pos_add, const ViewDev& Y, int* err, hipStream_t st);
 // Rolling append of one key and one value token per (layer, b, h) at pos[b], in one launch (layer l of
 // the views is cache layer l + l0).  slots: pos holds pool slots (page * T_cap + position; negative:
-// nothing to append) instead of row positions.
+// nothing to append) instead of row positions.  turn (rows that are not staged): the keys are turned by
+// turn[b] (negative: no token) as `plan` says.
 hipError_t launch_append(const ViewDev& Kn, const ViewDev& Vn, int l0, const int* pos, const GaugeDev& G,
                          const CodecDev& c, const CacheDev& kc, const CacheDev& vc, int* err, hipStream_t st,
-                         const PageDev& pt = PageDev(), bool slots = false);
+                         const PageDev& pt = PageDev(), bool slots = false, const int* turn = nullptr,
+                         const cg_rope_plan* plan = nullptr);
 
 }  // namespace cg

@@ -164,10 +164,13 @@ __global__ __launch_bounds__(256) void map_tokens(MapArgs a) {
   if (i < a.N) map_token(a, a.cu, i);
 }
 
-// Rows that are done give their pages back: pushed on the stack row by row, their table entries -1, length 0
+// Rows that are done give their pages back: pushed on the stack row by row, their table entries -1, length 0.
+// TRIM: `done` holds the positions that each row keeps, and the pages past them are given back.
+template <bool TRIM>
 __global__ __launch_bounds__(kMapThreads) void release_rows(MapArgs a, const int* done) {
   __shared__ int64_t sums[kMapThreads / 64][2];
   __shared__ int64_t first[kMapThreads + 1];  // table entries of the round's rows before each row
+  __shared__ int stay[TRIM ? kMapThreads : 1];  // entries that each row of the round keeps
   const int tid = threadIdx.x;
   int64_t base = min(max(*a.count, 0), a.n_pages);
   int flags = 0;
@@ -175,7 +178,19 @@ __global__ __launch_bounds__(kMapThreads) void release_rows(MapArgs a, const int
   for (int b0 = 0; b0 < a.B; b0 += kMapThreads) {
     const int b = b0 + tid;
     int64_t n = 0, ok = 0, entries, pushed;
-    if (b < a.B && done[b]) {
+    if constexpr (TRIM) {
+      if (b < a.B) {
+        const int len = a.lens[b], keep = done[b];
+        // (a row that cannot be trimmed stays as it is)
+        if (keep < 0 || keep > len || len > int64_t(a.max_pages) * a.P) {
+          flags |= CG_FLAG_POS_RANGE;
+        } else {
+          stay[tid] = pages_of(keep, a.P);
+          n = pages_of(len, a.P) - stay[tid];
+          a.lens[b] = keep;
+        }
+      }
+    } else if (b < a.B && done[b]) {
       const int len = a.lens[b];
       if (len < 0 || len > int64_t(a.max_pages) * a.P) flags |= CG_FLAG_POS_RANGE;
       n = min(pages_of(max(len, 0), a.P), a.max_pages);
@@ -189,7 +204,7 @@ __global__ __launch_bounds__(kMapThreads) void release_rows(MapArgs a, const int
       int pg = -1;
       if (k < entries) {
         const int r = row_of(first, k);
-        int* e = a.pages + size_t(b0 + r) * a.max_pages + int(k - first[r]);
+        int* e = a.pages + size_t(b0 + r) * a.max_pages + int(k - first[r]) + (TRIM ? stay[r] : 0);
         pg = *e;
         *e = -1;
       }
@@ -224,10 +239,11 @@ hipError_t launch_page_map(const int* held, const int* add, int B, const cg_page
 }
 
 hipError_t launch_page_release(int* lens, const int* done, int B, const cg_page_pool& pool, int* pages, int max_pages, int P,
-                               int* err, hipStream_t st) {
+                               int* err, bool trim, hipStream_t st) {
   if (B == 0) return hipSuccess;
   MapArgs a{nullptr, nullptr, B, 0, max_pages, P, pool.n_pages, pool.free_pages, pool.free_count, pages, nullptr, lens, nullptr, nullptr, err};
-  hipLaunchKernelGGL(release_rows, dim3(1), dim3(kMapThreads), 0, st, a, done);
+  if (trim) hipLaunchKernelGGL(release_rows<true>, dim3(1), dim3(kMapThreads), 0, st, a, done);
+  else hipLaunchKernelGGL(release_rows<false>, dim3(1), dim3(kMapThreads), 0, st, a, done);
   return hipGetLastError();
 }
 

@@ -15,6 +15,7 @@
 
 #include "cg_internal.h"
 #include "cg_device.h"
+#include "cg_rope.h"
 
 namespace cg {
 
@@ -27,27 +28,6 @@ struct RopeArgs {
   int inverse, per;     // rows (layer, head) of a thread
   int units, skip;      // units of 2 V channels a row has; units from `skip` on are left (in-place: nothing to copy)
 };
-
-// turns (64-bit fraction) -> sine and cosine
-__device__ __forceinline__ void sincos_turns(uint64_t f, float& s, float& c) {
-  const uint32_t q = uint32_t((f + (uint64_t(1) << 61)) >> 62);
-  const int64_t r = int64_t(f - (uint64_t(q) << 62));  // within an eighth of a turn
-  const float x = float(int32_t(r >> 32)) * 1.46291807926715968e-9f;  // 2 pi 2^-32
-  const float x2 = x * x;
-  float a = fmaf(x2, 2.755731922398589e-6f, -1.984126984126984e-4f);  // 1/9!, -1/7!
-  a = fmaf(x2, a, 8.333333333333333e-3f);
-  a = fmaf(x2, a, -1.666666666666667e-1f);
-  a = fmaf(x * x2, a, x);
-  float b = fmaf(x2, -2.755731922398589e-7f, 2.480158730158730e-5f);  // -1/10!, 1/8!
-  b = fmaf(x2, b, -1.388888888888889e-3f);
-  b = fmaf(x2, b, 4.166666666666667e-2f);
-  b = fmaf(x2, b, -0.5f);
-  b = fmaf(x2, b, 1.0f);
-  s = (q & 1) ? b : a;
-  c = (q & 1) ? a : b;
-  if (q & 2) s = -s;
-  if ((q + 1) & 2) c = -c;
-}
 
 // V neighbouring elements, as loaded and as binary32
 template <int V, bool BF16>
