@@ -15,6 +15,7 @@
 
 #include "cg_internal.h"
 #include "cg_chunk.h"
+#include "cg_tree_attend.h"
 
 using namespace cg;
 
@@ -1361,7 +1362,9 @@ size_t attend_tree_workspace_bytes(cg_gauge_shape shp, int32_t nl, int32_t N, in
   if (check_shape(shp) != CG_OK || check_chunk(nl, N, B, 1, Hq, max_pages, page_size, 0, 0, shp) != CG_OK || N == 0) return 0;
   const int64_t steps = int64_t(max_pages) * page_size / 64, parts = std::min<int64_t>(kChunkSplits, steps / 8);
   const double rows = parts > 1 ? std::min(double(nl) * N * Hq * parts, double(chunk_part_rows())) : 0.0;
-  return sizeof(float) * size_t(rows * (shp.d + 2));
+  // whatever the codec and the result's type
+  const double chunks = sizeof(float) * rows * (shp.d + 2);
+  return size_t(shp.d == 64 || shp.d == 128 ? std::max(chunks, tree_plan_limit(nl, N, B, shp.H, Hq, shp.d)) : chunks);
 }
 
 int32_t kv_attend_tree_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const int32_t* cu, int32_t B, int32_t max_q,
@@ -1383,11 +1386,20 @@ int32_t kv_attend_tree_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const 
   a.words = words;
   a.pos = pos;
   a.min_q = 1;
+  const CodecDev c = codec_dev(codec);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  if (!force_generic() && tree_attend_supported(c, shp.d, a.grp, a.o.bf16)) {
+    const TreePlan p = tree_plan(nl, q->T, B, max_q, shp.H, q->H, shp.d);
+    if (!workspace || !aligned16(workspace)) return workspace ? CG_ERR_ALIGN : CG_ERR_ARG;
+    if (int64_t(nl) * shp.H * p.nqc * std::max(p.ntile + 1, p.nwg) > INT32_MAX) return CG_ERR_CAPACITY;
+    const hipError_t e = launch_tree_attend(a, p, workspace, gauge_dev(G_dev, shp), c, st);
+    return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
+  }
   const ChunkPlan p = chunk_plan(nl, q->T, B, max_q, shp.H, q->H, shp.d, a.cap, window, sinks, false);
   if (p.ws_bytes && (!workspace || !aligned16(workspace))) return workspace ? CG_ERR_ALIGN : CG_ERR_ARG;
   if (int64_t(nl) * shp.H * p.nqc * p.ntile * p.nsplit > INT32_MAX) return CG_ERR_CAPACITY;
   set_plan(a, p, workspace);
-  const hipError_t e = launch_chunk(a, gauge_dev(G_dev, shp), codec_dev(codec), static_cast<hipStream_t>(stream));
+  const hipError_t e = launch_chunk(a, gauge_dev(G_dev, shp), c, st);
   return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
 }
 

@@ -28,7 +28,7 @@ class Tree(Case):
     def __init__(self, rows, kind="near", words=0, masks=None, **kw):
         super().__init__(rows, **kw)
         rng = np.random.default_rng(kw.get("seed", 1) + 77)
-        self.words = -(-self.max_q // 64) + words
+        self.words = max(2, -(-self.max_q // 64)) + words
         self.masks, self.hpos, self.seen = [], [], []
         for b, (held, n) in enumerate(rows):
             m, depth = T.closure(T.tree(n, kind, rng))
@@ -123,6 +123,7 @@ CASES = {
     "wide_rows": dict(rows=[(70, 1024), (0, 300)], H=1, grp=1, d=64, g=16, n=32),
     "negative_scale": dict(rows=RAGGED, scale=-0.05, H=1),
     "zero_scale": dict(rows=RAGGED, scale=0.0, H=1),
+    "many_rows": dict(rows=[(k % 90, k % 4) for k in range(600)], H=1, grp=2),
     "one_token": dict(rows=[(700, 1)], pad=0),
     "ones": dict(rows=[(700, 1), (0, 1), (64, 1), (130, 0), (63, 1), (131, 1)]),
 }
@@ -196,6 +197,18 @@ def test_rows_that_cannot_be_taken():
     c.call()
     torch.cuda.synchronize()
     assert int(c.err.item()) == cg.CG_FLAG_POS_RANGE and (c.out[:, 0, :, 9:] == 7.0).all() and (c.out[:, 0, :, :9] != 7.0).any()
+
+
+def test_rows_that_overlap():
+    """More tokens in the rows than there are: no row reads or writes past the batch."""
+    c = Tree([(60, 40), (60, 40), (60, 40)], H=1)
+    c.cu.copy_(torch.tensor([0, 120, 0, 120], dtype=torch.int32))
+    c.lens.copy_(torch.tensor([180, 180, 180], dtype=torch.int32))
+    c.call(max_q=64)
+    c.call(max_q=120)
+    torch.cuda.synchronize()
+    assert int(c.err.item()) == cg.CG_FLAG_POS_RANGE
+    assert (c.out[:, :, :, 120:] == 7.0).all()
 
 
 def test_pages_outside_the_pool_contribute_nothing():
