@@ -282,19 +282,13 @@ __global__ __launch_bounds__(512) void tree_join(TreeDev p, GaugeDev G) {
   const int hq = bid % inner;
   bid /= inner;
   const int t = bid % a.ntile, lv = bid / a.ntile, h = hq / a.nqc, qc = hq - h * a.nqc, l = lv + a.l0;
-  // the gauge's operands first: they depend on nothing that is read here
+  // the gauge first, in whole rows: it depends on nothing that is read here
   const size_t gb = ((size_t(l) * 2 + 1) * G.H + h) * G.R * size_t(G.g) * G.g;
   int g0, g1;
   reached(G.g, 32 * ct, 32, g0, g1);
-  bf16x8_t A[2][KK];
-  if (gr == 0) {
-#pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      if (16 * kk > g1 || 16 * kk + 15 < g0) continue;
-#pragma unroll
-      for (int pl = 0; pl < 2; ++pl) A[pl][kk] = gauge_operand8(G.tr[pl] + gb, G.g, D, 32 * ct + n, 16 * kk + 8 * hc);
-    }
-  }
+  constexpr int GPITCH = 2 * D + 16;
+  __shared__ __attribute__((aligned(16))) uint8_t gs[2 * D * GPITCH];
+  stage_gauge<2, D, KK, 512, 8>(gs, G.tr, gb, G.g, D, 0, 0);
   const TreeTile tile = p.tiles[t];
   if (tile.len == 0) return;
   const int w0 = tile.wg0, w1 = tile.wg1;
@@ -385,9 +379,11 @@ __global__ __launch_bounds__(512) void tree_join(TreeDev p, GaugeDev G) {
       b[0][e] = s[0];
       b[1][e] = s[1];
     }
-    y = mfma(A[0][kk], as_bf16x8(b[0]), y);
-    y = mfma(A[0][kk], as_bf16x8(b[1]), y);
-    y = mfma(A[1][kk], as_bf16x8(b[0]), y);
+    const uint8_t* row = gs + (32 * ct + n) * GPITCH + 32 * kk + 16 * hc;
+    const bf16x8_t A0 = as_bf16x8(*reinterpret_cast<const u32x4_t*>(row)), A1 = as_bf16x8(*reinterpret_cast<const u32x4_t*>(row + D * GPITCH));
+    y = mfma(A0, as_bf16x8(b[0]), y);
+    y = mfma(A0, as_bf16x8(b[1]), y);
+    y = mfma(A1, as_bf16x8(b[0]), y);
   }
   if (r >= tile.ntok * nh) return;
   const int tok = r / nh, jj = r - tok * nh;

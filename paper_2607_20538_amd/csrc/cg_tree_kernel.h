@@ -31,8 +31,8 @@ struct TreeShape {
   static constexpr int values = 16 * VP;                  // a wave's rows
   static constexpr int codes = (32 * RB + 1023) / 1024 * 1024, sides = 32 * (D / 32) * 4;  // a wave's next keys, and values
   static constexpr int wave = values + 2 * (codes + sides);
-  static constexpr int joined = 2 * QT * (CT / 2) * 4096; // the waves' sums on their way to each other
-  static constexpr int all = queries + (4 * wave > joined ? 4 * wave : joined) + 4 * 32 * QT * 8;
+  static constexpr int joined = 2 * QT * CT * 4096;       // two waves' sums on their way to the others
+  static constexpr int all = (queries + 4 * wave > joined ? queries + 4 * wave : joined) + 4 * 32 * QT * 8;
   static_assert(wave >= 4 * 2 * D * 4, "space of the rows in binary32");
 };
 
@@ -228,10 +228,17 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void tree_attend(TreeRun p) {
       const s16x4_t y1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(vb + 64 * ct + 8 * VP));
       return __builtin_bit_cast(f16x8_t, __builtin_shufflevector(y0, y1, 0, 1, 2, 3, 4, 5, 6, 7));
     };
+    // Workgroups on a CU would go by age, the last to finish alone: they take turns in going first
+    constexpr int TURNS = QT == 1 ? 3 : 2;
+    int prio = int(blockIdx.x / ((gridDim.x + TURNS - 1) / TURNS));
     bool left = false;  // units that binary16 does not hold
     for (; v < v1; ++v) {
       const int t0 = first_pos(v);
       if (t0 >= held) break;
+      if (++prio >= TURNS) prio = 0;
+      if (prio == 0) __builtin_amdgcn_s_setprio(0);
+      else if (prio == 1) __builtin_amdgcn_s_setprio(1);
+      else __builtin_amdgcn_s_setprio(2);
       const bool none = !have;  // nothing of a page outside the pool; positions from `held` on are zeros (their bytes may hold anything)
       const int live = none ? 0 : held - t0;
       landed();
@@ -443,8 +450,8 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void tree_attend(TreeRun p) {
       }
     }
 
-    // ---- the four waves' sums, joined: everything relative to the largest maximum, then waves 2 and 3 to 0 and 1, and these
-    // to each other, half of the channels each
+    // ---- the four waves' sums, joined: everything relative to the largest maximum, then waves 2 and 3 to 0 and 1, and what
+    // these hold by all four
     float M[QT];
 #pragma unroll
     for (int q = 0; q < QT; ++q) {
@@ -469,62 +476,42 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void tree_attend(TreeRun p) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) O[q][ct][e] = al == 0.0f ? 0.0f : O[q][ct][e] * al;
     }
-    constexpr int CH = CT / 2;
-    float4* const jb = reinterpret_cast<float4*>(sm + SH::queries);  // [2][QT][CH][4][64]
-    auto put = [&](int side, int c0) {
+    // (all of LDS but the exchanged maxima; the queries are read)
+    float4* const jb = reinterpret_cast<float4*>(sm);  // [2][QT][CT][4][64]
+    auto put = [&](int side) {
 #pragma unroll
       for (int q = 0; q < QT; ++q)
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
+        for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-          for (int f = 0; f < 4; ++f) {
-            const f32x16_t& x = O[q][c0 + i];
-            jb[(((side * QT + q) * CH + i) * 4 + f) * 64 + lane] = make_float4(x[4 * f], x[4 * f + 1], x[4 * f + 2], x[4 * f + 3]);
-          }
+          for (int f = 0; f < 4; ++f)
+            jb[(((side * QT + q) * CT + ct) * 4 + f) * 64 + lane] =
+                make_float4(O[q][ct][4 * f], O[q][ct][4 * f + 1], O[q][ct][4 * f + 2], O[q][ct][4 * f + 3]);
     };
-    auto add = [&](int side, int c0) {
-#pragma unroll
-      for (int q = 0; q < QT; ++q)
-#pragma unroll
-        for (int i = 0; i < CH; ++i)
-#pragma unroll
-          for (int f = 0; f < 4; ++f) {
-            const float4 y = jb[(((side * QT + q) * CH + i) * 4 + f) * 64 + lane];
-            f32x16_t& x = O[q][c0 + i];
-            x[4 * f] += y.x;
-            x[4 * f + 1] += y.y;
-            x[4 * f + 2] += y.z;
-            x[4 * f + 3] += y.w;
-          }
-    };
-    auto store = [&](int c0) {
-      float4* dst = reinterpret_cast<float4*>(p.part) + slot * (QT * CT * 4 * 64);
-#pragma unroll
-      for (int q = 0; q < QT; ++q)
-#pragma unroll
-        for (int i = 0; i < CH; ++i)
-#pragma unroll
-          for (int f = 0; f < 4; ++f) {
-            const f32x16_t& x = O[q][c0 + i];
-            dst[((q * CT + c0 + i) * 4 + f) * 64 + lane] = make_float4(x[4 * f], x[4 * f + 1], x[4 * f + 2], x[4 * f + 3]);
-          }
-    };
-#pragma unroll
-    for (int c0 = 0; c0 < CT; c0 += CH) {
-      if (w >= 2) put(w - 2, c0);
-      __syncthreads();
-      if (w < 2) add(w, c0);
-      __syncthreads();
-    }
-    if (w == 0) put(0, CH);
-    if (w == 1) put(1, 0);
+    if (w >= 2) put(w - 2);
     __syncthreads();
-    if (w == 0) {
-      add(1, 0);
-      store(0);
-    } else if (w == 1) {
-      add(0, CH);
-      store(CH);
+    if (w < 2) {
+#pragma unroll
+      for (int q = 0; q < QT; ++q)
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int f = 0; f < 4; ++f) {
+            const float4 y = jb[(((w * QT + q) * CT + ct) * 4 + f) * 64 + lane];
+            O[q][ct][4 * f] += y.x;
+            O[q][ct][4 * f + 1] += y.y;
+            O[q][ct][4 * f + 2] += y.z;
+            O[q][ct][4 * f + 3] += y.w;
+          }
+      put(w);  // (where the wave has just read)
+    }
+    __syncthreads();
+    float4* const dst = reinterpret_cast<float4*>(p.part) + slot * (QT * CT * 4 * 64) + lane;
+#pragma unroll
+    for (int i = 0; i < QT * CT; ++i) {  // a quarter of every channel tile's sums each
+      const int at = 4 * i + w;
+      const float4 x = jb[at * 64 + lane], y = jb[(QT * CT * 4 + at) * 64 + lane];
+      dst[at * 64] = make_float4(x.x + y.x, x.y + y.y, x.z + y.z, x.w + y.w);
     }
   }
 }
