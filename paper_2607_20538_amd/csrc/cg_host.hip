@@ -435,9 +435,15 @@ static hipError_t launch_append_slots(const ViewDev& Kn, const ViewDev& Vn, int 
                                       const CodecDev& c, const CacheDev& kc, const CacheDev& vc, int* err,
                                       hipStream_t st, const int* turn = nullptr, const cg_rope_plan* plan = nullptr) {
   constexpr int64_t kEncodeRows = 4096;  // token rows, all layers and heads
-  if (!turn && !force_generic() && int64_t(Kn.T) * Kn.L * Kn.H >= kEncodeRows && mfma_encode_supported(Kn, G, c, true) &&
-      mfma_encode_supported(Vn, G, c, true))
-    return launch_encode_slots(Kn, Vn, l0, slots, G, c, kc, vc, err, st);
+  constexpr int64_t kTurnRows = 4096;    // ... of keys that turn: two launches
+  if (!force_generic() && int64_t(Kn.T) * Kn.L * Kn.H >= (turn ? kTurnRows : kEncodeRows) && (!turn || turn_supported(*plan)) &&
+      mfma_encode_supported(Kn, G, c, true) && mfma_encode_supported(Vn, G, c, true)) {
+    if (turn) {
+      const hipError_t e = launch_encode_turned(Kn, l0, turn, *plan, slots, G, c, kc, err, st);
+      if (e != hipSuccess) return e;
+    }
+    return launch_encode_slots(Kn, Vn, l0, slots, G, c, kc, vc, err, st, turn);
+  }
   constexpr int kMost = 1 << 19;  // tokens of a launch: 2^15 groups of 16, of the 65535 that its grid's second dimension holds
   for (int i0 = 0; i0 < Kn.T; i0 += kMost) {
     ViewDev x[2] = {Kn, Vn};

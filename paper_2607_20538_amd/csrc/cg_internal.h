@@ -118,9 +118,14 @@ hipError_t launch_encode_mfma(int s, const ViewDev& X, int l0, const GaugeDev& G
                               const CacheDev& k, int t0, int tq, int* err, hipStream_t st,
                               const PageDev& pt = PageDev());
 // Packed tokens ([L][1][H][N][d], keys and values in one launch) to their slots, where
-// mfma_encode_supported(.., paged) takes both views
+// mfma_encode_supported(.., paged) takes both views.  turn: the values alone, without the tokens of negative turn
 hipError_t launch_encode_slots(const ViewDev& Kn, const ViewDev& Vn, int l0, const int* slots, const GaugeDev& G,
-                               const CodecDev& c, const CacheDev& kc, const CacheDev& vc, int* err, hipStream_t st);
+                               const CodecDev& c, const CacheDev& kc, const CacheDev& vc, int* err, hipStream_t st,
+                               const int* turn = nullptr);
+// The keys, turned by their positions first (turn; negative: left out), where mfma_encode_supported and turn_supported
+bool turn_supported(const cg_rope_plan& plan);
+hipError_t launch_encode_turned(const ViewDev& Kn, int l0, const int* turn, const cg_rope_plan& plan, const int* slots,
+                                const GaugeDev& G, const CodecDev& c, const CacheDev& kc, int* err, hipStream_t st);
 hipError_t launch_decode_mfma(int s, const CacheDev& k, int l0, const GaugeDev& G, const CodecDev& c, int t0,
                               int len, const int* pos, int pos_add, const ViewDev& Y, int* err, hipStream_t st);
 

@@ -42,6 +42,7 @@ struct MfmaArgs {
   // T_cap = P = page_size, cB = pages of the pool; slots: pages[token] is the token's slot
   const int* pages;
   int max_pages;
+  const int* turn;               // slots: the tokens' positions, negative: left out; NULL: none is
   struct {  // slots: the values' tokens and cache, in the same launch as the keys'
     char* x;
     int64_t sl, sh, st;
@@ -104,6 +105,15 @@ inline void plan(MfmaArgs& m, int nslices, int T, const void* fn) {
   if (const int f = forced_tiles_per_wg()) m.tiles_per_wg = f < ntiles ? f : (ntiles > 0 ? ntiles : 1);
   m.chunks = (ntiles + m.tiles_per_wg - 1) / m.tiles_per_wg;
   m.nslices = nslices;
+}
+
+// ... and where a workgroup takes at most `most` tiles
+inline void plan_at_most(MfmaArgs& m, int nslices, int T, const void* fn, int most) {
+  plan(m, nslices, T, fn);
+  if (m.tiles_per_wg > most) {
+    m.tiles_per_wg = most;
+    m.chunks = ((T + kTok - 1) / kTok + most - 1) / most;
+  }
 }
 
 inline int ksteps(int g) { return g >= 128 ? 8 : (g == 64 ? 4 : 2); }

@@ -33,6 +33,11 @@ __device__ __forceinline__ void pair_turn(const cg_rope_plan& plan, int pair, in
   s *= plan.amplitude;
   c *= plan.amplitude;
 }
+__device__ __forceinline__ void turn_pair(float& x0, float& x1, float s, float c) {
+  const float y0 = fmaf(x0, c, -(x1 * s));
+  x1 = fmaf(x0, s, x1 * c);
+  x0 = y0;
+}
 // Channels of a pair
 __device__ __forceinline__ void pair_channels(const cg_rope_plan& plan, int pair, int& c0, int& c1) {
   const bool half = plan.layout == CG_ROPE_HALF;
