@@ -37,6 +37,14 @@ struct AppendRopeArgs : AppendArgs {
   const int* turn;  // positions that the keys turn by (negative: no token)
   cg_rope_plan plan;
 };
+// ... and of queries, by the workgroups behind the two of a (layer, head) and its rows
+struct AppendQueryArgs : AppendRopeArgs {
+  RopeArgs q;
+  int qx, qy;
+};
+constexpr int kTurnNone = 0, kTurnKeys = 1, kTurnAll = 2, kTurnAllPairs = 3;  // (queries: bf16, eight pairs a thread)
+template <int TURN>
+using TurnedArgs = std::conditional_t<TURN == kTurnNone, AppendArgs, std::conditional_t<TURN == kTurnKeys, AppendRopeArgs, AppendQueryArgs>>;
 
 // Cache batch row and position inside it of batch row b's new token at position p of the row; false
 // (and flagged) when the position or its page is outside the cache.
@@ -61,9 +69,19 @@ __device__ __forceinline__ bool token_slot(const AppendArgs& a, const CacheDev& 
 // Per-token blocks and the error-free backend: workgroup (layer and head, 16 batch rows, K or V).
 constexpr int kRows = 16;
 
-// ROPE: the keys turn by their positions before the gauge, in binary32 in the tile (no rounding between the two).
-template <int KR, int NBW, bool ROPE>
-__global__ __launch_bounds__(kThreads) void append_rows(std::conditional_t<ROPE, AppendRopeArgs, AppendArgs> a) {
+// TURN: the keys turn by their positions before the gauge, in binary32 in the tile (no rounding between the two), and
+// the queries beside them: 206 tokens of 8 heads, d = g = 128, with 32 query heads, take 8.1 us (in a launch before this
+// one the queries take 5.9 us on their own).
+template <int KR, int NBW, int TURN>
+__global__ __launch_bounds__(kThreads) void append_rows(TurnedArgs<TURN> a) {
+  constexpr bool ROPE = TURN != kTurnNone;
+  if constexpr (TURN >= kTurnAll) {
+    if (blockIdx.z >= 2) {
+      const int at = ((blockIdx.z - 2) * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x, by = at / a.qx;
+      if (by < a.qy) rope_unit<8, true, TURN == kTurnAllPairs ? CG_ROPE_PAIRS : CG_ROPE_HALF>(a.q, at - by * a.qx, by);
+      return;
+    }
+  }
   extern __shared__ float sm[];
   __shared__ int64_t rowi[kRows];  // cache token row of each batch row, or -1
   const int s = blockIdx.z;
@@ -142,9 +160,7 @@ __global__ __launch_bounds__(kThreads) void append_rows(std::conditional_t<ROPE,
         float sn, cn;
         pair_channels(a.plan, i, c0, c1);
         pair_turn(a.plan, i, turns[t], sn, cn);
-        const float x0 = xs[t * dp + c0], x1 = xs[t * dp + c1];
-        xs[t * dp + c0] = fmaf(x0, cn, -(x1 * sn));
-        xs[t * dp + c1] = fmaf(x0, sn, x1 * cn);
+        turn_pair(xs[t * dp + c0], xs[t * dp + c1], sn, cn);
       }
     }
     __syncthreads();
@@ -279,8 +295,8 @@ __global__ __launch_bounds__(kThreads) void append_staged(AppendArgs a) {
 
 hipError_t launch_append(const ViewDev& Kn, const ViewDev& Vn, int l0, const int* pos, const GaugeDev& G,
                          const CodecDev& c, const CacheDev& kc, const CacheDev& vc, int* err, hipStream_t st,
-                         const PageDev& pt, bool slots, const int* turn, const cg_rope_plan* plan) {
-  AppendRopeArgs a;
+                         const PageDev& pt, bool slots, const int* turn, const cg_rope_plan* plan, const RopeSplit* q) {
+  AppendQueryArgs a;
   a.slots = slots;
   a.x[0] = Kn; a.x[1] = Vn;
   a.k[0] = kc; a.k[1] = vc;
@@ -292,21 +308,29 @@ hipError_t launch_append(const ViewDev& Kn, const ViewDev& Vn, int l0, const int
   a.pt = pt;
   a.turn = turn;
   if (turn) a.plan = *plan;
+  if (q) {
+    a.q = q->a;
+    a.qx = q->gx;
+    a.qy = q->gy;
+  }
   const int d = Kn.d, dp = d + kPad;
   const bool kivi = c.backend == CG_BACKEND_KIVI, staged = kivi || c.bt > 1;
   // codes of a staged tile: the widest row a codec can have (passthrough writes from the tile)
   const int unit = staged ? (kivi ? c.kg : c.bt) : kRows, rows = (unit + 15) / 16 * 16;
   size_t smem = size_t(2) * rows * dp * sizeof(float) + size_t(unit) * d;
   if (staged && !kivi) smem += size_t(unit) * (d / c.n) * sizeof(float2);
-  const dim3 grid = staged ? dim3(Kn.L * Kn.B * Kn.H, 1, 2) : dim3(Kn.L * Kn.H, (Kn.B + kRows - 1) / kRows, 2);
+  dim3 grid = staged ? dim3(Kn.L * Kn.B * Kn.H, 1, 2) : dim3(Kn.L * Kn.H, (Kn.B + kRows - 1) / kRows, 2);
+  if (q) grid.z += (q->gx * q->gy + grid.x * grid.y - 1) / (grid.x * grid.y);
   return by_gauge(G.g, d, [&](auto kr, auto nbw) {
     constexpr int KR = decltype(kr)::value, NBW = decltype(nbw)::value;
-    const void* fn = staged ? (const void*)append_staged<KR, NBW>
-                            : (turn ? (const void*)append_rows<KR, NBW, true> : (const void*)append_rows<KR, NBW, false>);
+    const void* fn = staged   ? (const void*)append_staged<KR, NBW>
+                     : !turn  ? (const void*)append_rows<KR, NBW, kTurnNone>
+                     : !q     ? (const void*)append_rows<KR, NBW, kTurnKeys>
+                     : plan->layout == CG_ROPE_HALF ? (const void*)append_rows<KR, NBW, kTurnAll>
+                                                    : (const void*)append_rows<KR, NBW, kTurnAllPairs>;
     hipError_t e = set_smem(fn, smem);
     if (e != hipSuccess) return e;
-    AppendArgs& plain = a;
-    void* args[] = {turn ? static_cast<void*>(&a) : static_cast<void*>(&plain)};
+    void* args[] = {&a};  // (the kernels that turn less read the front of it)
     return hipLaunchKernel(fn, grid, dim3(kThreads), args, smem, st);
   });
 }

@@ -116,10 +116,12 @@ __device__ __forceinline__ void cut3(float x0, float x1, uint32_t& hi, uint32_t&
 // kDestSlots (SLOTS): every token goes where its slot says (a.pages[token], page * T_cap + position; negative:
 // nowhere); the staged rows leave as before, each to its own place.  6000 tokens of 2 layers x 16 heads, g = 32,
 // 6 bits, keys and values: 41 us = 3.4 TB/s (append_rows 101), 12 tiles per workgroup.
-// kDestTurned (TURN): as kDestSlots, keys only, turned by their positions between LDS and the matrix core: eight lanes of a
-// token turn its 16 granules, as pairs of them or within them, in binary32, and cut every value into three bfloat16
-// planes that hold all of its 24 bits.  Six products with the gauge's three planes (those of at most two
-// lower steps in all) leave z as close to the binary64 product as the other encoders do.  @FIG@
+// kDestTurned (TURN): as kDestSlots, keys only, turned by their positions between LDS and the matrix core.  Eight lanes of
+// a token turn its 16 granules, as pairs of them or within them, in binary32, and cut every value into three bfloat16
+// planes that hold all of its 24 bits.  Six products with the gauge's three planes (the dropped ones are 2^-24 of the
+// largest) leave z as close to the binary64 product as the other encoders do.  12000 tokens of 8 heads, g = 128,
+// 4 bits: 33 us (append_rows 54); bound by the vector work of the sines and of cutting, 3.2 us per tile where two
+// workgroups share a CU, after 6 us until the first tile: all are resident at once, about six tiles each.
 // kDestPages (PAGED): the cache is a page pool; the rows of a tile (always inside one page) go to the page its
 // positions map to, looked up one tile ahead of the tile's first use.  Blocks with a non-finite value are
 // coded again after the range (recode_rows).
@@ -200,8 +202,9 @@ __global__ __launch_bounds__(kThreads, NP == 2 ? 3 : 2) void enc_mfma(std::condi
   __shared__ int spos[TURN ? slot_tiles(DEST) * kTok : 1];  // and the positions they turn by
   if constexpr (SLOTS) {
     for (int i = int(threadIdx.x); i < (te - tb) * kTok; i += kThreads) {
-      const int tok = tb * kTok + i, at = tok < a.T && a.turn ? a.turn[tok] : 0;
-      const int slot = tok < a.T && at >= 0 ? a.pages[tok] : -1;
+      const int tok = tb * kTok + i, from = min(tok, a.T - 1);
+      const int at = a.turn ? a.turn[from] : 0, to = a.pages[from];
+      const int slot = tok < a.T && at >= 0 ? to : -1;
       if constexpr (TURN) spos[i] = max(at, 0);
       const int pg = slot >= 0 ? slot / a.T_cap : -1;
       if (pg >= a.cB) flags |= CG_FLAG_POS_RANGE;
@@ -287,7 +290,7 @@ __global__ __launch_bounds__(kThreads, NP == 2 ? 3 : 2) void enc_mfma(std::condi
       tg1 = tj + a.plan.d_rot / 16;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) step64[i] = turns ? a.plan.step[8 * tj + i] : 0;
+    for (int i = 0; i < 8; ++i) step64[i] = a.plan.step[8 * tj + i];
   }
   auto turn_tile = [&](int tile) {
     if constexpr (TURN) {

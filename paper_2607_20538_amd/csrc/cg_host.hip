@@ -16,6 +16,7 @@
 #include "cg_internal.h"
 #include "cg_chunk.h"
 #include "cg_tree_attend.h"
+#include "cg_rope.h"
 
 using namespace cg;
 
@@ -433,16 +434,26 @@ hipError_t launch_decode(int s, const CacheDev& k, int l0, const GaugeDev& G, co
 // 512.  Below, they are even: both are the launch and one chain of loads.
 static hipError_t launch_append_slots(const ViewDev& Kn, const ViewDev& Vn, int l0, const int* slots, const GaugeDev& G,
                                       const CodecDev& c, const CacheDev& kc, const CacheDev& vc, int* err,
-                                      hipStream_t st, const int* turn = nullptr, const cg_rope_plan* plan = nullptr) {
+                                      hipStream_t st, const int* turn = nullptr, const cg_rope_plan* plan = nullptr,
+                                      const RopeSplit* q = nullptr) {
   constexpr int64_t kEncodeRows = 4096;  // token rows, all layers and heads
-  constexpr int64_t kTurnRows = 4096;    // ... of keys that turn: two launches
+  // ... where keys turn, in two launches beside that of the queries: 22 us (rows of an append: 19) at 800 tokens of 8 heads, 42
+  // : 42 at 2200, 67 : 95 at 6400; 8 layers of 8 heads 43 : 42 at 307, 68 : 96 at 845 (32 query heads turned as well)
+  constexpr int64_t kTurnRows = 20480;
+  constexpr int kJoinTokens = 2048;        // at most so many: their queries turn in the append's launch
   if (!force_generic() && int64_t(Kn.T) * Kn.L * Kn.H >= (turn ? kTurnRows : kEncodeRows) && (!turn || turn_supported(*plan)) &&
       mfma_encode_supported(Kn, G, c, true) && mfma_encode_supported(Vn, G, c, true)) {
     if (turn) {
-      const hipError_t e = launch_encode_turned(Kn, l0, turn, *plan, slots, G, c, kc, err, st);
+      hipError_t e = q ? launch_rope_split(*q, st) : hipSuccess;
+      if (e == hipSuccess) e = launch_encode_turned(Kn, l0, turn, *plan, slots, G, c, kc, err, st);
       if (e != hipSuccess) return e;
     }
     return launch_encode_slots(Kn, Vn, l0, slots, G, c, kc, vc, err, st, turn);
+  }
+  if (q && (q->gx == 0 || q->V != 8 || Kn.T > kJoinTokens)) {
+    const hipError_t e = launch_rope_split(*q, st);
+    if (e != hipSuccess) return e;
+    q = nullptr;
   }
   constexpr int kMost = 1 << 19;  // tokens of a launch: 2^15 groups of 16, of the 65535 that its grid's second dimension holds
   for (int i0 = 0; i0 < Kn.T; i0 += kMost) {
@@ -454,7 +465,7 @@ static hipError_t launch_append_slots(const ViewDev& Kn, const ViewDev& Vn, int 
       v.T = 1;
     }
     const hipError_t e = launch_append(x[0], x[1], l0, slots + i0, G, c, kc, vc, err, st, PageDev(), true,
-                                       turn ? turn + i0 : nullptr, plan);
+                                       turn ? turn + i0 : nullptr, plan, q);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
@@ -1130,12 +1141,11 @@ int32_t kv_append_rope(int32_t l0, int32_t l1, const cg_rope_plan* plan, const c
   if (!aligned4(slots) || !aligned4(pos) || !aligned4(err_flag)) return CG_ERR_ALIGN;
   if (q && (rc = check_turned(q, q_out, nullptr, nullptr, pos)) != CG_OK) return rc;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  hipError_t e = hipSuccess;
+  RopeSplit turned;
   const ViewDev none{};
-  if (q) e = launch_rope(*plan, view_dev(q), view_dev(q_out), none, none, pos, false, st);
-  if (e == hipSuccess)
-    e = launch_append_slots(view_dev(k_new), view_dev(v_new), l0, slots, gauge_dev(G_dev, shp), codec_dev(codec),
-                            cache_dev(kc), cache_dev(vc), err_flag, st, pos, plan);
+  if (q && !rope_split(*plan, view_dev(q), view_dev(q_out), none, none, pos, false, turned)) return CG_ERR_DEVICE;
+  const hipError_t e = launch_append_slots(view_dev(k_new), view_dev(v_new), l0, slots, gauge_dev(G_dev, shp), codec_dev(codec),
+                                           cache_dev(kc), cache_dev(vc), err_flag, st, pos, plan, q ? &turned : nullptr);
   return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
 }
 

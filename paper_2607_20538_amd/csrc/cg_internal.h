@@ -228,10 +228,11 @@ hipError_t launch_decode(int s, const CacheDev& k, int l0, const GaugeDev& G, co
 // Rolling append of one key and one value token per (layer, b, h) at pos[b], in one launch (layer l of
 // the views is cache layer l + l0).  slots: pos holds pool slots (page * T_cap + position; negative:
 // nothing to append) instead of row positions.  turn (rows that are not staged): the keys are turned by
-// turn[b] (negative: no token) as `plan` says.
+// turn[b] (negative: no token) as `plan` says; q (then): queries to turn in the same launch, 8 pairs of bf16 a thread.
+struct RopeSplit;
 hipError_t launch_append(const ViewDev& Kn, const ViewDev& Vn, int l0, const int* pos, const GaugeDev& G,
                          const CodecDev& c, const CacheDev& kc, const CacheDev& vc, int* err, hipStream_t st,
                          const PageDev& pt = PageDev(), bool slots = false, const int* turn = nullptr,
-                         const cg_rope_plan* plan = nullptr);
+                         const cg_rope_plan* plan = nullptr, const RopeSplit* q = nullptr);
 
 }  // namespace cg

@@ -70,10 +70,31 @@ def _setup(oc, d, g, dtype, N, L=2, H=3, seed=0):
     return P, G, shp, Gd, to_cg(oc), pages, rng, slots, pos, xs
 
 
+# as many token rows (2 layers x 3 heads) as go through the matrix-core encoder
+MANY = {
+    "b4_g128": (BU(4, 64), 128, 128, "bf16", 3600, 128, cg.ROPE_HALF),
+    "b4_g128_pairs": (BU(4, 64), 128, 128, "bf16", 3501, 128, cg.ROPE_PAIRS),
+    "b6_g32": (BU(6, 64), 128, 32, "bf16", 3450, 64, cg.ROPE_HALF),
+    "b6_g32_pairs": (BU(6, 16), 128, 32, "bf16", 3450, 32, cg.ROPE_PAIRS),
+    "b3_g64": (BU(3, 32), 128, 64, "bf16", 3517, 96, cg.ROPE_HALF),
+    "b8_g16": (BU(8, 16), 128, 16, "bf16", 3431, 112, cg.ROPE_PAIRS),
+    "b2_g8": (BU(2, 32), 128, 8, "bf16", 3440, 16, cg.ROPE_HALF),
+    "rot40": (BU(4, 32), 128, 128, "bf16", 3500, 40, cg.ROPE_HALF),     # not in sixteens: the kernel of few tokens
+}
+
+
 @pytest.mark.parametrize("tokens_first", [True, False])
 @pytest.mark.parametrize("name", CASES)
 def test_against_the_oracle(name, tokens_first):
-    oc, d, g, dtype, N, rot, layout = CASES[name]
+    _check(*CASES[name], tokens_first)
+
+
+@pytest.mark.parametrize("name", MANY)
+def test_many_tokens_against_the_oracle(name):
+    _check(*MANY[name], True)
+
+
+def _check(oc, d, g, dtype, N, rot, layout, tokens_first):
     L, H = 2, 3
     P, G, shp, Gd, c, pages, rng, slots, pos, xs = _setup(oc, d, g, dtype, N)
     if N > 1:
@@ -122,7 +143,7 @@ def test_against_the_oracle(name, tokens_first):
         check_fused_codes(rows, code, z["codes"], oc, s, d, n)
 
 
-@pytest.mark.parametrize("N", [20, 1500])
+@pytest.mark.parametrize("N", [20, 3500])
 def test_without_a_turn_it_appends_as_kv_append_slots_does(N):
     """Position 0 and amplitude 1: the keys are what they were.  Values always are."""
     oc = BU(4, 64)
@@ -141,7 +162,7 @@ def test_without_a_turn_it_appends_as_kv_append_slots_does(N):
             check_fused_codes(_rows(cache_to_host(pool[s], oc, s), slots.tolist(), P), want, z["codes"], oc, s, 128, N)
 
 
-@pytest.mark.parametrize("N", [20, 1500])
+@pytest.mark.parametrize("N", [20, 1500, 3500])
 def test_flags(N):
     """Slots past the pool and non-finite tokens raise their flags; a token left out raises none."""
     oc = BU(4, 64)
@@ -198,3 +219,47 @@ def test_layers_of_a_pool():
     for a, b in zip(both, one):
         half = a.codes.numel() // 2
         assert torch.equal(a.codes[half:], b.codes[half:]) and (b.codes[:half] == 0xA5).all()
+
+
+@pytest.mark.parametrize("bits,n,layout", [(4, 64, cg.ROPE_HALF), (6, 16, cg.ROPE_PAIRS), (3, 32, cg.ROPE_HALF)])
+def test_long_ranges_and_tokens_that_are_not_finite(monkeypatch, bits, n, layout):
+    """The bytes do not depend on how many tiles of tokens a workgroup takes; tokens with an infinity, a NaN or a channel
+    near binary32's largest get the bytes that the kernel of few tokens gives them."""
+    oc = BU(bits, n)
+    N, L, H, P = 12001, 1, 2, 64
+    pages = N // P + 2
+    shp, Gd = S.gauge_dev(S.haar(L, H, 128, 64, 7))
+    torch.manual_seed(N + bits)
+    x = [torch.randn((L, 1, N, H, 128), device="cuda").to(torch.bfloat16).transpose(2, 3) for _ in (0, 1)]
+    x[0][0, 0, 1, 2200, 5] = float("inf")
+    x[0][0, 0, 0, 2201, 100] = float("nan")
+    x[0][0, 0, 0, 9000, 64] = 3e38
+    x[1][0, 0, 1, 77, 1] = float("-inf")
+    odd = [(0, 1, 2200), (0, 0, 2201), (0, 0, 9000), (1, 1, 77)]    # (keys or values, head, token)
+    slots = torch.randperm(pages * P, device="cuda")[:N].to(torch.int32)
+    slots[5::97] = -1
+    pos = torch.randint(0, 100000, (N,), dtype=torch.int32, device="cuda")
+    pos[6::97] = -7
+    plan = cg.rope_make(128, layout)
+    got = []
+    for tiles in ("1", "3", "40", "", "generic"):
+        if tiles == "generic":
+            monkeypatch.delenv("CG_TILES_PER_WG")
+            monkeypatch.setenv("CG_KERNELS", "generic")
+        else:
+            monkeypatch.setenv("CG_TILES_PER_WG", tiles)
+        pools = _pools(to_cg(oc), L, pages, H, P, 128)
+        err = torch.zeros(1, dtype=torch.int32, device="cuda")
+        cg.kv_append_rope(0, L, plan, *x, pos, slots, Gd, shp, to_cg(oc), *pools, err_flag=err)
+        torch.cuda.synchronize()
+        assert int(err.item()) == cg.CG_FLAG_NONFINITE | cg.CG_FLAG_SIDE_OVERFLOW
+        got.append([(p.codes.clone(), p.side.clone()) for p in pools])
+    for g in got[1:4]:
+        for (ca, sa), (cb, sb) in zip(got[0], g):
+            assert torch.equal(ca, cb) and torch.equal(sa, sb)
+    sl = slots.tolist()
+    for kv, h, i in odd:
+        page, at = divmod(sl[i], P)
+        (ca, sa), (cb, sb) = ([t.reshape(pages, H, P, -1)[page, h, at].contiguous() for t in g[kv]] for g in (got[0], got[4]))
+        sa, sb = sa.view(torch.float16), sb.view(torch.float16)     # (a NaN has either sign)
+        assert torch.equal(ca, cb) and torch.allclose(sa, sb, rtol=0, atol=0, equal_nan=True)
