@@ -16,11 +16,13 @@ struct TreeTile {
   int base, held;          // positions before the row's new tokens, and with them (a row that cannot be taken: 0, 0)
   int wg0, wg1;            // first and last workgroup on it
 };
-// Order of a run of 32 channels in operands: dword j of granule g holds the channels of part 0 and 1: 4 and 2 bits as the
-// bytes of a masked word hold them, other widths as code_pair takes them.
+// Order of a run of 32 channels in operands: dword j of granule g holds the channels of part 0 and 1: 4, 3 and 2 bits as
+// the bytes of a masked word hold them, other widths as code_pair takes them.
 __host__ __device__ constexpr int tree_channel(int bits, int g, int j, int part) {
-  return bits == 4 ? 8 * g + 4 * (j & 1) + (j >> 1) + 2 * part
-                   : (bits == 2 ? 8 * g + j + 4 * part : 16 * (g >> 1) + 4 * (g & 1) + j + 8 * part);
+  return bits == 4   ? 8 * g + 4 * (j & 1) + (j >> 1) + 2 * part
+         : bits == 3 ? 2 * g + (j >> 1) + 16 * (j & 1) + 8 * part
+         : bits == 2 ? 8 * g + j + 4 * part
+                     : 16 * (g >> 1) + 4 * (g & 1) + j + 8 * part;
 }
 struct TreeLine {
   int64_t total, per;  // blocks of the line, and of a workgroup

@@ -257,11 +257,14 @@ __global__ __launch_bounds__(256) void tree_queries(TreeDev p, GaugeDev G) {
           const auto u = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[8 * kk + j]), __float_as_uint(x[8 * kk + 4 + j]), false, false);
           o[j] = pk_h(__uint_as_float(u[0]), __uint_as_float(u[1]));
         }
+      } else if (p.bits == 3) {  // granules 2 hc and 2 hc + 1 lie in the lane
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = pk_h(x[8 * (j & 1) + 2 * kk + (j >> 1)], x[8 * (j & 1) + 2 * kk + (j >> 1) + 4]);
       } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[j] = pk_h(x[8 * kk + j], x[8 * kk + 4 + j]);
       }
-      put(2 * kk + hc, o);
+      put(p.bits == 3 ? 2 * hc + kk : 2 * kk + hc, o);
     }
   }
 }

@@ -144,6 +144,13 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void tree_attend(TreeRun p) {
 #pragma unroll
         for (int i = 0; i < BITS; ++i) o.w[i] = x[i];
       }
+      if constexpr (BITS == 3) {
+        // codes c, c + 8, c + 16, c + 24 lie 24 bits apart: bytes i, i + 3, i + 6, i + 9 in a word hold them at one place
+        const uint32_t a = o.w[0], b = o.w[1], c = o.w[2];
+        o.w[0] = __builtin_amdgcn_perm(c, __builtin_amdgcn_perm(b, a, 0x0c060300u), 0x05020100u);
+        o.w[1] = __builtin_amdgcn_perm(c, __builtin_amdgcn_perm(b, a, 0x0c070401u), 0x06020100u);
+        o.w[2] = __builtin_amdgcn_perm(c, __builtin_amdgcn_perm(b, a, 0x0c0c0502u), 0x07040100u);
+      }
       o.side = *reinterpret_cast<const uint32_t*>(src + SH::codes + 4 * (pos * nblk + 32 * run / p.n));
       return o;
     };
@@ -188,7 +195,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void tree_attend(TreeRun p) {
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) O[q][ct] = f32x16_t{};
     }
-    uint32_t one = 0x64006400u, cm = ((1u << BITS) - 1u) * (BITS == 4 || BITS == 2 ? 0x01010101u : 0x00010001u);
+    uint32_t one = 0x64006400u, cm = ((1u << BITS) - 1u) * (BITS <= 4 ? 0x01010101u : 0x00010001u);
     asm("" : "+v"(one), "+v"(cm));
     // side word of a run as the pairs' operands; true if its zhat are not all in binary16 (its largest code's is not)
     auto ranges = [&](uint32_t s, f16x2_t& mn, f16x2_t& sc) {
@@ -200,7 +207,20 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void tree_attend(TreeRun p) {
     // granule g of a run: 8 channels as pairs (tree_channel)
     auto granule = [&](const Raw32& rw, int g, f16x2_t mn, f16x2_t sc) {
       u32x4_t o;
-      if constexpr (BITS == 4 || BITS == 2) {
+      if constexpr (BITS == 3) {
+        const uint32_t* z = rw.w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int c = 2 * g + (j >> 1);  // of 8: at bit 3 c of the words' bytes in a row
+          const uint32_t by = c == 2   ? ((z[0] >> 6) & 0x03030303u) | ((z[1] << 2) & 0x04040404u)
+                              : c == 5 ? ((z[1] >> 7) & 0x01010101u) | ((z[2] << 1) & 0x06060606u)
+                              : c == 3 ? z[1] & (cm << 1)  // twice the codes
+                                       : (z[3 * c / 8] >> (3 * c % 8)) & cm;
+          const float of = c == 3 ? 256.0f : 512.0f;
+          const f16x2_t q = j & 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(by, of, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(by, of, false);
+          o[j] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(q, sc, mn));
+        }
+      } else if constexpr (BITS == 4 || BITS == 2) {
         // a code alone in a byte is 2^-9 of it in 8-bit floating point (e4m3: numbers below 2^-5 are multiples of
         // 2^-9), so one conversion makes binary16 of two
 #pragma unroll
