@@ -136,6 +136,73 @@ def test_against_binary64(name):
     c.check()
 
 
+NARROW = [(0, 1), (0, 8), (130, 0), (63, 1), (64, 5), (1200, 8), (127, 2)]   # all of a row's queries in one group of 32
+
+
+@pytest.mark.parametrize("d,n", [(128, 64), (128, 32), (128, 128), (64, 64)])
+@pytest.mark.parametrize("bits", [2, 3, 4, 6, 8])
+def test_narrow_and_wide_tiles_of_every_width(bits, d, n):
+    for rows, grp in ((NARROW, 4), (RAGGED, 2)):
+        c = Tree(rows, bits=bits, d=d, n=n, g=32 if bits % 4 else 64, grp=grp, seed=bits)
+        c.call()
+        c.check()
+
+
+@pytest.mark.parametrize("kw", [
+    dict(rows=RAGGED), dict(rows=RAGGED, bits=3, d=64, g=16, n=32), dict(rows=NARROW, bits=6, grp=4),
+    dict(rows=[(300, 33), (700, 20), (130, 9)], window=130, sinks=70), dict(rows=RAGGED, masks="random"),
+])
+def test_the_kernel_of_every_other_shape(monkeypatch, kw):
+    """The shapes of the kernel over block-uniform pools, through the one that takes all of them."""
+    monkeypatch.setenv("CG_KERNELS", "generic")
+    c = Tree(**kw)
+    c.call()
+    c.check()
+
+
+def test_one_layer_of_two():
+    """Views of one layer read the pool's that l0 names."""
+    c = Tree([(300, 40), (129, 3)], L=2, grp=4)
+    c.call()
+    torch.cuda.synchronize()
+    both = c.out.clone()
+    c.base.fill_(7.0)
+    for l in (0, 1):
+        cg.kv_attend_tree_paged(l, l + 1, c.qd[l: l + 1], c.cu, c.max_q, c.mask, c.kc, c.vc, cg.page_table(c.pages, c.P), c.Gd, c.shp,
+                                c.codec, c.lens, c.scale, c.out[l: l + 1], None, 0, 0, c.workspace()[0], c.err)
+    torch.cuda.synchronize()
+    _, bound = c.ref()
+    err, size = (c.out - both)[:, 0].double().cpu().norm(dim=-1), both[:, 0].double().cpu().norm(dim=-1)
+    used = int(c.first[-1])    # (parts of other lengths: the error's bound from either side)
+    assert (err <= 2 * bound + 2.0 ** -7 * size)[:, :, :used].all() and int(c.err.item()) == 0
+
+
+def test_two_graphs_that_share_a_workspace():
+    """Captured into two graphs with one workspace, replayed in turn, lengths changed in between: as eager calls."""
+    cases = [Tree([(500, 30), (64, 3)], seed=1), Tree([(77, 16), (900, 9), (3, 5)], bits=3, seed=2)]
+    ws = torch.empty(max(c.workspace()[1] for c in cases), dtype=torch.uint8, device="cuda")
+    stream, graphs = torch.cuda.Stream(), []
+    for c in cases:
+        with torch.cuda.stream(stream):
+            c.call(ws)
+            stream.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=stream):
+                c.call(ws)
+        graphs.append(g)
+    for step in range(4):
+        for c, g in zip(cases, graphs):
+            c.lens.copy_(torch.tensor([h - step for h in c.held], dtype=torch.int32))
+            c.base.fill_(7.0)
+            g.replay()
+            torch.cuda.synchronize()
+            got = c.out.clone()
+            c.base.fill_(7.0)
+            c.call(ws)
+            torch.cuda.synchronize()
+            assert torch.equal(got, c.out) and (got != 7.0).any()
+
+
 def test_masks_of_chains_give_what_the_chunk_attention_gives():
     """The same batch through both: two roundings to bf16 and the operands' 11 bits apart (the bound of the reference, twice)."""
     rows = [(300, 40), (64, 1), (5, 17)]
@@ -251,3 +318,51 @@ def test_on_another_stream():
         c.call()
     s.synchronize()
     c.check()
+
+
+def test_pools_of_more_than_4_gib():
+    """Append, attention, keep in the last pages of pools whose codes pass 2^32 bytes: the bytes of a small pool."""
+    L, H, grp, d, P, n = 1, 8, 4, 128, 256, 64
+    codec = cg.Codec(cg.BLOCK_UNIFORM, 8, n)
+    many, few = 17000, 6                               # 17000 pages of 256 KiB: 4.15 GiB of codes
+    shp, Gd = S.gauge_dev(S.haar(L, H, d, 128, 3))
+    torch.manual_seed(5)
+    rows, N = [(300, 20), (0, 12), (500, 33)], 65
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    cu, lens = i32([0, 20, 32, 65]), i32([320, 12, 533])
+    low = np.array([[0, 1, -1, -1], [2, -1, -1, -1], [3, 4, 5, -1]], np.int32)
+    rng = np.random.default_rng(3)
+    masks, parent, pos = [], [], []
+    for h, t in rows:
+        par = T.tree(t, "near", rng)
+        m, depth = T.closure(par)
+        masks.append(T.words_of(m, 2))
+        parent += list(par)
+        pos += [h + k for k in depth]
+    mask, pos = torch.from_numpy(np.concatenate(masks)).cuda(), i32(pos)
+    path = torch.full((N,), -1, dtype=torch.int32, device="cuda")
+    kept = i32([2, 1, 3])
+    path[0:2], path[20], path[32:35] = i32([0, 5]), 0, i32([0, 7, 20])
+    x = [torch.randn((L, 1, h, N, d), device="cuda").to(torch.bfloat16) for h in (H * grp, H, H)]
+    old = [torch.randn((L, 1, H, 512, d), device="cuda").to(torch.bfloat16) for _ in (0, 1)]
+    plan, res = cg.rope_make(d), []
+    for pages, shift in ((few, 0), (many, many - few)):
+        pools = [cg.Cache(codec, s, L, pages, H, P, d) for s in (0, 1)]
+        table = torch.from_numpy(np.where(low >= 0, low + shift, -1).astype(np.int32)).cuda()
+        slot = lambda b, p: int(low[b][p // P] + shift) * P + p % P  # noqa: E731
+        for b, (h, _) in enumerate(rows):
+            if h:
+                cg.kv_append_slots(0, L, *(t[:, :, :, :h] for t in old), i32([slot(b, p) for p in range(h)]), Gd, shp, codec, *pools)
+        slots = i32([slot(b, h + i) for b, (h, t) in enumerate(rows) for i in range(t)])
+        q, out, err, held = torch.empty_like(x[0]), torch.zeros_like(x[0]), i32([0]), i32([0, 0, 0])
+        cg.kv_append_rope(0, L, plan, x[1], x[2], pos, slots, Gd, shp, codec, *pools, x[0], q, err)
+        ws = torch.empty(cg.attend_tree_workspace_bytes(shp, L, N, 3, H * grp, 4, P), dtype=torch.uint8, device="cuda")
+        pt = cg.page_table(table, P)
+        cg.kv_attend_tree_paged(0, L, q, cu, 33, mask, *pools, pt, Gd, shp, codec, lens, d ** -0.5, out, None, 0, 0, ws, err)
+        cg.kv_tree_keep(0, L, path, kept, cu, lens, pt, codec, *pools, held, err)
+        torch.cuda.synchronize()
+        assert int(err.item()) == 0 and held.tolist() == [302, 1, 503]
+        res.append([out] + [t.view(torch.uint8).view(pages, -1)[shift: shift + few].clone() for p in pools for t in (p.codes, p.side)])
+        del pools
+    assert all(torch.equal(a, b) for a, b in zip(*res))
+    assert (res[0][0] != 0).any(-1).all()
