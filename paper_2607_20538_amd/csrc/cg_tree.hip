@@ -51,7 +51,7 @@ __global__ __launch_bounds__(kTreeThreads) void tree_map(TreeMapArgs a) {
     if (tid == 0 && a.err) atomicOr(a.err, CG_FLAG_POS_RANGE);
     return;
   }
-  const int base = a.lens[b] - n;
+  const int len = a.lens[b], base = len < n ? -1 : len - n;  // (any int may stand there)
   bool bad = base < 0;
   for (int i = tid; i < n; i += kTreeThreads) {
     int p = a.parent[first + i];
@@ -234,8 +234,8 @@ __global__ __launch_bounds__(kTreeThreads) void tree_keep(TreeKeepArgs a) {
   const int b = blockIdx.x / a.groups, grp = blockIdx.x - b * a.groups, tid = threadIdx.x;
   int first;
   const int n = row_nodes(a.cu, b, a.N, CG_TREE_MOST, first);
-  const int len = a.lens[b], kept = a.kept[b], base = len - n, P = a.pt.page_size;
-  bool ok = n >= 0 && base >= 0 && kept >= 0 && kept <= n && len <= int64_t(a.pt.max_pages) * P;
+  const int len = a.lens[b], kept = a.kept[b], base = n < 0 || len < n ? -1 : len - n, P = a.pt.page_size;
+  bool ok = base >= 0 && kept >= 0 && kept <= n && len <= int64_t(a.pt.max_pages) * P;
   int stay = 0;  // nodes at their places: the first ones
   bool fine = true, out = false;
   for (int j = tid; ok && j < kept; j += kTreeThreads) {
@@ -247,7 +247,7 @@ __global__ __launch_bounds__(kTreeThreads) void tree_keep(TreeKeepArgs a) {
   if (!ok) {  // nothing of the row is kept of what was added, where that is known
     if (tid == 0 && grp == 0) {
       if (a.err) atomicOr(a.err, CG_FLAG_POS_RANGE);
-      a.held[b] = n >= 0 && base >= 0 ? base : len;
+      a.held[b] = base >= 0 ? base : len;
     }
     return;
   }

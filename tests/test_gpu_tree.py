@@ -230,6 +230,27 @@ def test_paths_that_cannot_be_kept():
     p.same(p.moved([[], [], [1, 4], [], [], [], []], 0, 1))
 
 
+def test_lengths_that_are_none():
+    """Lengths that no row has, down to the least int32: flagged, nothing of the row moved, read or written."""
+    low, high = -2 ** 31, 2 ** 31 - 1
+    pos, mask, err = torch.full((8,), 77, dtype=torch.int32, device="cuda"), torch.zeros((8, 1), dtype=torch.int64, device="cuda"), i32([0])
+    cg.kv_tree_map(i32([-1, 0] * 4), i32([0, 2, 4, 6, 8]), i32([low, low + 1, -1, 9]), pos, mask, err)
+    torch.cuda.synchronize()
+    assert int(err.item()) == cg.CG_FLAG_POS_RANGE and pos.tolist() == [-1] * 6 + [7, 8] and mask[:, 0].tolist() == [1, 3] * 4
+    rows = [(10, 8)] * 5
+    p = Pools(rows, BU(4, 64), 1, 2, 64, 128, 6)
+    lens, held, err = i32([low, low + 7, -1, high, 18]), i32([9] * 5), i32([0])
+    pt = cg.page_table(p.pages, 64)
+    cg.kv_tree_keep(0, 1, i32(([0, 3, 5] + [-1] * 5) * 5), i32([3] * 5), i32(p.cu), lens, pt, p.codec, *p.dev, held, err)
+    torch.cuda.synchronize()
+    assert int(err.item()) == cg.CG_FLAG_POS_RANGE and held.tolist() == [low, low + 7, -1, high - 8, 13]
+    p.same(p.moved([[], [], [], [], [0, 3, 5]], 0, 1))
+    before, err = p.pages.clone(), i32([0])
+    cg.kv_page_trim(lens, i32([low, low + 7, -1, 3, 13]), p.pool, p.pages, 64, err)
+    torch.cuda.synchronize()
+    assert int(err.item()) == cg.CG_FLAG_POS_RANGE and lens.tolist() == [low, low + 7, -1, high, 13] and torch.equal(before, p.pages)
+
+
 def test_pages_outside_the_pool_are_not_moved():
     rows = [(60, 10), (5, 4)]
     p = Pools(rows, BU(4, 64), 1, 2, 64, 128, 7)
