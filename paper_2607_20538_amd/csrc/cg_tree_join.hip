@@ -8,8 +8,11 @@ namespace cg {
 
 namespace {
 
-// The plan (workgroup 0): every row's tiles, in order, on one line of blocks, cut into `nwg` equal pieces of at least
-// kLeast blocks.  A thread takes a row at a time.
+// The plan (workgroup 0, beside those that make the queries' operands: nothing there waits for it): every row's tiles, in
+// order, on one line of blocks, cut into `nwg` equal pieces, but of at least kLeast blocks and half the root of the longest
+// tile's (a few long rows: a piece costs about 1.3 us a block, joining about 0.4 us a part).  32 short trees behind 200
+// positions: pieces of at least 1, 2, 4, 8 blocks 43, 43, 42, 50 us a call; one tree behind 30000: 4, 8, 12 blocks 68, 58, 61.  A thread takes a
+// row at a time.
 constexpr int kPlanThreads = 256;
 constexpr int kLeast = 4;
 
@@ -26,8 +29,10 @@ __device__ __forceinline__ int tree_blocks(const ChunkDev& a, int base, int held
 __device__ void tree_line(const TreeDev& p) {
   const ChunkDev& a = p.c;
   __shared__ int64_t sums[2][kPlanThreads / 64];
+  __shared__ int longest;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  int turn = 0;
+  int turn = 0, most = 0;
+  if (tid == 0) longest = 0;
   // sum of v over the threads before this one, and over all
   auto scan = [&](int64_t v, int64_t& all) {
     int64_t s = v;
@@ -79,10 +84,14 @@ __device__ void tree_line(const TreeDev& p) {
   int64_t tiles0 = 0, total0 = 0;
   for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
     round(b0, tiles0, total0, true);
+    most = max(most, len);
     tiles0 = tiles;
     total0 = total;
   }
-  const int64_t line = total0, per = max(int64_t(kLeast), (line + p.nwg - 1) / p.nwg);
+  if (most) atomicMax(&longest, most);
+  __syncthreads();
+  const int64_t least = max(kLeast, int(ceilf(0.5f * sqrtf(float(longest)))));
+  const int64_t line = total0, per = max(least, (line + p.nwg - 1) / p.nwg);
   if (tid == 0) *p.line = TreeLine{line, per};
   for (int i = int(min(tiles0, int64_t(a.ntile))) + tid; i < a.ntile; i += kPlanThreads) p.tiles[i] = TreeTile{line, 0, -1, 0, 0, 0, 0, 0, -1};
   tiles0 = total0 = 0;
@@ -142,6 +151,8 @@ __device__ __forceinline__ bf16x8_t gauge_operand8(const uint16_t* blk, int g, i
 
 // q' = G_K q of a tile's queries as the operands that tree_attend reads, one wave per 32 queries and CT / (4 / QT)
 // channel tiles, from the bf16 matrix cores (two split planes of G as in the chunk attention; three of binary32 queries).
+// Latency: 10.4 us for 256 tiles of 64 rows, of which 2.8 until the gauge's loads are under way, 1 to find the tile, 3.4 for
+// queries, gauge and products, 1 to store.
 template <int D, int QT>
 __global__ __launch_bounds__(256) void tree_queries(TreeDev p, GaugeDev G) {
   constexpr int KK = D / 16, CT = D / 32, PARTS = 4 / QT, PER = CT >= PARTS ? CT / PARTS : 1, RH = D / 64;
@@ -270,7 +281,8 @@ __global__ __launch_bounds__(256) void tree_queries(TreeDev p, GaugeDev G) {
 }
 
 // The parts of a tile joined: o = G_V^T (sum_s w_s O_s / sum_s w_s l_s), w_s = 2^(m_s - max m).  A wave takes one group of
-// 32 queries, one channel tile and every GR-th part; then the gauge, an output tile per wave.
+// 32 queries, one channel tile and every GR-th part; then the gauge, an output tile per wave.  Latency: 11.5 us for 256 tiles
+// of 64 rows in 3 parts (2.5 until the parts are asked for, 2.7 until they are here, 1.5 to add the waves', 2 for the gauge).
 template <int D, int QT>
 __global__ __launch_bounds__(512) void tree_join(TreeDev p, GaugeDev G) {
   constexpr int KK = D / 16, CT = D / 32, GR = 8 / (QT * CT) > 0 ? 8 / (QT * CT) : 1, PITCH = D + 4;
@@ -416,7 +428,7 @@ TreePlan tree_plan(int nl, int N, int B, int max_q, int H, int Hq, int d) {
   const int rows = std::min(N, B);
   p.ntile = int(std::min<int64_t>(int64_t(N) / p.tq + rows, std::min<int64_t>(N, int64_t(rows) * ((mq + p.tq - 1) / p.tq))));
   const int64_t lh = int64_t(nl) * H * p.nqc;
-  // two workgroups per CU, what LDS and registers let run at once
+  // as many workgroups as LDS and registers let run at once
   p.nwg = int(std::max<int64_t>(1, (p.qt == 1 ? 3 : 2) * cu_count() / lh));
   size_t off = 256;
   p.off_tiles = off;
