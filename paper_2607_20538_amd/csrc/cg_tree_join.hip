@@ -13,7 +13,7 @@ namespace {
 // tile's (a few long rows: a piece costs about 1.3 us a block, joining about 0.4 us a part).  32 short trees behind 200
 // positions: pieces of at least 1, 2, 4, 8 blocks 43, 43, 42, 50 us a call; one tree behind 30000: 4, 8, 12 blocks 68, 58, 61.  A thread takes a
 // row at a time.
-constexpr int kPlanThreads = 256;
+constexpr int kPlanThreads = 512;
 constexpr int kLeast = 4;
 
 __device__ __forceinline__ int tree_blocks(const ChunkDev& a, int base, int held) {
@@ -149,19 +149,19 @@ __device__ __forceinline__ bf16x8_t gauge_operand8(const uint16_t* blk, int g, i
   return as_bf16x8(o);
 }
 
-// q' = G_K q of a tile's queries as the operands that tree_attend reads, one wave per 32 queries and CT / (4 / QT)
-// channel tiles, from the bf16 matrix cores (two split planes of G as in the chunk attention; three of binary32 queries).
-// Latency: 10.4 us for 256 tiles of 64 rows, of which 2.8 until the gauge's loads are under way, 1 to find the tile, 3.4 for
-// queries, gauge and products, 1 to store.
+// q' = G_K q of a tile's queries as the operands that tree_attend reads, one wave per 32 queries and channel tile (or more
+// of them), from the bf16 matrix cores (two split planes of G as in the chunk attention; three of binary32 queries).
+// Latency: 8.0 us for 256 tiles of 64 rows, with eight waves that fetch queries and gauge together (10.4 with four, the gauge
+// before the tile was known).
 template <int D, int QT>
-__global__ __launch_bounds__(256) void tree_queries(TreeDev p, GaugeDev G) {
-  constexpr int KK = D / 16, CT = D / 32, PARTS = 4 / QT, PER = CT >= PARTS ? CT / PARTS : 1, RH = D / 64;
+__global__ __launch_bounds__(kPlanThreads) void tree_queries(TreeDev p, GaugeDev G) {
+  constexpr int KK = D / 16, CT = D / 32, PARTS = kPlanThreads / 64 / QT, PER = CT >= PARTS ? CT / PARTS : 1, RH = D / 64;
   const ChunkDev& a = p.c;
   if (blockIdx.x == 0) {
     tree_line(p);
     return;
   }
-  __shared__ float mxs[4][32];
+  __shared__ float mxs[kPlanThreads / 64][32];
   const int lane = threadIdx.x & 63, n = lane & 31, hc = lane >> 5, w = threadIdx.x >> 6, q = w % QT, part = w / QT;
   const int inner = a.kc.H * a.nqc;
   int bid = blockIdx.x - 1;
@@ -176,32 +176,34 @@ __global__ __launch_bounds__(256) void tree_queries(TreeDev p, GaugeDev G) {
   // against 9 so)
   constexpr int GPITCH = 2 * D + 16;
   __shared__ __attribute__((aligned(16))) uint8_t gs[2 * D * GPITCH];
-  stage_gauge<2, D, KK, 256, 8>(gs, G.hi, gb, G.g, D, 0, 0);
   int tok0, ntok;
   if (!query_tile(a, t, tok0, ntok)) return;
+  const int j0 = qc * a.heads, nh = min(a.heads, a.grp - j0), rows = ntok * nh;
+  const int r = min(32 * q + n, rows - 1), tok = r / nh, jj = r - tok * nh;
+  const size_t qoff = size_t(lv) * a.q.sl + size_t(h * a.grp + j0 + jj) * a.q.sh + size_t(tok0 + tok) * a.q.st;
+  u32x4_t xb[KK];  // bf16 queries, on their way with the gauge
+  if (on && a.q.bf16) {
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) xb[kk] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(a.q.ptr) + qoff + 16 * kk + 8 * hc);
+  }
+  stage_gauge<2, D, KK, kPlanThreads, 8>(gs, G.hi, gb, G.g, D, 0, 0);
   __syncthreads();
   auto operand = [&](int i, int pl, int kk) {
     return as_bf16x8(*reinterpret_cast<const u32x4_t*>(gs + (pl * D + 32 * (PER * part + i) + n) * GPITCH + 32 * kk + 16 * hc));
   };
-  const int j0 = qc * a.heads, nh = min(a.heads, a.grp - j0), rows = ntok * nh;
-  const int r = min(32 * q + n, rows - 1), tok = r / nh, jj = r - tok * nh;
-  const size_t qoff = size_t(lv) * a.q.sl + size_t(h * a.grp + j0 + jj) * a.q.sh + size_t(tok0 + tok) * a.q.st;
   f32x16_t z[PER];
 #pragma unroll
   for (int i = 0; i < PER; ++i) z[i] = f32x16_t{};
   float mx = 0.0f;
   if (on) {
     if (a.q.bf16) {
-      u32x4_t x[KK];
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) x[kk] = *reinterpret_cast<const u32x4_t*>(static_cast<const uint16_t*>(a.q.ptr) + qoff + 16 * kk + 8 * hc);
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) {
         if (16 * kk > g1 || 16 * kk + 15 < g0) continue;
 #pragma unroll
         for (int i = 0; i < PER; ++i)
 #pragma unroll
-          for (int pl = 0; pl < 2; ++pl) z[i] = mfma(operand(i, pl, kk), as_bf16x8(x[kk]), z[i]);
+          for (int pl = 0; pl < 2; ++pl) z[i] = mfma(operand(i, pl, kk), as_bf16x8(xb[kk]), z[i]);
       }
     } else {
 #pragma unroll
@@ -281,8 +283,8 @@ __global__ __launch_bounds__(256) void tree_queries(TreeDev p, GaugeDev G) {
 }
 
 // The parts of a tile joined: o = G_V^T (sum_s w_s O_s / sum_s w_s l_s), w_s = 2^(m_s - max m).  A wave takes one group of
-// 32 queries, one channel tile and every GR-th part; then the gauge, an output tile per wave.  Latency: 11.5 us for 256 tiles
-// of 64 rows in 3 parts (2.5 until the parts are asked for, 2.7 until they are here, 1.5 to add the waves', 2 for the gauge).
+// 32 queries, one channel tile and every GR-th part; then the gauge, an output tile per wave.  11.5 us for 256 tiles of
+// 64 rows in 3 parts each: 25 MB of parts beside a chain of loads (the first parts fetched with the gauge: no faster).
 template <int D, int QT>
 __global__ __launch_bounds__(512) void tree_join(TreeDev p, GaugeDev G) {
   constexpr int KK = D / 16, CT = D / 32, GR = 8 / (QT * CT) > 0 ? 8 / (QT * CT) : 1, PITCH = D + 4;
@@ -486,7 +488,7 @@ hipError_t launch_tree_attend(const ChunkDev& c0, const TreePlan& p, void* ws, c
   void* args[] = {&a, &g};
   const void* fn = d == 64 ? (p.qt == 1 ? (const void*)tree_queries<64, 1> : (const void*)tree_queries<64, 2>)
                            : (p.qt == 1 ? (const void*)tree_queries<128, 1> : (const void*)tree_queries<128, 2>);
-  hipError_t e = hipLaunchKernel(fn, dim3(unsigned(tiles + 1)), dim3(256), args, 0, st);
+  hipError_t e = hipLaunchKernel(fn, dim3(unsigned(tiles + 1)), dim3(kPlanThreads), args, 0, st);
   if (e != hipSuccess) return e;
   const ChunkDev& b = a.c;
   const TreeRun r{b.kc.codes, b.vc.codes, b.kc.side, b.vc.side, b.pt.pages, b.mask, b.pos, b.err, a.line, a.tiles, a.first, a.qf, a.qs,
