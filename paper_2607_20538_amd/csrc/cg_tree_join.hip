@@ -173,7 +173,7 @@ __global__ __launch_bounds__(kPlanThreads) void tree_queries(TreeDev p, GaugeDev
   int g0 = 0, g1 = -1;
   if (on) reached(G.g, 32 * PER * part, 32 * PER, g0, g1);
   // the gauge comes to LDS in whole rows (operands straight from memory are 64 pieces of 64 lines a load: 15 us a call
-  // against 9 so)
+  // where whole rows took 9)
   constexpr int GPITCH = 2 * D + 16;
   __shared__ __attribute__((aligned(16))) uint8_t gs[2 * D * GPITCH];
   int tok0, ntok;

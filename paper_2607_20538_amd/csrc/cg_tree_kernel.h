@@ -17,14 +17,14 @@
 // Bound by the issue of vector instructions beside the products.  A unit (32 positions, 64 query rows, 128 channels) costs a
 // wave 457 vector instructions and 32 products, 1830 + 1050 cycles that two waves per SIMD overlap in part: about 4000
 // cycles a unit.  32 trees of 8 to 16 nodes behind up to 8192 positions, 8 KV heads x 4, 4 bits: 84 to 87 us over the positions
-// where the bytes take 30 and the products 28; a call 109, by the chunk attention's kernel with masks 237.  Codes become
+// where the bytes take 30 and the products 28; a call 106, by the chunk attention's kernel with masks 237.  Codes become
 // binary16 by one conversion from 8-bit floating point for two (with a mask and a fused multiply-add 11 cycles of issue a
 // pair); 3 bits, four of them to a word after six byte permutations a run: 103 us where code by code it was 124 (24 trees
 // of 25 nodes behind 4096 positions, 16 KV heads x 2).  Without any load of codes a call takes 7 us less, so nothing is fetched further
 // ahead; one wave per SIMD with all 512 registers, or the next unit's scores beside this one's values, took longer;
 // leaving out the second group of queries in tiles of at most 32 rows won 2%, at twice the code.  Workgroups that take
 // turns in priority: 1 to 2%.  A tile of 64 rows where a row's queries fill more than 32: two waves per SIMD instead of
-// three, and a code is decoded half as often (a call for 8 nodes a tree takes 77 us, in tiles of 32, for 16 109).
+// three, and a code is decoded half as often (a call for 8 nodes a tree takes 75 us, in tiles of 32, for 16 106).
 #pragma once
 
 #include "cg_chunk_kernel.h"
