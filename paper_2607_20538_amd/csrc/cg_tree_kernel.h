@@ -15,9 +15,9 @@
 // summed position by position in binary32, in a loop of its own behind the others (within theirs its registers spill).
 //
 // Bound by the issue of vector instructions beside the products.  A unit (32 positions, 64 query rows, 128 channels) costs a
-// wave 457 vector instructions and 32 products, 1830 + 1050 cycles that two waves per SIMD overlap in part: about 4000
+// wave about 430 vector instructions and 32 products, 1720 + 1050 cycles that two waves per SIMD overlap in part: about 4000
 // cycles a unit.  32 trees of 8 to 16 nodes behind up to 8192 positions, 8 KV heads x 4, 4 bits: 84 to 87 us over the positions
-// where the bytes take 30 and the products 28; a call 106, by the chunk attention's kernel with masks 237.  Codes become
+// where the bytes take 30 and the products 28; a call 105, by the chunk attention's kernel with masks 237.  Codes become
 // binary16 by one conversion from 8-bit floating point for two (with a mask and a fused multiply-add 11 cycles of issue a
 // pair); 3 bits, four of them to a word after six byte permutations a run: 103 us where code by code it was 124 (24 trees
 // of 25 nodes behind 4096 positions, 16 KV heads x 2).  Without any load of codes a call takes 7 us less, so nothing is fetched further
@@ -47,6 +47,9 @@ struct TreeShape {
   static constexpr int all = (queries + 4 * wave > joined ? queries + 4 * wave : joined) + 4 * 32 * QT * 8;
   static_assert(wave >= 4 * 2 * D * 4, "space of the rows in binary32");
 };
+
+constexpr float kMostWeight = 16384.0f;  // 2^(kPBias + kLag)
+static_assert(kPBias + kLag == 14.0f, "largest weight");
 
 template <int D, int QT, int BITS>
 __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void tree_attend(TreeRun p) {
@@ -332,32 +335,7 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void tree_attend(TreeRun p) {
       // hidden positions
       const bool whole = !odd && !none && t0 + 32 <= base && (p.window == 0 || t0 > most - p.window || t0 + 32 <= p.sinks);
       f16x8_t W[QT][2];  // weights
-#pragma unroll
-      for (int q = 0; q < QT; ++q) {
-        if (!whole) {
-          const uint32_t seen = odd || none ? 0u : uint32_t(seen_from(q, t0 + 4 * hc));
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const uint32_t keep = uint32_t(__builtin_amdgcn_sbfe(int(seen), 8 * (e >> 2) + (e & 3), 1));
-            S[q][e] = __uint_as_float((__float_as_uint(S[q][e]) & keep) | (0xff800000u & ~keep));
-          }
-        }
-        float mx = S[q][0];
-#pragma unroll
-        for (int e = 1; e < 16; ++e) mx = fmaxf(mx, S[q][e]);
-        mx = halves_max(mx);
-        // the maximum moves only when a score passes it by 2^kLag: the sums are seldom rescaled
-        const bool lift = mx > m[q] && (m[q] == -INFINITY || (mx - m[q]) * cs[q] > kLag);
-        if (__builtin_amdgcn_ballot_w64(lift)) {
-          const float mn = fmaxf(m[q], mx);
-          const float al = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[q] - mn) * cs[q]);
-          m[q] = mn;
-          lsum[q] *= al;
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) O[q][ct][e] *= al;
-        }
+      auto weigh = [&](int q) {
         const float o = kPBias - (m[q] == -INFINITY ? 0.0f : m[q] * cs[q]);
         float ls[2] = {0.0f, 0.0f};
 #pragma unroll
@@ -373,8 +351,46 @@ __global__ __launch_bounds__(256, QT == 1 ? 3 : 2) void tree_attend(TreeRun p) {
           }
           W[q][kp] = as_f16x8(f);
         }
-        lsum[q] += ls[0] + ls[1];
+        return ls[0] + ls[1];
+      };
+      // Weights relative to the largest score so far, before this unit's scores are compared with it: while their sum is at most
+      // 2^(kPBias + kLag) none of them passes what binary16 holds, and the largest score may stay what it was.  Seldom not:
+      // then it is found, and they are formed again (8 trees of 60 nodes 196 -> 190 us a call)
+      float ls[QT];
+      bool again = false;
+#pragma unroll
+      for (int q = 0; q < QT; ++q) {
+        if (!whole) {
+          const uint32_t seen = odd || none ? 0u : uint32_t(seen_from(q, t0 + 4 * hc));
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const uint32_t keep = uint32_t(__builtin_amdgcn_sbfe(int(seen), 8 * (e >> 2) + (e & 3), 1));
+            S[q][e] = __uint_as_float((__float_as_uint(S[q][e]) & keep) | (0xff800000u & ~keep));
+          }
+        }
+        ls[q] = weigh(q);
+        again |= m[q] == -INFINITY || !(ls[q] <= kMostWeight);
       }
+      if (__builtin_amdgcn_ballot_w64(again)) {
+#pragma unroll
+        for (int q = 0; q < QT; ++q) {
+          float mx = S[q][0];
+#pragma unroll
+          for (int e = 1; e < 16; ++e) mx = fmaxf(mx, S[q][e]);
+          mx = halves_max(mx);
+          const float mn = fmaxf(m[q], mx);
+          const float al = mn == m[q] ? 1.0f : __builtin_amdgcn_exp2f((m[q] - mn) * cs[q]);
+          m[q] = mn;
+          lsum[q] *= al;
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) O[q][ct][e] *= al;
+          ls[q] = weigh(q);
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < QT; ++q) lsum[q] += ls[q];
       // values, 16 positions at a time through the wave's rows
 #pragma unroll
       for (int kp = 0; kp < 2; ++kp) {
