@@ -109,65 +109,63 @@ struct Elems {
   }
 };
 
-// Workgroup (bx, by) of a split
+// One row of a thread's channels: the V from c0 and the V from c1, turned
+template <int V, bool BF16, int LAYOUT>
+__device__ __forceinline__ void turn_row(const char* src, char* dst, int c0, int c1, bool turn, const float (&sn)[V], const float (&cn)[V]) {
+  constexpr int ES = BF16 ? 2 : 4;
+  Elems<V, BF16> e0, e1;
+  e0.load(src + ES * c0);
+  e1.load(src + ES * c1);
+  if (turn) {
+    float o0[V], o1[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      if constexpr (LAYOUT == CG_ROPE_HALF) {
+        const float x0 = e0.get(i), x1 = e1.get(i);
+        o0[i] = fmaf(x0, cn[i], -(x1 * sn[i]));
+        o1[i] = fmaf(x0, sn[i], x1 * cn[i]);
+      } else {  // pairs (2 i, 2 i + 1) of the unit's 2 V channels
+        const float x0 = 2 * i < V ? e0.get(2 * i < V ? 2 * i : 0) : e1.get(2 * i < V ? 0 : 2 * i - V);
+        const float x1 = 2 * i + 1 < V ? e0.get(2 * i + 1 < V ? 2 * i + 1 : 0) : e1.get(2 * i + 1 < V ? 0 : 2 * i + 1 - V);
+        const float y0 = fmaf(x0, cn[i], -(x1 * sn[i])), y1 = fmaf(x0, sn[i], x1 * cn[i]);
+        if (2 * i < V) o0[2 * i < V ? 2 * i : 0] = y0;
+        else o1[2 * i < V ? 0 : 2 * i - V] = y0;
+        if (2 * i + 1 < V) o0[2 * i + 1 < V ? 2 * i + 1 : 0] = y1;
+        else o1[2 * i + 1 < V ? 0 : 2 * i + 1 - V] = y1;
+      }
+    }
+    e0.set(o0);
+    e1.set(o1);
+  }
+  e0.store(dst + ES * c0);
+  e1.store(dst + ES * c1);
+}
+// Workgroup (bx, by) of the split of one view
 template <int V, bool BF16, int LAYOUT>
 __device__ __forceinline__ void rope_unit(const RopeArgs& a, int bx, int by) {
   constexpr int ES = BF16 ? 2 : 4;
-  const int idx = bx * 256 + int(threadIdx.x);
-  const int u = idx % a.units, tk = idx / a.units, T = a.x[0].T;
-  if (tk >= a.x[0].B * T || u >= a.skip) return;
-  const int b = tk / T, t = tk - b * T;
-  const int p = a.pos[tk];
-  if (p < 0) return;  // padding: the row stays as it was
-  const int hr = a.plan.d_rot / 2;
+  const ViewDev &X = a.x[0], &Y = a.y[0];
+  const int idx = bx * 256 + int(threadIdx.x), u = idx % a.units, tk = idx / a.units;
+  if (tk >= X.B * X.T || u >= a.skip) return;
+  const int b = tk / X.T, t = tk - b * X.T, p = a.pos[tk], hr = a.plan.d_rot / 2;
+  if (p < 0) return;
   const bool turn = u < hr / V;
   float sn[V], cn[V];
   if (turn) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      sincos_turns(uint64_t(uint32_t(p)) * a.plan.step[u * V + i], sn[i], cn[i]);
-      sn[i] *= a.inverse ? -a.plan.amplitude : a.plan.amplitude;
-      cn[i] *= a.plan.amplitude;
+      pair_turn(a.plan, u * V + i, p, sn[i], cn[i]);
+      if (a.inverse) sn[i] = -sn[i];
     }
   }
-  // first and second run of V channels of the unit
   const int c0 = LAYOUT == CG_ROPE_HALF && turn ? u * V : 2 * u * V;
   const int c1 = LAYOUT == CG_ROPE_HALF && turn ? hr + u * V : c0 + V;
-  const int n0 = a.x[0].L * a.x[0].H, rows = n0 + (a.x[1].H ? a.x[1].L * a.x[1].H : 0);
-  const int r1 = min(rows, (by + 1) * a.per);
+  const int r1 = min(X.L * X.H, (by + 1) * a.per);
 #pragma unroll 2
   for (int r = by * a.per; r < r1; ++r) {
-    const int k = r >= n0, rr = k ? r - n0 : r;
-    const ViewDev &X = a.x[k], &Y = a.y[k];
-    const int lv = rr / X.H, h = rr - lv * X.H;
-    const char* src = static_cast<const char*>(X.ptr) + ES * (lv * X.sl + b * X.sb + h * X.sh + t * X.st);
-    char* dst = static_cast<char*>(Y.ptr) + ES * (lv * Y.sl + b * Y.sb + h * Y.sh + t * Y.st);
-    Elems<V, BF16> e0, e1;
-    e0.load(src + ES * c0);
-    e1.load(src + ES * c1);
-    if (turn) {
-      float o0[V], o1[V];
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        if constexpr (LAYOUT == CG_ROPE_HALF) {
-          const float x0 = e0.get(i), x1 = e1.get(i);
-          o0[i] = fmaf(x0, cn[i], -(x1 * sn[i]));
-          o1[i] = fmaf(x0, sn[i], x1 * cn[i]);
-        } else {  // pairs (2 i, 2 i + 1) of the unit's 2 V channels
-          const float x0 = 2 * i < V ? e0.get(2 * i < V ? 2 * i : 0) : e1.get(2 * i < V ? 0 : 2 * i - V);
-          const float x1 = 2 * i + 1 < V ? e0.get(2 * i + 1 < V ? 2 * i + 1 : 0) : e1.get(2 * i + 1 < V ? 0 : 2 * i + 1 - V);
-          const float y0 = fmaf(x0, cn[i], -(x1 * sn[i])), y1 = fmaf(x0, sn[i], x1 * cn[i]);
-          if (2 * i < V) o0[2 * i < V ? 2 * i : 0] = y0;
-          else o1[2 * i < V ? 0 : 2 * i - V] = y0;
-          if (2 * i + 1 < V) o0[2 * i + 1 < V ? 2 * i + 1 : 0] = y1;
-          else o1[2 * i + 1 < V ? 0 : 2 * i + 1 - V] = y1;
-        }
-      }
-      e0.set(o0);
-      e1.set(o1);
-    }
-    e0.store(dst + ES * c0);
-    e1.store(dst + ES * c1);
+    const int lv = r / X.H, h = r - lv * X.H;
+    turn_row<V, BF16, LAYOUT>(static_cast<const char*>(X.ptr) + ES * (lv * X.sl + b * X.sb + h * X.sh + t * X.st),
+                              static_cast<char*>(Y.ptr) + ES * (lv * Y.sl + b * Y.sb + h * Y.sh + t * Y.st), c0, c1, turn, sn, cn);
   }
 }
 

@@ -23,7 +23,38 @@ namespace {
 
 template <int V, bool BF16, int LAYOUT>
 __global__ __launch_bounds__(256) void rope_rows(RopeArgs a) {
-  rope_unit<V, BF16, LAYOUT>(a, blockIdx.x, blockIdx.y);
+  constexpr int ES = BF16 ? 2 : 4;
+  const int idx = blockIdx.x * 256 + threadIdx.x;
+  const int u = idx % a.units, tk = idx / a.units, T = a.x[0].T;
+  if (tk >= a.x[0].B * T || u >= a.skip) return;
+  const int b = tk / T, t = tk - b * T;
+  const int p = a.pos[tk];
+  if (p < 0) return;  // padding: the row stays as it was
+  const int hr = a.plan.d_rot / 2;
+  const bool turn = u < hr / V;
+  float sn[V], cn[V];
+  if (turn) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      sincos_turns(uint64_t(uint32_t(p)) * a.plan.step[u * V + i], sn[i], cn[i]);
+      sn[i] *= a.inverse ? -a.plan.amplitude : a.plan.amplitude;
+      cn[i] *= a.plan.amplitude;
+    }
+  }
+  // first and second run of V channels of the unit
+  const int c0 = LAYOUT == CG_ROPE_HALF && turn ? u * V : 2 * u * V;
+  const int c1 = LAYOUT == CG_ROPE_HALF && turn ? hr + u * V : c0 + V;
+  const int n0 = a.x[0].L * a.x[0].H, rows = n0 + (a.x[1].H ? a.x[1].L * a.x[1].H : 0);
+  const int r1 = min(rows, int(blockIdx.y + 1) * a.per);
+#pragma unroll 2
+  for (int r = blockIdx.y * a.per; r < r1; ++r) {
+    const int k = r >= n0, rr = k ? r - n0 : r;
+    const ViewDev &X = a.x[k], &Y = a.y[k];
+    const int lv = rr / X.H, h = rr - lv * X.H;
+    const char* src = static_cast<const char*>(X.ptr) + ES * (lv * X.sl + b * X.sb + h * X.sh + t * X.st);
+    char* dst = static_cast<char*>(Y.ptr) + ES * (lv * Y.sl + b * Y.sb + h * Y.sh + t * Y.st);
+    turn_row<V, BF16, LAYOUT>(src, dst, c0, c1, turn, sn, cn);
+  }
 }
 
 template <int V, bool BF16>
