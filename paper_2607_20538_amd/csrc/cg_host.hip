@@ -440,7 +440,6 @@ static hipError_t launch_append_slots(const ViewDev& Kn, const ViewDev& Vn, int 
   // ... where keys turn, in two launches beside that of the queries: 22 us (rows of an append: 19) at 800 tokens of 8 heads, 42
   // : 42 at 2200, 67 : 95 at 6400; 8 layers of 8 heads 43 : 42 at 307, 68 : 96 at 845 (32 query heads turned as well)
   constexpr int64_t kTurnRows = 20480;
-  constexpr int kJoinTokens = 2048;        // at most so many: their queries turn in the append's launch
   if (!force_generic() && int64_t(Kn.T) * Kn.L * Kn.H >= (turn ? kTurnRows : kEncodeRows) && (!turn || turn_supported(*plan)) &&
       mfma_encode_supported(Kn, G, c, true) && mfma_encode_supported(Vn, G, c, true)) {
     if (turn) {
@@ -450,12 +449,14 @@ static hipError_t launch_append_slots(const ViewDev& Kn, const ViewDev& Vn, int 
     }
     return launch_encode_slots(Kn, Vn, l0, slots, G, c, kc, vc, err, st, turn);
   }
-  if (q && (q->gx == 0 || q->V != 8 || Kn.T > kJoinTokens)) {
+  constexpr int kMost = 1 << 19;  // tokens of a launch: 2^15 groups of 16, of the 65535 that its grid's second dimension holds
+  // queries turn in the append's launch where it is one: 8.2 us (in a launch of their own before it 11.8) for 206 tokens of 8
+  // heads and 32 query heads, 32 : 36 for 1685, 48 : 52 for 8450 of 64 channels
+  if (q && (q->gx == 0 || q->V != 8 || Kn.T > kMost)) {
     const hipError_t e = launch_rope_split(*q, st);
     if (e != hipSuccess) return e;
     q = nullptr;
   }
-  constexpr int kMost = 1 << 19;  // tokens of a launch: 2^15 groups of 16, of the 65535 that its grid's second dimension holds
   for (int i0 = 0; i0 < Kn.T; i0 += kMost) {
     ViewDev x[2] = {Kn, Vn};
     for (ViewDev& v : x) {
