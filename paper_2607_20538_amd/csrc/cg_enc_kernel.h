@@ -120,8 +120,9 @@ __device__ __forceinline__ void cut3(float x0, float x1, uint32_t& hi, uint32_t&
 // a token turn its 16 granules, as pairs of them or within them, in binary32, and cut every value into three bfloat16
 // planes that hold all of its 24 bits.  Six products with the gauge's three planes (the dropped ones are 2^-24 of the
 // largest) leave z as close to the binary64 product as the other encoders do.  9187 tokens of 8 heads, g = 128,
-// 4 bits: 31 to 33 us, the values 19 in a launch of their own (append_rows 108 for both); bound by the vector work of the sines and of cutting, 3.2 us per tile where two
-// workgroups share a CU, after 6 us until the first tile: all are resident at once, five tiles each.
+// 4 bits: 31 to 33 us, the values 19 in a launch of their own (append_rows 108 for both); bound by the vector work of
+// the sines and of cutting, 3.2 us per tile where two workgroups share a CU, after 6 us until the first tile: all are
+// resident at once, five tiles each.
 // kDestPages (PAGED): the cache is a page pool; the rows of a tile (always inside one page) go to the page its
 // positions map to, looked up one tile ahead of the tile's first use.  Blocks with a non-finite value are
 // coded again after the range (recode_rows).
