@@ -497,9 +497,9 @@ int32_t kv_page_trim(int32_t* lens, const int32_t* keep, int32_t B, const cg_pag
 /* A step that checks trees of drafted tokens: every row adds a tree (or several) of tokens behind the positions it
  * holds, packed row after row as kv_page_map packs them (cu, lens and slots are its), the model runs once over all of
  * them, and one path of each tree is kept.  parent: device int32 [N], the parent of a packed token as an index within its row's
- * nodes (-1: a root), always an earlier node.  A row has at most CG_TREE_MOST nodes.  In order: kv_page_map, kv_tree_map,
- * for every layer kv_append_rope and kv_attend_tree_paged, then kv_tree_accept (or a rule of the caller's), kv_tree_keep,
- * kv_page_trim. */
+ * nodes (-1: a root), always an earlier node.  A row has at most CG_TREE_MOST nodes.  In order: kv_page_map, kv_tree_map
+ * (kv_tree_map_window where the attention has a window), for every layer kv_append_rope and kv_attend_tree_paged, then
+ * kv_tree_accept (or a rule of the caller's), kv_tree_keep, kv_page_trim. */
 
 /* Positions and masks of trees, from their parents:
  *   pos[i]   lens[b] - n_b + depth of the token's node (device int32 [N]; roots have depth 0)
@@ -511,6 +511,13 @@ int32_t kv_page_trim(int32_t* lens, const int32_t* keep, int32_t B, const cg_pag
  * sets it and is left as it was.  Errors: CG_ERR_ARG, CG_ERR_ALIGN, CG_ERR_DEVICE. */
 int32_t kv_tree_map(const int32_t* parent, const int32_t* cu, const int32_t* lens, int32_t B, int32_t N, int32_t words,
                     int32_t* pos, uint64_t* mask, int32_t* err_flag, void* stream);
+
+/* kv_tree_map for an attention with a window: a node's mask leaves out the ancestors that `window` hides, those at positions
+ * q <= p - window of a node at position p, unless q < sinks (positions as in pos; of a row whose lens is below n_b as
+ * if its roots were at 0).  window 0: kv_tree_map.  Errors: as kv_tree_map; CG_ERR_ARG for a negative window or sinks. */
+int32_t kv_tree_map_window(const int32_t* parent, const int32_t* cu, const int32_t* lens, int32_t B, int32_t N,
+                           int32_t words, int32_t window, int32_t sinks, int32_t* pos, uint64_t* mask,
+                           int32_t* err_flag, void* stream);
 
 /* kv_rope of keys and queries and kv_append_slots in one call: token i of k_new, v_new [l1 - l0][1][H][N][d] goes to
  * slots[i], its key turned by pos[i] (device int32 [N]) as `plan` says, with no rounding between turn and gauge; q
@@ -533,9 +540,10 @@ size_t attend_tree_workspace_bytes(cg_gauge_shape shp, int32_t nl, int32_t N, in
  * n_b, with base = lens[b] - n_b positions held before them, sees
  *   positions t < base    with  window == 0 or t > p - window or t < sinks,   p = max(pos[i], base),
  *   positions base + j    with  bit j of its mask set, j < n_b (itself only if its own bit is),
- * so a tree's masks (kv_tree_map) give every node what it would see at the end of its own path.  mask: device uint64
- * [N][words], words >= ceil(max_q / 64), 8-byte aligned.  pos: device int32 [N] (NULL if window is 0).  The window hides no node.  A token
- * that sees nothing gets zeros.  Everything else as kv_attend_chunk_paged; max_q at most CG_TREE_MOST.  workspace: as
+ * so a tree's masks give every node what it would see at the end of its own path: those of kv_tree_map, or with a window
+ * those of kv_tree_map_window for the same window and sinks (of the new tokens the window itself hides none here: masks
+ * without it show a node all of its ancestors).  mask: device uint64 [N][words], words >= ceil(max_q / 64), 8-byte aligned.
+ * pos: device int32 [N] (NULL if window is 0).  A token that sees nothing gets zeros.  Everything else as kv_attend_chunk_paged; max_q at most CG_TREE_MOST.  workspace: as
  * attend_tree_workspace_bytes says, 16-byte aligned.  Errors: as kv_attend_chunk_paged. */
 int32_t kv_attend_tree_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const int32_t* cu, int32_t B, int32_t max_q,
                              const uint64_t* mask, int32_t words, const int32_t* pos, const cg_cache* kc,

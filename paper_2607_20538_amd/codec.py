@@ -33,7 +33,7 @@ EXPORTS = ["cg_status_str", "gauge_device_bytes", "gauge_make", "cache_bytes", "
            "attend_paged_workspace_bytes", "kv_attend_paged", "kv_encode_paged", "kv_append_paged",
            "kv_page_map", "kv_page_release", "rope_make", "kv_rope", "kv_append_slots",
            "attend_chunk_workspace_bytes", "attend_chunk_workspace_limit", "kv_attend_chunk_paged",
-           "kv_page_trim", "kv_tree_map", "kv_append_rope", "attend_tree_workspace_bytes", "kv_attend_tree_paged",
+           "kv_page_trim", "kv_tree_map", "kv_tree_map_window", "kv_append_rope", "attend_tree_workspace_bytes", "kv_attend_tree_paged",
            "kv_tree_accept", "kv_tree_keep", "cg_selftest", "cg_stream_probe"]
 
 
@@ -164,6 +164,8 @@ def lib() -> C.CDLL:
         L.kv_page_trim.restype = i32
         L.kv_tree_map.argtypes = [p, p, p, i32, i32, i32, p, p, p, p]
         L.kv_tree_map.restype = i32
+        L.kv_tree_map_window.argtypes = [p, p, p, i32, i32, i32, i32, i32, p, p, p, p]
+        L.kv_tree_map_window.restype = i32
         L.kv_append_rope.argtypes = [i32, i32, C.POINTER(RopePlan), C.POINTER(KvView), C.POINTER(KvView),
                                      C.POINTER(KvView), C.POINTER(KvView), p, p, p, GaugeShape, C.POINTER(CodecStruct),
                                      C.POINTER(CacheStruct), C.POINTER(CacheStruct), p, p]
@@ -644,18 +646,19 @@ def _mask(fn: str, mask, N: int) -> int:
     return mask.shape[1]
 
 
-def kv_tree_map(parent, cu, lens, pos, mask, err_flag=None, stream=None):
+def kv_tree_map(parent, cu, lens, pos, mask, err_flag=None, stream=None, window: int = 0, sinks: int = 0):
     """Positions pos (int32 [N]) and masks (int64 [N][words]: bit j mod 64 of word j / 64 for the node itself and its
     ancestors) of the packed trees whose nodes' parents (int32 [N], indices within the row, -1: a root) are `parent`;
-    row b's nodes are cu[b] .. cu[b + 1], the last of its lens[b] positions."""
+    row b's nodes are cu[b] .. cu[b + 1], the last of its lens[b] positions.  window, sinks: those of the attention that
+    reads the masks; an ancestor `window` or more positions before its node is left out unless its position is below `sinks`."""
     _on_device("kv_tree_map", parent=parent, cu=cu, lens=lens, pos=pos, mask=mask, err_flag=err_flag)
     B, N = lens.numel(), parent.numel()
     _int32("kv_tree_map", N, parent=parent, pos=pos)
     _int32("kv_tree_map", B, lens=lens)
     _int32("kv_tree_map", B + 1, cu=cu)
     words = _mask("kv_tree_map", mask, N)
-    rc = lib().kv_tree_map(_ptr(parent), _ptr(cu), _ptr(lens), B, N, words, _ptr(pos), _ptr(mask), _ptr(err_flag),
-                           _stream(stream))
+    rc = lib().kv_tree_map_window(_ptr(parent), _ptr(cu), _ptr(lens), B, N, words, window, sinks, _ptr(pos), _ptr(mask),
+                                  _ptr(err_flag), _stream(stream))
     _check("kv_tree_map", rc)
 
 
@@ -685,8 +688,8 @@ def kv_attend_tree_paged(l0: int, l1: int, q, cu, max_q: int, mask, kc: Cache, v
                          workspace=None, err_flag=None, stream=None):
     """Attention of the packed tokens q [l1-l0][1][Hq][N][d] (row b's: cu[b] .. cu[b+1], at most max_q) over page pools that
     hold them: all of what the row held before them (behind a window by the tokens' pos, int32 [N], the first `sinks` stay
-    visible) and of its new tokens those whose bits are set in a token's mask (int64 [N][words]); lens: int32 [B] positions
-    held with the new tokens.  Writes out (q's shape)."""
+    visible) and of its new tokens those whose bits are set in a token's mask (int64 [N][words]; with a window made by
+    kv_tree_map with the same window and sinks); lens: int32 [B] positions held with the new tokens.  Writes out (q's shape)."""
     _on_device("kv_attend_tree_paged", q=q, cu=cu, mask=mask, pos=pos, codes=kc.codes, v_codes=vc.codes, G_dev=G_dev, lens=lens,
                out=out, workspace=workspace, err_flag=err_flag)
     B = lens.numel()

@@ -1152,10 +1152,18 @@ int32_t kv_append_rope(int32_t l0, int32_t l1, const cg_rope_plan* plan, const c
 
 int32_t kv_tree_map(const int32_t* parent, const int32_t* cu, const int32_t* lens, int32_t B, int32_t N, int32_t words,
                     int32_t* pos, uint64_t* mask, int32_t* err_flag, void* stream) {
+  return kv_tree_map_window(parent, cu, lens, B, N, words, 0, 0, pos, mask, err_flag, stream);
+}
+
+int32_t kv_tree_map_window(const int32_t* parent, const int32_t* cu, const int32_t* lens, int32_t B, int32_t N,
+                           int32_t words, int32_t window, int32_t sinks, int32_t* pos, uint64_t* mask,
+                           int32_t* err_flag, void* stream) {
   if (!cu || !lens || B <= 0 || B == INT32_MAX || N < 0 || words <= 0 || (N && (!parent || !pos || !mask))) return CG_ERR_ARG;
+  if (window < 0 || sinks < 0) return CG_ERR_ARG;
   if (!aligned4(parent) || !aligned4(cu) || !aligned4(lens) || !aligned4(pos) || !aligned4(err_flag) || !aligned8(mask))
     return CG_ERR_ALIGN;
-  hipError_t e = launch_tree_map(parent, cu, lens, B, N, words, pos, mask, err_flag, static_cast<hipStream_t>(stream));
+  hipError_t e = launch_tree_map(parent, cu, lens, B, N, words, window, sinks, pos, mask, err_flag,
+                                 static_cast<hipStream_t>(stream));
   return e == hipSuccess ? CG_OK : CG_ERR_DEVICE;
 }
 

@@ -199,8 +199,8 @@ hipError_t launch_page_map(const int* held, const int* add, int B, const cg_page
 hipError_t launch_page_release(int* lens, const int* done, int B, const cg_page_pool& pool, int* pages, int max_pages,
                                int P, int* err, bool trim, hipStream_t st);
 // Trees of drafted tokens: positions and masks, the accepted paths, their entries moved together.
-hipError_t launch_tree_map(const int* parent, const int* cu, const int* lens, int B, int N, int words, int* pos,
-                           uint64_t* mask, int* err, hipStream_t st);
+hipError_t launch_tree_map(const int* parent, const int* cu, const int* lens, int B, int N, int words, int window,
+                           int sinks, int* pos, uint64_t* mask, int* err, hipStream_t st);
 hipError_t launch_tree_accept(const int* parent, const int* cu, const int* draft, const int* target, const int* head,
                               int B, int N, int* path, int* kept, int* next, int* err, hipStream_t st);
 hipError_t launch_tree_keep(const int* path, const int* kept, const int* cu, const int* lens, int B, int N,

@@ -27,13 +27,26 @@ __device__ __forceinline__ int row_nodes(const int* cu, int b, int N, int most, 
 // gives that word and the first ancestor below it; then from word to word, whole words at a time.  So a node
 // takes at most 64 + n / 64 dependent LDS reads, a shallow one as many as its depth.  32 trees of 16 nodes 2.8 us, 256 of up
 // to 250 (1.5 MB of masks) 3.5: little more than a launch.
+//
+// A window hides ancestors as it hides held positions: of a node at depth k, position base + k, those at depths from
+// sinks - base up to k - window.  Ancestors lie in order of their depth in a mask (a parent is an earlier node), so they
+// are a run of its set bits; the depth is counted before the words are written.
 struct TreeMapArgs {
   const int *parent, *cu, *lens;
-  int B, N, words;
+  int B, N, words, window, sinks;
   int* pos;
   uint64_t* mask;
   int* err;
 };
+
+// m without its set bits of rank lo .. hi - 1, counted from the lowest
+__device__ __forceinline__ uint64_t without_ranks(uint64_t m, int lo, int hi) {
+  uint64_t x = m;
+  for (int i = 0; i < lo; ++i) x &= x - 1;
+  uint64_t y = x;
+  for (int i = lo; i < hi; ++i) y &= y - 1;
+  return (m ^ x) | y;
+}
 
 __global__ __launch_bounds__(kTreeThreads) void tree_map(TreeMapArgs a) {
   __shared__ int up[CG_TREE_MOST];         // parent
@@ -75,14 +88,26 @@ __global__ __launch_bounds__(kTreeThreads) void tree_map(TreeMapArgs a) {
     out[i] = x;
   }
   __syncthreads();
+  const int shown = a.window > 0 ? min(max(a.sinks - max(base, 0), 0), n) : 0;  // depths that are sinks
   for (int i = tid; i < n; i += kTreeThreads) {
     uint64_t* dst = a.mask + size_t(first + i) * a.words;
-    int x = i, depth = -1, w = a.words - 1;
+    int depth = -1;
+    if (a.window > 0) {
+      for (int x = i; x >= 0; x = out[x]) depth += __popcll(own[x]);
+    }
+    const int hidden = depth - a.window + 1;  // ancestors at depths below, where there is a window
+    int left = depth + 1, x = i, w = a.words - 1;
     while (x >= 0) {
       for (; w > x >> 6; --w) dst[w] = 0;
-      const uint64_t m = own[x];
+      uint64_t m = own[x];
+      if (a.window > 0) {
+        const int k = __popcll(m);
+        left -= k;  // depth of the word's first
+        m = without_ranks(m, min(max(shown - left, 0), k), min(max(hidden - left, 0), k));
+      } else {
+        depth += __popcll(m);
+      }
       dst[w--] = m;
-      depth += __popcll(m);
       x = out[x];
     }
     for (; w >= 0; --w) dst[w] = 0;
@@ -283,9 +308,9 @@ __global__ __launch_bounds__(kTreeThreads) void tree_keep(TreeKeepArgs a) {
 
 }  // namespace
 
-hipError_t launch_tree_map(const int* parent, const int* cu, const int* lens, int B, int N, int words, int* pos, uint64_t* mask,
-                           int* err, hipStream_t st) {
-  TreeMapArgs a{parent, cu, lens, B, N, words, pos, mask, err};
+hipError_t launch_tree_map(const int* parent, const int* cu, const int* lens, int B, int N, int words, int window, int sinks,
+                           int* pos, uint64_t* mask, int* err, hipStream_t st) {
+  TreeMapArgs a{parent, cu, lens, B, N, words, window, sinks, pos, mask, err};
   hipLaunchKernelGGL(tree_map, dim3(B + 1), dim3(kTreeThreads), 0, st, a);
   return hipGetLastError();
 }
