@@ -566,8 +566,9 @@ int32_t kv_tree_accept(const int32_t* parent, const int32_t* cu, const int32_t* 
 
 /* Moves kept paths together: for layers [l0, l1) and every head of both pools, the entry of row b's position
  * base + path[cu[b] + j] (base = lens[b] - n_b) goes to position base + j, j < kept[b], bit for bit; what was written behind them
- * stays, and is no part of the row once it is trimmed.  path as kv_tree_accept writes it: ascending nodes.  held[b] (device int32 [B], not
- * lens itself) becomes base + kept[b], what kv_page_trim takes.  lens is not modified.  A row whose kept is negative or
+ * stays, and is no part of the row once it is trimmed.  path as kv_tree_accept writes it: ascending nodes.  held[b] becomes
+ * base + kept[b], what kv_page_trim takes (device int32 [B], no element of it in lens, kept, cu or path: CG_ERR_ARG, as other
+ * workgroups of a row still read them).  lens is not modified.  A row whose kept is negative or
  * above n_b, whose path does not ascend within the row, whose lens is below n_b or past its table, or whose cu is as in
  * kv_tree_accept, sets CG_FLAG_POS_RANGE and moves nothing; held[b] becomes base (lens[b] where that is not known).  A
  * page outside the pool sets it and its entries are not moved.  Caches: page pools as in kv_attend_paged, no page in two rows'

@@ -734,8 +734,8 @@ def kv_tree_accept(parent, cu, draft, target, path, kept, next, head=None, err_f
 def kv_tree_keep(l0: int, l1: int, path, kept, cu, lens, pt: PageTable, codec: Codec, kc: Cache, vc: Cache, held,
                  err_flag=None, stream=None):
     """Moves the entries of each row's kept nodes (path, kept: as kv_tree_accept writes them) of both pools to the first places
-    behind what the row held before its cu[b + 1] - cu[b] nodes; held (int32 [B]) becomes the positions it then holds, for
-    kv_page_trim (lens stay as they are)."""
+    behind what the row held before its cu[b + 1] - cu[b] nodes; held (int32 [B], a buffer of its own) becomes the positions it
+    then holds, for kv_page_trim (lens stay as they are)."""
     _on_device("kv_tree_keep", path=path, kept=kept, cu=cu, lens=lens, held=held, codes=kc.codes, v_codes=vc.codes,
                err_flag=err_flag)
     B, N = lens.numel(), path.numel()

@@ -385,6 +385,11 @@ int32_t check_apart(const cg_kv_view* v) {
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 bool aligned8(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 7u) == 0; }
+// Whether n int32 of one and m of the other share an element
+bool share(const int32_t* a, int64_t n, const int32_t* b, int64_t m) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + 4 * uintptr_t(m) && y < x + 4 * uintptr_t(n);
+}
 
 // A query or output view of kv_attend: [nl][B][Hq][1][d], Hq a multiple of the KV heads.
 int32_t check_qview(const cg_kv_view* v, const cg_gauge_shape& s, int L) {
@@ -1196,6 +1201,9 @@ int32_t kv_tree_keep(int32_t l0, int32_t l1, const int32_t* path, const int32_t*
   if (int64_t(kc->B) * kc->T_cap > INT32_MAX || int64_t(pages->max_pages) * pages->page_size > INT32_MAX)
     return CG_ERR_CAPACITY;
   if (int64_t(2) * (l1 - l0) * shp.H > INT32_MAX / B) return CG_ERR_CAPACITY;
+  // (one workgroup of a row writes held while others of it read the rest)
+  if (share(held, B, lens, B) || share(held, B, kept, B) || share(held, B, cu, int64_t(B) + 1) || share(held, B, path, N))
+    return CG_ERR_ARG;
   PageDev pt;
   pt.pages = pages->pages;
   pt.max_pages = pages->max_pages;
