@@ -505,9 +505,9 @@ int32_t kv_page_trim(int32_t* lens, const int32_t* keep, int32_t B, const cg_pag
  *   pos[i]   lens[b] - n_b + depth of the token's node (device int32 [N]; roots have depth 0)
  *   mask[i]  bit j mod 64 of word j / 64: node j of the row is the token itself or one of its ancestors (device uint64
  *            [N][words])
- * with n_b = cu[b + 1] - cu[b] nodes and lens[b] positions held, the nodes among them (device int32 [B]).  Tokens behind the last row
- * get pos -1 and mask 0.  A parent that is not an earlier node sets CG_FLAG_POS_RANGE and counts as -1; a row whose lens
- * is below n_b sets it and gets pos -1; a row whose cu runs backwards, past N, or over min(64 words, CG_TREE_MOST) nodes
+ * with n_b = cu[b + 1] - cu[b] nodes and lens[b] positions held, the nodes among them (device int32 [B]).  Tokens behind the rows
+ * (from the largest of cu on) get pos -1 and mask 0.  A parent that is not an earlier node sets CG_FLAG_POS_RANGE and
+ * counts as -1; a row whose lens is below n_b sets it and gets pos -1; a row whose cu runs backwards, past N, or over min(64 words, CG_TREE_MOST) nodes
  * sets it and is left as it was.  Errors: CG_ERR_ARG, CG_ERR_ALIGN, CG_ERR_DEVICE. */
 int32_t kv_tree_map(const int32_t* parent, const int32_t* cu, const int32_t* lens, int32_t B, int32_t N, int32_t words,
                     int32_t* pos, uint64_t* mask, int32_t* err_flag, void* stream);
@@ -557,8 +557,8 @@ int32_t kv_attend_tree_paged(int32_t l0, int32_t l1, const cg_kv_view* q, const 
  *   path[cu[b] + j], j < kept[b]   the kept nodes of row b in order, -1 from there to the row's end (device int32 [N])
  *   kept[b]                        their number (device int32 [B])
  *   next[b]                        the model's choice after the last of them (none: head[b], or -1; device int32 [B])
- * and path -1 behind the last row.  A parent that is not an earlier node sets CG_FLAG_POS_RANGE, its node is not kept; a row whose cu
- * runs backwards, past N or over CG_TREE_MOST nodes sets it, gets kept 0 and next -1, and its path is left as it was.
+ * and path -1 behind the rows (from the largest of cu on).  A parent that is not an earlier node sets CG_FLAG_POS_RANGE,
+ * its node is not kept; a row whose cu runs backwards, past N or over CG_TREE_MOST nodes sets it, gets kept 0 and next -1, and its path is left as it was.
  * Errors: CG_ERR_ARG, CG_ERR_ALIGN, CG_ERR_DEVICE. */
 int32_t kv_tree_accept(const int32_t* parent, const int32_t* cu, const int32_t* draft, const int32_t* target,
                        const int32_t* head, int32_t B, int32_t N, int32_t* path, int32_t* kept, int32_t* next,

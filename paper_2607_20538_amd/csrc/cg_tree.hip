@@ -20,6 +20,18 @@ __device__ __forceinline__ int row_nodes(const int* cu, int b, int N, int most, 
   return first < 0 || n < 0 || first > N - n || n > most ? -1 : n;
 }
 
+// First token behind all rows: cu[B], or where rows run backwards (other workgroups write the tokens of those before
+// them) the largest of cu.  By each wave for itself
+__device__ __forceinline__ int rows_end(const int* cu, int B, int N) {
+  int end = cu[B];
+  if (end < N) {
+    for (int b = threadIdx.x & 63; b < B; b += 64) end = max(end, cu[b]);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) end = max(end, __shfl_xor(end, o));
+  }
+  return min(max(end, 0), N);
+}
+
 // ------------------------------------------------------------------------------------------
 // positions and masks
 // ------------------------------------------------------------------------------------------
@@ -54,7 +66,7 @@ __global__ __launch_bounds__(kTreeThreads) void tree_map(TreeMapArgs a) {
   __shared__ int out[CG_TREE_MOST];        // its first ancestor below that word, -1: none
   const int b = blockIdx.x, tid = threadIdx.x;
   if (b == a.B) {  // behind the last row
-    const int end = min(max(a.cu[a.B], 0), a.N);
+    const int end = rows_end(a.cu, a.B, a.N);
     for (int64_t x = int64_t(end) * a.words + tid; x < int64_t(a.N) * a.words; x += kTreeThreads) a.mask[x] = 0;
     for (int i = end + tid; i < a.N; i += kTreeThreads) a.pos[i] = -1;
     return;
@@ -132,7 +144,7 @@ __global__ __launch_bounds__(64) void tree_accept(TreeAcceptArgs a) {
   __shared__ int up[CG_TREE_MOST], said[CG_TREE_MOST];
   const int b = blockIdx.x, lane = threadIdx.x;
   if (b == a.B) {
-    for (int i = min(max(a.cu[a.B], 0), a.N) + lane; i < a.N; i += 64) a.path[i] = -1;
+    for (int i = rows_end(a.cu, a.B, a.N) + lane; i < a.N; i += 64) a.path[i] = -1;
     return;
   }
   int first;
