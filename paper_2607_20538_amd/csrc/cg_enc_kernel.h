@@ -82,7 +82,7 @@ constexpr int kModePass = 1;   // error-free backend: binary32 z
 constexpr int kModeKeys = 2;   // KIVI keys: one block per channel over a 32-token group
 constexpr int kModeZfp = 3;    // zfp-style fixed-rate blocks of 4 tokens x 4 channels (BITS = rate)
 
-// where rows go: the batch row, its pages, the tokens' slots (at most kSlotTiles tiles per workgroup), the slots after
+// where rows go: the batch row, its pages, the tokens' slots (at most slot_tiles tiles per workgroup), the slots after
 // the keys' turn
 constexpr int kDestRows = 0, kDestPages = 1, kDestSlots = 2, kDestTurned = 3;
 constexpr int slot_tiles(int dest) { return dest == kDestTurned ? 16 : 32; }

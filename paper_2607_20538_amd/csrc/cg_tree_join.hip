@@ -136,19 +136,6 @@ __device__ __forceinline__ bool query_tile(const ChunkDev& a, int tile, int& tok
   return false;
 }
 
-// Element row r, channels 16 kk + 8 hc .. + 7 of a head's block-diagonal matrix out of one bf16 plane
-__device__ __forceinline__ bf16x8_t gauge_operand8(const uint16_t* blk, int g, int d, int row, int c0) {
-  u32x4_t o = {0u, 0u, 0u, 0u};
-  if (g % 8) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) o[e >> 1] |= gauge_at(blk, g, d, row, c0 + e) << (16 * (e & 1));
-  } else {
-    const int r = row / g;
-    if (c0 >= r * g && c0 < (r + 1) * g) o = *reinterpret_cast<const u32x4_t*>(blk + size_t(r) * g * g + (row - r * g) * g + (c0 - r * g));
-  }
-  return as_bf16x8(o);
-}
-
 // q' = G_K q of a tile's queries as the operands that tree_attend reads, one wave per 32 queries and channel tile (or more
 // of them), from the bf16 matrix cores (two split planes of G as in the chunk attention; three of binary32 queries).
 // Latency: 8.0 us for 256 tiles of 64 rows, with eight waves that fetch queries and gauge together (10.4 with four, the gauge
@@ -448,8 +435,7 @@ TreePlan tree_plan(int nl, int N, int B, int max_q, int H, int Hq, int d) {
   return p;
 }
 
-// lh (nwg + ntile) is at most 2 CUs + lh (1 + ntile); a tile is of 32 or 64 rows, at least 32 of them (half, where heads do not
-// divide them) of tokens but for one tile of every row
+// lh nwg is at most 3 CUs (one group of 32 rows; two: 2), or lh where that is more; a row's tiles are full but for its last one
 double tree_plan_limit(int nl, int N, int B, int H, int Hq, int d) {
   const int grp = Hq / H;
   double most = 0;
@@ -457,7 +443,7 @@ double tree_plan_limit(int nl, int N, int B, int H, int Hq, int d) {
     const int M = 32 * qt, heads = std::min(grp, M), nqc = (grp + heads - 1) / heads, tq = M / heads, rows = std::min(N, B);
     const double lh = double(nl) * H * nqc, ntile = std::min<double>(double(N) / tq + rows, N);
     const double parts = std::max(3.0 * cu_count(), lh) + lh * ntile;
-    most = std::max(most, 256.0 * 8 + sizeof(TreeTile) * ntile + 8.0 * cu_count() + lh * ntile * (qt * (d / 16) * 1024.0 + M * 4.0) +
+    most = std::max(most, 256.0 * 8 + sizeof(TreeTile) * ntile + 12.0 * cu_count() + lh * ntile * (qt * (d / 16) * 1024.0 + M * 4.0) +
                               parts * M * (d * 4.0 + 8.0));
   }
   return most;
