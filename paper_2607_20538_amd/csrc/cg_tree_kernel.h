@@ -14,9 +14,11 @@
 // Operands are binary16 as in the chunk attention (11 bits, cg_chunk_kernel.h), and a unit with zhat beyond it, an infinity or a NaN is
 // summed position by position in binary32, in a loop of its own behind the others (within theirs its registers spill).
 //
-// Bound by the issue of vector instructions beside the products.  A unit (32 positions, 64 query rows, 128 channels) costs a
-// wave about 430 vector instructions and 32 products, 1720 + 1050 cycles that two waves per SIMD overlap in part: about 4000
-// cycles a unit.  32 trees of 8 to 16 nodes behind up to 8192 positions, 8 KV heads x 4, 4 bits: 84 to 87 us over the positions
+// Bound by what a unit has to do in order, at two waves per SIMD.  A unit (32 positions, 64 query rows, 128 channels) is
+// about 430 vector instructions and 32 products, 1720 + 1050 cycles of its SIMD, and takes 4060 of them (8 long rows; 4980
+// where 32 shorter rows open and join more tiles): vector instructions issue in 46 (37)% of the cycles, products run in 28 (20)%.  A
+// wave has an instruction issued in 45 (40)% of its time, waits for its turn in 24 (19)%, and for results of LDS and of
+// products in 31 (40)%.  32 trees of 8 to 16 nodes behind up to 8192 positions, 8 KV heads x 4, 4 bits: 84 to 87 us over the positions
 // where the bytes take 30 and the products 28; a call 105, by the chunk attention's kernel with masks 237.  Codes become
 // binary16 by one conversion from 8-bit floating point for two (with a mask and a fused multiply-add 11 cycles of issue a
 // pair); 3 bits, four of them to a word after six byte permutations a run: 103 us where code by code it was 124 (24 trees
